@@ -132,7 +132,7 @@ def prepare(case, seed):
     if case["op"] == "step":
         w = torch.randn((n_blocks, BLOCK), generator=gen, device="cuda") * 0.05
         s["weight"] = laid_out(w if in_use is None else torch.where(in_use, w, torch.zeros_like(w)), case["weight"])
-        s["copy"] = torch.empty_like(s["weight"], dtype=TYPES[case["copy"]]) if case["copy"] else None
+        s["copy"] = torch.zeros_like(s["weight"], dtype=TYPES[case["copy"]]) if case["copy"] else None
         del w
         m = heavy((n_blocks, BLOCK)) * 0.25
         v = heavy((n_blocks, BLOCK)).square_() * 0.3 + m.square()
