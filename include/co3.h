@@ -379,6 +379,98 @@ int co3_balanced_split(const double* cost, const int32_t* seg, int64_t n, int32_
 int co3_moments_static(const float* grad, const float* residual, int64_t n, float gamma,
                        double* moments, void* cuda_stream);
 
+/* ---- The optimizer step on the averaged gradient ------------------------------------------------------
+ * (The paper's update is plain descent, co3_decode_aggregate_update; these calls are for training with AdamW.)
+ * AdamW over many tensors at once.  For every element of tensor l, with g' = info->factor * g:
+ *   m <- beta1 m + (1 - beta1) g'        v <- beta2 v + (1 - beta2) g'^2
+ *   w <- w - lr (decay_l w + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * where t counts the steps from 1.  Each product and sum of the two moments is rounded to 32 bits by itself, so the
+ * moments are the same bits wherever an element lies.  An element whose new v would not be below 2^126 (a gradient
+ * that is not finite, or beyond 1e19) keeps w, m and v, is counted, and raises CO3_FLAG_NONFINITE in
+ * co3_adamw_status.  If info->nonfinite is not 0 the whole step is left out and not counted as one: nothing changes.
+ *
+ * Tensors.  Weights, gradients and copies are given by one device pointer per tensor in host arrays, which are read
+ * before the call returns; the pointers may change from call to call and need only the alignment of their type, so
+ * the segments of a gradient row serve as they are.  Tensors may be empty.  The moments are one array each: tensor l
+ * starts at a multiple of 256 elements (the sum over the tensors before it of their sizes rounded up to 256), and
+ * places that belong to no element are neither read nor written, except that the 8-bit forms read them.
+ *
+ * 8-bit moments (state_bits = 8).  Codes of one byte, and per block of 256 elements of a tensor the exponent `top` of
+ * its largest magnitude, stored as a 32-bit float stores its own (at least 17 for m, 33 for v).
+ *   m: sign, 4 exponent bits e, 3 mantissa bits k (the (1,4,3) format of the conversion), exponent field 14 = top:
+ *      |m| = (8 + k) 2^(e-1) u, or k u for e = 0, with u = 2^(top-127-16);
+ *   v: 5 exponent bits, 3 mantissa bits, no sign, exponent field 30 = top, u = 2^(top-127-32).
+ * A new value goes to the grid point above it with the probability that its distance from the one below has (an
+ * average that moves by a tenth of a percent per step would stand still under rounding to nearest); a positive v
+ * never goes to 0.  The random bits are a function of (seed, t, place in the moment array) alone, so a run can be
+ * repeated.  Weights in bf16 are rounded in the same manner, with either kind of moments.
+ *
+ * The handle owns its tables and scratch (one allocation); no call after co3_adamw_create allocates device memory.
+ * Step count and bias corrections live on the device: co3_grad_norm and co3_adamw_step only enqueue kernels and may
+ * be captured into a graph and replayed (give the learning rate through d_lr where it changes).  Calls on one handle
+ * must be issued on one stream, or be ordered by the caller, and with the handle's device current. */
+typedef struct co3_adamw co3_adamw; /* opaque, library-owned */
+
+#define CO3_F32 0
+#define CO3_BF16 1
+#define CO3_F16 2
+#define CO3_NONE (-1)
+
+typedef struct {
+    int32_t n_tensors;    /* >= 1                                                                            */
+    const int64_t* sizes; /* host, elements per tensor, each >= 0; at most 2^31 - 1 blocks of 256 in all     */
+    const float* decay;   /* host, decay_l per tensor, or NULL: weight_decay for all                         */
+    int32_t weight_type;  /* CO3_F32 or CO3_BF16                                                             */
+    int32_t grad_type;    /* CO3_F32, CO3_BF16 or CO3_F16                                                    */
+    int32_t copy_type;    /* CO3_BF16 / CO3_F16: f32 weights are also written in that type; else CO3_NONE    */
+    int32_t state_bits;   /* 32 or 8                                                                         */
+    double beta1, beta2;  /* in [0, 1)                                                                       */
+    double eps, weight_decay;
+    uint32_t seed;        /* of the stochastic rounding                                                      */
+    int32_t reserved;     /* 0                                                                               */
+} co3_adamw_config;
+
+typedef struct {          /* the moments, device, caller-owned, zero before the first step                   */
+    void *m, *v;          /* [n_blocks][256] f32, or u8 codes; 32-byte aligned                               */
+    uint8_t *m_exp, *v_exp; /* [n_blocks], state_bits = 8 only                                               */
+} co3_adamw_state;
+
+typedef struct {          /* device, 16-byte aligned: written by co3_grad_norm (or by the caller), read by co3_adamw_step */
+    float factor;         /* what gradients are multiplied by                                                */
+    float norm;
+    uint64_t nonfinite;
+} co3_grad_info;
+
+int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg);
+void co3_adamw_destroy(co3_adamw* h);
+int co3_adamw_sizes(const co3_adamw* h, int64_t* n_blocks, int64_t* n_elements);
+
+/* L2 norm of all gradients together, of the finite elements: norm = |grad_scale| sqrt(sum g^2), and what the step is to
+ * multiply them by: factor = grad_scale min(1, max_norm / norm), or grad_scale if max_norm <= 0.  nonfinite counts the
+ * elements that are infinite or NaN.  tensor_norms: device [n_tensors] f32 or NULL, the same norm per tensor.
+ * Squares are formed without overflow or underflow for every finite gradient and summed in 64 bits in a fixed order:
+ * the same gradients give the same bits. */
+int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_scale, float max_norm, float* tensor_norms,
+                  co3_grad_info* info, void* cuda_stream);
+
+/* One step.  copies: NULL if copy_type is CO3_NONE.  d_lr: device f32 or NULL; takes the place of lr.  info: NULL means
+ * factor 1 and no check beforehand. */
+int co3_adamw_step(co3_adamw* h, void* const* weights, const void* const* grads, void* const* copies,
+                   const co3_adamw_state* state, double lr, const float* d_lr, const co3_grad_info* info,
+                   void* cuda_stream);
+
+/* What 8-bit moments stand for: device [n_blocks][256] each, 16-byte aligned, CO3_F32 or CO3_BF16 (exact in both: a
+ * code has four significant bits). */
+int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void* m_values, void* v_values, int32_t value_type,
+                     void* cuda_stream);
+
+/* Synchronising calls: sticky flags with the counts of elements and steps left out (clear != 0 resets all three);
+ * steps taken, to be stored beside the moments and set again when a run is resumed. */
+int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped_elements, uint64_t* skipped_steps, int32_t clear);
+int co3_adamw_steps_export(co3_adamw* h, int64_t* steps);
+int co3_adamw_steps_import(co3_adamw* h, int64_t steps);
+int64_t co3_adamw_launch_count(const co3_adamw* h);
+
 const char* co3_strerror(int code);
 
 #ifdef __cplusplus

@@ -29,6 +29,8 @@ EXPORTS = [
     "co3_profile_stride", "co3_tiled_begin", "co3_tiled_statistics", "co3_tiled_convert", "co3_tiled_finish",
     "co3_moments_export", "co3_moments_import", "co3_set_fit_override", "co3_debug_encode_stalled",
     "co3_model_checksum", "co3_balanced_split",
+    "co3_adamw_create", "co3_adamw_destroy", "co3_adamw_sizes", "co3_grad_norm", "co3_adamw_step", "co3_adamw_values",
+    "co3_adamw_status", "co3_adamw_steps_export", "co3_adamw_steps_import", "co3_adamw_launch_count",
 ]
 ELIMIT = -7
 STATIC_MAX_ELEMENTS = 1 << 29
@@ -46,6 +48,21 @@ class Config(C.Structure):
                 ("n_segments", C.c_int32), ("seg_offsets", C.POINTER(C.c_int64)),
                 ("gamma", C.c_float), ("bias_mode", C.c_int32), ("cap_words", C.c_int64),
                 ("bias_rule", C.c_int32), ("reserved", C.c_int32)]
+
+
+F32, BF16, F16, NONE = 0, 1, 2, -1
+STATE_BLOCK = 256          # elements of a tensor that share an exponent in 8-bit moments
+
+
+class AdamwConfig(C.Structure):
+    _fields_ = [("n_tensors", C.c_int32), ("sizes", C.POINTER(C.c_int64)), ("decay", C.POINTER(C.c_float)),
+                ("weight_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("state_bits", C.c_int32),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("seed", C.c_uint32), ("reserved", C.c_int32)]
+
+
+class AdamwState(C.Structure):
+    _fields_ = [("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p)]
 
 
 HDR_DTYPE = np.dtype([("bias", np.int8), ("ibeta", np.int8), ("ir", np.int16)])
@@ -140,6 +157,26 @@ def lib():
     L.co3_model_checksum.argtypes = [Format]
     L.co3_balanced_split.restype = C.c_int
     L.co3_balanced_split.argtypes = [vp, vp, C.c_int64, C.c_int32, C.c_int32, vp]
+    L.co3_adamw_create.restype = C.c_int
+    L.co3_adamw_create.argtypes = [C.POINTER(vp), C.POINTER(AdamwConfig)]
+    L.co3_adamw_destroy.restype = None
+    L.co3_adamw_destroy.argtypes = [vp]
+    L.co3_adamw_sizes.restype = C.c_int
+    L.co3_adamw_sizes.argtypes = [vp, i64p, i64p]
+    L.co3_grad_norm.restype = C.c_int
+    L.co3_grad_norm.argtypes = [vp, vp, C.c_float, C.c_float, vp, vp, vp]
+    L.co3_adamw_step.restype = C.c_int
+    L.co3_adamw_step.argtypes = [vp, vp, vp, vp, vp, C.c_double, vp, vp, vp]
+    L.co3_adamw_values.restype = C.c_int
+    L.co3_adamw_values.argtypes = [vp, vp, vp, vp, C.c_int32, vp]
+    L.co3_adamw_status.restype = C.c_int
+    L.co3_adamw_status.argtypes = [vp, C.POINTER(C.c_uint32), C.POINTER(C.c_uint64), C.POINTER(C.c_uint64), C.c_int32]
+    L.co3_adamw_steps_export.restype = C.c_int
+    L.co3_adamw_steps_export.argtypes = [vp, i64p]
+    L.co3_adamw_steps_import.restype = C.c_int
+    L.co3_adamw_steps_import.argtypes = [vp, C.c_int64]
+    L.co3_adamw_launch_count.restype = C.c_int64
+    L.co3_adamw_launch_count.argtypes = [vp]
     L.co3_strerror.restype = C.c_char_p
     L.co3_strerror.argtypes = [C.c_int]
     _lib = L
@@ -522,3 +559,223 @@ def hdr_from_numpy(hdr3, device="cuda"):
     raw = np.zeros(len(hdr3), HDR_DTYPE)
     raw["bias"], raw["ibeta"], raw["ir"] = hdr3[:, 0], hdr3[:, 1], hdr3[:, 2]
     return torch.from_numpy(raw.view(np.int32).copy()).to(device)
+
+
+# ---- optimizer: gradient norm and AdamW over many tensors ---------------------------------------------------------
+def _type_code(dtype):
+    import torch
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(dtype)
+    if code is None:
+        raise TypeError(f"float32, bfloat16 or float16 expected, got {dtype}")
+    return code
+
+
+def _dense(t):
+    """Whether the elements of t fill one piece of memory, in whatever order of dimensions."""
+    at = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def _order(t):
+    """The order in memory of t's elements: None for the usual one, else its sizes and strides."""
+    return None if t.is_contiguous() else tuple((n, st) for n, st in zip(t.shape, t.stride()) if n != 1)
+
+
+class TensorList:
+    """Tensors of one dtype whose pointers have been looked at and put into a host array once (GradNorm.bind_grads).  It keeps
+    the tensors; bind again after giving one of them other storage."""
+
+    def __init__(self, tensors, sizes, dtype, device, what, order=None):
+        self.tensors = list(tensors)
+        if len(self.tensors) != len(sizes):
+            raise ValueError(f"{len(sizes)} {what} expected, got {len(self.tensors)}")
+        for i, (t, n) in enumerate(zip(self.tensors, sizes)):
+            if t.dtype != dtype or t.device != device:
+                raise ValueError(f"{what} {i}: {dtype} on {device} expected, got {t.dtype} on {t.device}")
+            if t.numel() != n:
+                raise ValueError(f"{what} {i}: {n} elements expected, got {t.numel()}")
+            if n and not _dense(t):
+                raise ValueError(f"{what} {i}: its elements do not fill one piece of memory (shape {tuple(t.shape)}, strides {t.stride()})")
+            if order is not None and n and _order(t) != order[i]:
+                raise ValueError(f"{what} {i}: its elements lie in another order than those of its weights")
+        self.pointers = (C.c_void_p * len(sizes))(*[t.data_ptr() if n else None for t, n in zip(self.tensors, sizes)])
+
+
+class GradNorm:
+    """Gradient norm, clipping factor and count of non-finite elements of a set of tensors (co3_grad_norm), on the current
+    CUDA device.  `sizes`: elements per tensor."""
+
+    def __init__(self, sizes, grad_dtype=None):
+        import torch
+        self._create([int(n) for n in sizes], torch.float32, grad_dtype or torch.float32, None, 32, (0.0, 0.0), 0.0, 0.0, 0)
+
+    def _create(self, sizes, weight_dtype, grad_dtype, copy_dtype, state_bits, betas, eps, weight_decay, seed, device=None):
+        import torch
+        self.torch, self.sizes, self.grad_dtype = torch, sizes, grad_dtype
+        self._order = None
+        n = np.ascontiguousarray(sizes, np.int64)
+        per_tensor = None if np.ndim(weight_decay) == 0 else np.ascontiguousarray(weight_decay, np.float32)
+        if per_tensor is not None and per_tensor.shape != n.shape:
+            raise ValueError(f"weight_decay: one number, or one for each of the {len(n)} tensors")
+        cfg = AdamwConfig(len(n), n.ctypes.data_as(C.POINTER(C.c_int64)),
+                          None if per_tensor is None else per_tensor.ctypes.data_as(C.POINTER(C.c_float)),
+                          _type_code(weight_dtype), _type_code(grad_dtype), NONE if copy_dtype is None else _type_code(copy_dtype),
+                          int(state_bits), float(betas[0]), float(betas[1]), float(eps),
+                          float(weight_decay) if per_tensor is None else 0.0, int(seed) & 0xFFFFFFFF, 0)
+        h = C.c_void_p()
+        rc = lib().co3_adamw_create(C.byref(h), C.byref(cfg))
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_create")
+        self.handle = h
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        nb = C.c_int64()
+        lib().co3_adamw_sizes(h, C.byref(nb), None)
+        self.n_blocks = nb.value
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().co3_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _stream(self, stream, *tensors):
+        if stream is None:
+            return self.torch.cuda.current_stream(self.device).cuda_stream
+        for t in tensors:                     # the allocator must not hand their memory on while that stream uses it
+            if t is not None:
+                t.record_stream(stream)
+        return stream.cuda_stream
+
+    def bind_grads(self, grads):
+        """Check the gradient tensors and keep their pointers, for programs whose gradients stay where they are."""
+        return TensorList(grads, self.sizes, self.grad_dtype, self.device, "gradients", self._order)
+
+    def _grads(self, grads):
+        return grads if type(grads) is TensorList else self.bind_grads(grads)
+
+    def grad_norm(self, grads, info=None, max_norm=0.0, grad_scale=1.0, tensor_norms=None, stream=None):
+        """grads: the tensors, or what bind_grads returned.  info: 4 float32 on the device, written and returned: factor, norm,
+        and in the last two the count of non-finite elements as one int64 (`info[2:].view(torch.int64)`)."""
+        g = self._grads(grads)
+        if info is None:
+            info = self.torch.empty(4, dtype=self.torch.float32, device=self.device)
+        _check(info, self.torch.float32, 4, self.device, "info")
+        if tensor_norms is not None:
+            _check(tensor_norms, self.torch.float32, len(self.sizes), self.device, "tensor_norms")
+        s = self._stream(stream, info, tensor_norms, *(g.tensors if stream is not None else ()))
+        rc = lib().co3_grad_norm(self.handle, g.pointers, grad_scale, max_norm,
+                                 None if tensor_norms is None else tensor_norms.data_ptr(), info.data_ptr(), s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_grad_norm")
+        return info
+
+    def status(self, clear=False):
+        """(flags, elements left out, steps left out); synchronises."""
+        f, e, s = C.c_uint32(), C.c_uint64(), C.c_uint64()
+        rc = lib().co3_adamw_status(self.handle, C.byref(f), C.byref(e), C.byref(s), int(clear))
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_status")
+        return int(f.value), int(e.value), int(s.value)
+
+    def launch_count(self):
+        return int(lib().co3_adamw_launch_count(self.handle))
+
+
+def _check(t, dtype, n, device, what):
+    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous {dtype} on {device} expected, got {t.numel()} {t.dtype} on {t.device}")
+
+
+class AdamW(GradNorm):
+    """AdamW over the tensors `params` (float32 or bfloat16, on the current CUDA device, updated in place; any dense order of
+    dimensions, gradients and copies in the same).  copies: tensors of bfloat16 or float16 that receive the new float32 weights.
+    weight_decay: one number, or one per tensor.  state_bits: 32, or 8 for moments of one byte each (include/co3.h).
+    The moments are the attributes m, v (and m_exp, v_exp): [n_blocks][256]; `state` gives existing ones (set_steps then sets the
+    steps that they come from)."""
+
+    def __init__(self, params, grad_dtype=None, copies=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32,
+                 seed=0, state=None):
+        import torch
+        params = list(params)
+        if not params:
+            raise ValueError("no tensors")
+        sizes = [p.numel() for p in params]
+        dtype = params[0].dtype
+        copies = None if copies is None else list(copies)
+        if copies is not None and not copies:
+            raise ValueError("no copies")
+        self._create(sizes, dtype, grad_dtype or dtype, copies[0].dtype if copies else None, state_bits, betas, eps, weight_decay, seed)
+        self.lr, self.state_bits = float(lr), int(state_bits)
+        self.params = TensorList(params, sizes, dtype, self.device, "weights")
+        self._order = [_order(p) for p in params]
+        self.copies = None if copies is None else TensorList(copies, sizes, copies[0].dtype, self.device, "copies", self._order)
+        kind = torch.float32 if self.state_bits == 32 else torch.uint8
+        names = ("m", "v") if self.state_bits == 32 else ("m", "v", "m_exp", "v_exp")
+        for k in names:
+            shape = (self.n_blocks, STATE_BLOCK) if k in ("m", "v") else (self.n_blocks,)
+            t = torch.zeros(shape, dtype=kind, device=self.device) if state is None else state[k]
+            _check(t, kind, int(np.prod(shape)), self.device, k)
+            setattr(self, k, t)
+        self._state = AdamwState(*[getattr(self, k).data_ptr() if k in names else None for k in ("m", "v", "m_exp", "v_exp")])
+        self._state_p = C.byref(self._state)
+
+    def step(self, grads, info=None, lr=None, stream=None):
+        """One step.  info: what grad_norm returned (its factor multiplies the gradients, and nothing is changed if it counted
+        non-finite elements).  lr: a number, or one float32 on the device, in place of the optimizer's."""
+        g = self._grads(grads)
+        d_lr = None
+        if lr is None:
+            lr = self.lr
+        elif isinstance(lr, self.torch.Tensor):
+            _check(lr, self.torch.float32, 1, self.device, "lr")
+            d_lr, lr = lr, 0.0
+        if info is not None:
+            _check(info, self.torch.float32, 4, self.device, "info")
+        s = self._stream(stream, info, d_lr, *(self._all(g) if stream is not None else ()))
+        rc = lib().co3_adamw_step(self.handle, self.params.pointers, g.pointers, None if self.copies is None else self.copies.pointers,
+                                  self._state_p, lr, None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_step")
+
+    def _all(self, g):
+        state = [getattr(self, k) for k in ("m", "v", "m_exp", "v_exp") if hasattr(self, k)]
+        return g.tensors + self.params.tensors + (self.copies.tensors if self.copies else []) + state
+
+    def state_values(self, m_out=None, v_out=None, stream=None):
+        """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""
+        if m_out is None or v_out is None:
+            m_out, v_out = (self.torch.empty((self.n_blocks, STATE_BLOCK), dtype=self.torch.bfloat16, device=self.device) for _ in range(2))
+        for t, what in ((m_out, "m_out"), (v_out, "v_out")):
+            _check(t, m_out.dtype, self.n_blocks * STATE_BLOCK, self.device, what)
+        s = self._stream(stream, m_out, v_out, *([self.m, self.v, self.m_exp, self.v_exp] if stream is not None and self.state_bits == 8 else ()))
+        rc = lib().co3_adamw_values(self.handle, self._state_p, m_out.data_ptr(), v_out.data_ptr(), _type_code(m_out.dtype), s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_values")
+        return m_out, v_out
+
+    def moments_of(self, i):
+        """Views of the two moment arrays (codes with 8 bits) of tensor i, in the order in memory of its weights."""
+        b = sum((n + STATE_BLOCK - 1) // STATE_BLOCK for n in self.sizes[:i]) * STATE_BLOCK
+        return tuple(t.view(-1)[b:b + self.sizes[i]] for t in (self.m, self.v))
+
+    def steps(self):
+        """Steps taken so far (synchronises)."""
+        n = C.c_int64()
+        rc = lib().co3_adamw_steps_export(self.handle, C.byref(n))
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_steps_export")
+        return n.value
+
+    def set_steps(self, steps):
+        rc = lib().co3_adamw_steps_import(self.handle, int(steps))
+        if rc != OK:
+            raise Co3Error(rc, "co3_adamw_steps_import")
