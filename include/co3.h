@@ -459,7 +459,7 @@ int co3_adamw_step(co3_adamw* h, void* const* weights, const void* const* grads,
                    const co3_adamw_state* state, double lr, const float* d_lr, const co3_grad_info* info,
                    void* cuda_stream);
 
-/* What 8-bit moments stand for: device [n_blocks][256] each, 16-byte aligned, CO3_F32 or CO3_BF16 (exact in both: a
+/* What 8-bit moments stand for: device [n_blocks][256] each, 32-byte aligned, CO3_F32 or CO3_BF16 (exact in both: a
  * code has four significant bits). */
 int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void* m_values, void* v_values, int32_t value_type,
                      void* cuda_stream);

@@ -21,7 +21,8 @@ constexpr int PER_LANE = BLK / 32;
 constexpr int INLINE_TENSORS = 128;           // pointers of so many tensors travel with the launch itself
 constexpr int TABLE_TENSORS = 1300;           // ... and of so many with one launch of the kernel that fills the device table
 constexpr int MAX_TENSORS = 1 << 20;
-constexpr int NORM_WARPS = 4736;              // warps that the norm aims for: 148 SMs x 32
+constexpr int NORM_CTAS = 592;                // thread blocks of the norm at most: four on each of 148 SMs, whatever the device,
+                                              // so that a sum does not depend on where it is formed
 
 struct Pointers {
     const void* grad;
@@ -65,21 +66,66 @@ __device__ __forceinline__ uint32_t counter_bits(uint32_t key, uint32_t place) {
     const uint32_t s = key + place * 0x9E3779B9u;
     return (s ^ (s >> 15)) * 0x2C1B3C6Du;
 }
-__device__ __forceinline__ uint32_t key_of(uint32_t key, int64_t place) { return key + (uint32_t)(place >> 32) * 0x632BE5ABu; }
+// The key that makes counter_bits(block_key(key, place), i) the bits of `place` + i, for whole blocks at `place`.
+__device__ __forceinline__ uint32_t block_key(uint32_t key, int64_t place) {
+    return key + (uint32_t)(place >> 32) * 0x632BE5ABu + (uint32_t)place * 0x9E3779B9u;
+}
 
 __device__ __forceinline__ float pow2i(int e) {          // 2^e, -149 <= e <= 127
     return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << (e + 149));
 }
 
-template <typename T> __device__ __forceinline__ float to_f32(T x);
-template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-
-__device__ __forceinline__ float load_grad(const void* p, int64_t i, int type) {
-    if (type == CO3_F32) return static_cast<const float*>(p)[i];
-    if (type == CO3_BF16) return to_f32(static_cast<const __nv_bfloat16*>(p)[i]);
-    return to_f32(static_cast<const __half*>(p)[i]);
-}
+// A type of weights, gradients or copies: one element, and a lane's eight neighbouring ones in one access.
+struct F32 {
+    typedef float type;
+    static constexpr uintptr_t ALIGN = 31;
+    static __device__ __forceinline__ float to(float x) { return x; }
+    static __device__ __forceinline__ void load8(const float* p, float* x) {
+        asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
+    }
+    static __device__ __forceinline__ void store8(float* p, const float* x) {
+        asm volatile("st.global.v8.f32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                     :: "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "l"(p) : "memory");
+    }
+};
+struct Bf16 {
+    typedef __nv_bfloat16 type;
+    static constexpr uintptr_t ALIGN = 15;
+    static __device__ __forceinline__ float to(type x) { return __bfloat162float(x); }
+    static __device__ __forceinline__ void load8(const type* p, float* x) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ void store8(type* p, const float* x) {
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
+    }
+};
+struct F16 {
+    typedef __half type;
+    static constexpr uintptr_t ALIGN = 15;
+    static __device__ __forceinline__ float to(type x) { return __half2float(x); }
+    static __device__ __forceinline__ void load8(const type* p, float* x) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+            x[2 * k] = f.x; x[2 * k + 1] = f.y;
+        }
+    }
+    static __device__ __forceinline__ void store8(type* p, const float* x) {
+        __half2 h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = __floats2half2_rn(x[2 * k], x[2 * k + 1]);
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
+    }
+};
 
 // ---- 8-bit moments ---------------------------------------------------------------------------------------------------
 // A code is a float with three mantissa bits.  Its exponent field counts octaves up to that of the largest magnitude of the
@@ -88,6 +134,7 @@ __device__ __forceinline__ float load_grad(const void* p, int64_t i, int type) {
 // exponent bits, no sign (32 octaves: sixteen of its square root).  Scaled so that its grid lies at the lower end of the
 // 32-bit floats, a code IS the upper bits of the float, subnormal codes included, and both directions are a product and a shift.
 template <int TOP> struct Scale {
+    static constexpr int FIELD = TOP;
     static constexpr int LEAST = TOP + 3;                // smallest stored exponent: the grid stays within normal floats
     // 2^(top - TOP), as two factors since their product can leave the range
     static __device__ __forceinline__ float up1(int top) { return pow2i(top - 127); }
@@ -100,6 +147,34 @@ template <int TOP> struct Scale {
     // rand: 20 bits.  x goes to the grid point above it with the probability that its distance from the one below has.
     static __device__ __forceinline__ uint32_t encode(float x, int top, uint32_t rand) {
         return (__float_as_uint(__fmul_rn(__fmul_rn(x, down1(top)), down2())) + rand) >> 20;
+    }
+    // Eight codes of a lane, with the scale as one factor.
+    template <bool SIGNED> static __device__ __forceinline__ void decode8(uint2 c, float up, float* x) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t w = (k < 4 ? c.x : c.y) << (24 - 8 * (k & 3));      // the code on top
+            const uint32_t f = SIGNED ? (uint32_t)((int32_t)w >> 4) & 0x87F00000u : (w >> 4) & 0x0FF00000u;
+            x[k] = __fmul_rn(__uint_as_float(f), up);
+        }
+    }
+    // r: the counters; the first moment takes bits 0..19, the second 12..31.  The sum is formed four places up, so that the code
+    // ends on top of its word and moves into the packed word with one funnel shift.
+    template <bool SIGNED> static __device__ __forceinline__ uint2 encode8(const float* x, float down, const uint32_t* r) {
+        uint32_t pack[2] = {0, 0};
+#pragma unroll
+        for (int k = 7; k >= 0; --k) {
+            float y = __fmul_rn(x[k], down);
+            uint32_t z;
+            if (SIGNED) {
+                z = (__float_as_uint(y) << 4) + ((r[k] << 4) & 0x00FFFFF0u);
+                z = (z & 0x7FFFFFFFu) | (__float_as_uint(y) & 0x80000000u);
+            } else {
+                if (x[k] > 0.0f) y = fmaxf(y, 0x1p-129f);                      // code 1: never to zero
+                z = (__float_as_uint(y) << 4) + (r[k] >> 8);                   // bits 8..11 lie below what counts
+            }
+            pack[k >> 2] = __funnelshift_l(z, pack[k >> 2], 8);
+        }
+        return make_uint2(pack[0], pack[1]);
     }
 };
 using ScaleM = Scale<14>;
@@ -131,19 +206,180 @@ struct StepArgs {
     double beta1, beta2;
     float b1, a1, b2, a2, eps, lr;
     uint32_t seed;
-    int grad_type, copy_type;
+    int copy_type;
     Pointers inline_ptr[INLINE_TENSORS];
 };
 
-template <int BITS, bool W16>
-__global__ void __launch_bounds__(32 * WARPS) adamw_kernel(const __grid_constant__ StepArgs a) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float inv_c1 = a.sc->inv_c1, rsqrt_c2 = a.sc->rsqrt_c2;
+struct Step {                                 // what is the same for all elements of a block
+    float factor, rate, rsqrt_c2, decay;
+    uint32_t key;                             // key + place of the block, in the counters' sense
+};
+
+// An element whose second moment is not below this (or is no number) is left as it was.  The bound keeps the exponents
+// of 8-bit moments, and first moments with them, far from the end of the range.
+constexpr float V_LIMIT = 0x1p126f;
+// Up to these stored exponents the two factors of a scale can be multiplied beforehand.
+constexpr int M_TOP_PLAIN = 127 + ScaleM::FIELD, V_TOP_PLAIN = 127 + ScaleV::FIELD;
+
+__device__ __forceinline__ void moments(float& m, float& v, float g, const StepArgs& a) {
+    m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.a1));
+    v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.a2));
+}
+
+// Root and quotient to two units in the last place: 2^-22 of the update, itself a small part of the weight.
+__device__ __forceinline__ float new_weight(float w, float m, float v, const Step& s, float eps) {
+    float root;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
+    return w - __fmaf_rn(w, s.decay, __fdividef(m * s.rate, __fmaf_rn(root, s.rsqrt_c2, eps)));
+}
+
+// The general way for one block: any alignment, any count, any values.  Lane i takes the elements i, i + 32, ...
+template <int BITS, class W, class G>
+__device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, const Pointers& p, int64_t b, int64_t e0, int n) {
+    const int lane = threadIdx.x & 31;
+    const int64_t place = b * BLK;
+    typename W::type* pw = static_cast<typename W::type*>(p.weight) + e0;
+    const typename G::type* pg = static_cast<const typename G::type*>(p.grad) + e0;
+    float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
+    uint32_t kept = 0;
+#pragma unroll
+    for (int k = 0; k < PER_LANE; ++k) {
+        const int i = lane + 32 * k;
+        g[k] = i < n ? G::to(pg[i]) : 0.0f;
+        w[k] = i < n ? W::to(pw[i]) : 0.0f;
+        if (BITS == 32) {
+            m[k] = i < n ? static_cast<const float*>(a.m)[place + i] : 0.0f;
+            v[k] = i < n ? static_cast<const float*>(a.v)[place + i] : 0.0f;
+        } else {
+            const uint32_t c = static_cast<const uint8_t*>(a.m)[place + i];
+            m[k] = ScaleM::decode(c & 127u, a.m_exp[b]);
+            if (c & 128u) m[k] = -m[k];
+            v[k] = ScaleV::decode(static_cast<const uint8_t*>(a.v)[place + i], a.v_exp[b]);
+            if (i >= n) m[k] = v[k] = 0.0f;
+        }
+    }
+    float m_max = 0.0f, v_max = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PER_LANE; ++k) {
+        const int i = lane + 32 * k;
+        float m1 = m[k], v1 = v[k];
+        moments(m1, v1, __fmul_rn(g[k], s.factor), a);
+        if (v1 < V_LIMIT) {
+            m[k] = m1;
+            v[k] = v1;
+            w[k] = new_weight(w[k], m1, v1, s, a.eps);
+            if (i < n) {
+                if (sizeof(typename W::type) == 2) reinterpret_cast<__nv_bfloat16*>(pw)[i] = bf16_stochastic(w[k], counter_bits(s.key, (uint32_t)i) >> 10);
+                else reinterpret_cast<float*>(pw)[i] = w[k];
+            }
+        } else {
+            ++kept;                                       // never one of the places past n: their moments are 0
+        }
+        if (i < n) {
+            if (a.copy_type == CO3_BF16) static_cast<__nv_bfloat16*>(p.copy)[e0 + i] = __float2bfloat16_rn(w[k]);
+            if (a.copy_type == CO3_F16) static_cast<__half*>(p.copy)[e0 + i] = __float2half_rn(w[k]);
+            if (BITS == 32) {
+                static_cast<float*>(a.m)[place + i] = m[k];
+                static_cast<float*>(a.v)[place + i] = v[k];
+            }
+        }
+        m_max = fmaxf(m_max, fabsf(m[k]));
+        v_max = fmaxf(v_max, v[k]);
+    }
+    if (BITS == 8) {
+        const int m_top = warp_top(m_max, ScaleM::LEAST), v_top = warp_top(v_max, ScaleV::LEAST);
+        if (lane == 0) { a.m_exp[b] = (uint8_t)m_top; a.v_exp[b] = (uint8_t)v_top; }
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) {
+            const int i = lane + 32 * k;
+            const uint32_t r = counter_bits(s.key, (uint32_t)i);
+            uint32_t c = ScaleM::encode(fabsf(m[k]), m_top, r & 0xFFFFFu);
+            if (m[k] < 0.0f) c |= 128u;
+            if (i < n) static_cast<uint8_t*>(a.m)[place + i] = (uint8_t)c;
+            c = ScaleV::encode(v[k], v_top, r >> 12);
+            if (c == 0 && v[k] > 0.0f) c = 1;
+            if (i < n) static_cast<uint8_t*>(a.v)[place + i] = (uint8_t)c;
+        }
+    }
+    return kept;
+}
+
+// The usual way: a whole block whose tensors are aligned.  Lane i takes the elements 8i .. 8i + 7, each array in one access.
+// Returns false, before anything is written, if a value needs the general way.
+template <int BITS, class W, class G>
+__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, const Pointers& p, int64_t b, int64_t e0) {
+    const int lane = threadIdx.x & 31;
+    const int64_t at = b * BLK + PER_LANE * lane;
+    typename W::type* pw = static_cast<typename W::type*>(p.weight) + e0 + PER_LANE * lane;
+    float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
+    G::load8(static_cast<const typename G::type*>(p.grad) + e0 + PER_LANE * lane, g);
+    W::load8(pw, w);
+    if (BITS == 32) {
+        F32::load8(static_cast<const float*>(a.m) + at, m);
+        F32::load8(static_cast<const float*>(a.v) + at, v);
+    } else {
+        const uint2 cm = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + at);
+        const uint2 cv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + at);
+        const int m_top = a.m_exp[b], v_top = a.v_exp[b];
+        if (m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN) return false;
+        ScaleM::decode8<true>(cm, pow2i(m_top - ScaleM::FIELD), m);
+        ScaleV::decode8<false>(cv, pow2i(v_top - ScaleV::FIELD), v);
+    }
+    uint32_t v_max = 0;
+    float m_max = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PER_LANE; ++k) {
+        moments(m[k], v[k], __fmul_rn(g[k], s.factor), a);
+        v_max = max(v_max, __float_as_uint(v[k]));        // as whole numbers: NaN of either sign is above the limit too
+        if (BITS == 8) m_max = fmaxf(m_max, fabsf(m[k]));
+        w[k] = new_weight(w[k], m[k], v[k], s, a.eps);
+    }
+    int m_top = 0, v_top = 0;
+    if (BITS == 8) {
+        v_max = __reduce_max_sync(0xffffffffu, v_max);
+        v_top = max((int)(v_max >> 23), ScaleV::LEAST);
+        m_top = warp_top(m_max, ScaleM::LEAST);
+        if (v_max >= __float_as_uint(V_LIMIT) || m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN) return false;
+    } else if (__any_sync(0xffffffffu, v_max >= __float_as_uint(V_LIMIT))) {
+        return false;
+    }
+    uint32_t r[PER_LANE];
+    if (BITS == 8 || sizeof(typename W::type) == 2) {
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) r[k] = counter_bits(s.key, (uint32_t)(PER_LANE * lane + k));
+    }
+    if (sizeof(typename W::type) == 2) {
+        uint32_t h[PER_LANE];
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) h[k] = __bfloat16_as_ushort(bf16_stochastic(w[k], r[k] >> 10));
+        *reinterpret_cast<uint4*>(pw) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    } else {
+        F32::store8(reinterpret_cast<float*>(pw), w);
+        if (a.copy_type == CO3_BF16) Bf16::store8(static_cast<__nv_bfloat16*>(p.copy) + e0 + PER_LANE * lane, w);
+        if (a.copy_type == CO3_F16) F16::store8(static_cast<__half*>(p.copy) + e0 + PER_LANE * lane, w);
+    }
+    if (BITS == 32) {
+        F32::store8(static_cast<float*>(a.m) + at, m);
+        F32::store8(static_cast<float*>(a.v) + at, v);
+    } else {
+        if (lane == 0) { a.m_exp[b] = (uint8_t)m_top; a.v_exp[b] = (uint8_t)v_top; }
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + at) = ScaleM::encode8<true>(m, pow2i(ScaleM::FIELD - m_top), r);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + at) = ScaleV::encode8<false>(v, pow2i(ScaleV::FIELD - v_top), r);
+    }
+    return true;
+}
+
+template <int BITS, class W, class G>
+__global__ void __launch_bounds__(32 * WARPS, 3) adamw_kernel(const __grid_constant__ StepArgs a) {
+    const int warp = threadIdx.x >> 5;
+    const float inv_c1 = a.sc->inv_c1;
     const uint32_t step_key = a.sc->key;
     const bool skip = a.info && a.info->nonfinite != 0;
-    const float factor = a.info ? a.info->factor : 1.0f;
     const float lr = a.d_lr ? *a.d_lr : a.lr;
-    const float rate = lr * inv_c1;
+    Step s;
+    s.factor = a.info ? a.info->factor : 1.0f;
+    s.rate = lr * inv_c1;
+    s.rsqrt_c2 = a.sc->rsqrt_c2;
     __syncthreads();                                      // every thread has read what the last block changes below
     uint32_t kept = 0;
     if (!skip) {
@@ -151,69 +387,12 @@ __global__ void __launch_bounds__(32 * WARPS) adamw_kernel(const __grid_constant
             const int t = a.owner[b];
             const Tensor tn = a.tensors[t];
             const Pointers p = a.table ? a.table[t] : a.inline_ptr[t];
-            const int64_t e0 = (b - tn.block0) * BLK, place = b * BLK;
+            const int64_t e0 = (b - tn.block0) * BLK;
             const int n = (int)(tn.size - e0 < BLK ? tn.size - e0 : BLK);
-            const float decay = lr * tn.decay;
-            const uint32_t key = key_of(step_key, place);
-            float m[PER_LANE], v[PER_LANE];
-            int m_top = 0, v_top = 0;
-            if (BITS == 8) { m_top = a.m_exp[b]; v_top = a.v_exp[b]; }
-            float m_max = 0.0f, v_max = 0.0f;
-#pragma unroll
-            for (int k = 0; k < PER_LANE; ++k) {
-                const int i = lane + 32 * k;
-                m[k] = v[k] = 0.0f;
-                if (i >= n) continue;
-                const float g = __fmul_rn(load_grad(p.grad, e0 + i, a.grad_type), factor);
-                float w = W16 ? to_f32(static_cast<const __nv_bfloat16*>(p.weight)[e0 + i]) : static_cast<const float*>(p.weight)[e0 + i];
-                float m0, v0;
-                if (BITS == 8) {
-                    const uint32_t c = static_cast<const uint8_t*>(a.m)[place + i];
-                    m0 = ScaleM::decode(c & 127u, m_top);
-                    if (c & 128u) m0 = -m0;
-                    v0 = ScaleV::decode(static_cast<const uint8_t*>(a.v)[place + i], v_top);
-                } else {
-                    m0 = static_cast<const float*>(a.m)[place + i];
-                    v0 = static_cast<const float*>(a.v)[place + i];
-                }
-                const float m1 = __fadd_rn(__fmul_rn(m0, a.b1), __fmul_rn(g, a.a1));
-                const float v1 = __fadd_rn(__fmul_rn(v0, a.b2), __fmul_rn(__fmul_rn(g, g), a.a2));
-                const bool fine = v1 < 0x1p126f;          // also false for NaN
-                m[k] = fine ? m1 : m0;
-                v[k] = fine ? v1 : v0;
-                if (!fine) { ++kept; }
-                else {
-                    w = w - (w * decay + rate * m1 / (sqrtf(v1) * rsqrt_c2 + a.eps));
-                    if (W16) static_cast<__nv_bfloat16*>(p.weight)[e0 + i] = bf16_stochastic(w, counter_bits(key, (uint32_t)(place + i)) >> 10);
-                    else static_cast<float*>(p.weight)[e0 + i] = w;
-                }
-                if (a.copy_type == CO3_BF16) static_cast<__nv_bfloat16*>(p.copy)[e0 + i] = __float2bfloat16_rn(w);
-                if (a.copy_type == CO3_F16) static_cast<__half*>(p.copy)[e0 + i] = __float2half_rn(w);
-                if (BITS == 8) {
-                    m_max = fmaxf(m_max, fabsf(m[k]));
-                    v_max = fmaxf(v_max, v[k]);
-                } else {
-                    static_cast<float*>(a.m)[place + i] = m[k];
-                    static_cast<float*>(a.v)[place + i] = v[k];
-                }
-            }
-            if (BITS == 8) {
-                m_top = warp_top(m_max, ScaleM::LEAST);
-                v_top = warp_top(v_max, ScaleV::LEAST);
-                if (lane == 0) { a.m_exp[b] = (uint8_t)m_top; a.v_exp[b] = (uint8_t)v_top; }
-#pragma unroll
-                for (int k = 0; k < PER_LANE; ++k) {
-                    const int i = lane + 32 * k;
-                    if (i >= n) continue;
-                    const uint32_t r = counter_bits(key, (uint32_t)(place + i));
-                    uint32_t c = ScaleM::encode(fabsf(m[k]), m_top, r & 0xFFFFFu);
-                    if (m[k] < 0.0f) c |= 128u;
-                    static_cast<uint8_t*>(a.m)[place + i] = (uint8_t)c;
-                    c = ScaleV::encode(v[k], v_top, r >> 12);
-                    if (c == 0 && v[k] > 0.0f) c = 1;
-                    static_cast<uint8_t*>(a.v)[place + i] = (uint8_t)c;
-                }
-            }
+            s.decay = lr * tn.decay;
+            s.key = block_key(step_key, b * BLK);
+            const uintptr_t off = ((uintptr_t)p.weight & W::ALIGN) | ((uintptr_t)p.grad & G::ALIGN) | ((uintptr_t)p.copy & 15);
+            if (n < BLK || off || !block_whole<BITS, W, G>(a, s, p, b, e0)) kept += block_any<BITS, W, G>(a, s, p, b, e0, n);
         }
     }
     if (kept) {                                           // rare: elements left as they were
@@ -228,31 +407,31 @@ __global__ void __launch_bounds__(32 * WARPS) adamw_kernel(const __grid_constant
                 atomicOr(&a.sc->flags, CO3_FLAG_NONFINITE);
                 a.sc->skipped_steps += 1;
             } else {
-                Scalars s = *a.sc;
-                s.steps += 1;
-                s.pow1 *= a.beta1;
-                s.pow2 *= a.beta2;
-                next_scalars(s, a.beta1, a.beta2, a.seed);
-                a.sc->steps = s.steps; a.sc->pow1 = s.pow1; a.sc->pow2 = s.pow2;
-                a.sc->inv_c1 = s.inv_c1; a.sc->rsqrt_c2 = s.rsqrt_c2; a.sc->key = s.key;
+                Scalars n = *a.sc;
+                n.steps += 1;
+                n.pow1 *= a.beta1;
+                n.pow2 *= a.beta2;
+                next_scalars(n, a.beta1, a.beta2, a.seed);
+                a.sc->steps = n.steps; a.sc->pow1 = n.pow1; a.sc->pow2 = n.pow2;
+                a.sc->inv_c1 = n.inv_c1; a.sc->rsqrt_c2 = n.rsqrt_c2; a.sc->key = n.key;
             }
         }
     }
 }
 
 // ---- gradient norm ------------------------------------------------------------------------------------------------------
-// Warp q takes the blocks q*K .. q*K + K-1 and leaves one partial sum for every tensor that it meets, at slot q + tensor
-// (going on to the next warp or to the next tensor moves one slot on, so the slots are all different and those of a tensor
-// lie side by side).  The thread block that finishes last adds them up, always in the same order.
+// Thread block c takes the blocks c*K .. c*K + K-1, warp w an eighth of them in a row, and leaves one partial sum for every
+// tensor that it meets, at slot c + tensor: going on to the next thread block or to the next tensor moves at least one slot on,
+// so the slots are all different, and those of a tensor lie side by side.  Slots that nothing maps to stay zero.  The thread
+// block that finishes last adds them up, always in the same order.
 struct NormArgs {
     const Tensor* tensors;
     const int32_t* owner;
     const Pointers* table;
-    int64_t n_blocks;
-    int n_tensors, per_warp, grad_type;
+    int64_t n_blocks, per_cta;
+    int n_tensors, n_slots;
     float grad_scale, max_norm;
     double* slots;
-    double* sums;                             // per tensor
     unsigned long long* bad;                  // per thread block
     float* tensor_norms;
     co3_grad_info* info;
@@ -260,7 +439,11 @@ struct NormArgs {
     Pointers inline_ptr[INLINE_TENSORS];
 };
 
-__device__ __forceinline__ double warp_sum(double x) {
+constexpr int NORM_UNROLL = 4;                // blocks whose loads a warp has in flight
+constexpr int NORM_STAGE = 2048;              // slots that the last thread block brings into shared memory
+
+template <typename T>
+__device__ __forceinline__ T warp_sum(T x) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
@@ -268,51 +451,123 @@ __device__ __forceinline__ double warp_sum(double x) {
 
 template <typename T>
 __device__ __forceinline__ T block_sum(T x, T* sh) {      // same value in every thread
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    x = warp_sum(x);
     __syncthreads();
-    if (lane == 0) sh[warp] = x;
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
     __syncthreads();
     T s = 0;
+#pragma unroll
     for (int w = 0; w < WARPS; ++w) s += sh[w];
     return s;
 }
 
-__global__ void __launch_bounds__(32 * WARPS) norm_kernel(const __grid_constant__ NormArgs a) {
-    __shared__ double sh[WARPS];
-    __shared__ unsigned long long sh_n[WARPS];
-    __shared__ bool last;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t q = (int64_t)blockIdx.x * WARPS + warp;
-    const int64_t b0 = q * a.per_warp, b1 = b0 + a.per_warp < a.n_blocks ? b0 + a.per_warp : a.n_blocks;
-    unsigned long long bad = 0;
-    int t = -1;
-    double s = 0.0;
-    for (int64_t b = b0; b < b1; ++b) {
-        const int tb = a.owner[b];
-        if (tb != t) {
-            if (t >= 0) { s = warp_sum(s); if (lane == 0) a.slots[q + t] = s; }
-            t = tb;
-            s = 0.0;
+// The square of a 32-bit float is exact in 64 bits: no range is lost, and the sum rounds at 2^-53.
+__device__ __forceinline__ void add_squares(const float* x, double& s0, double& s1, uint32_t& bad) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < PER_LANE; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+    if (top < 0x7F800000u) {
+#pragma unroll
+        for (int k = 0; k < PER_LANE; k += 2) {
+            const double d0 = (double)x[k], d1 = (double)x[k + 1];
+            s0 = __fma_rn(d0, d0, s0);
+            s1 = __fma_rn(d1, d1, s1);
         }
-        const Tensor tn = a.tensors[t];
-        const void* g = (a.table ? a.table[t] : a.inline_ptr[t]).grad;
-        const int64_t e0 = (b - tn.block0) * BLK;
-        const int n = (int)(tn.size - e0 < BLK ? tn.size - e0 : BLK);
+    } else {
 #pragma unroll
         for (int k = 0; k < PER_LANE; ++k) {
-            const int i = lane + 32 * k;
-            if (i >= n) continue;
-            const float x = load_grad(g, e0 + i, a.grad_type);
-            if (!(fabsf(x) < INFINITY)) { ++bad; continue; }
-            const double d = (double)x;
-            s = __fma_rn(d, d, s);
+            if ((__float_as_uint(x[k]) & 0x7FFFFFFFu) >= 0x7F800000u) { ++bad; continue; }
+            const double d = (double)x[k];
+            s0 = __fma_rn(d, d, s0);
         }
     }
-    if (t >= 0) { s = warp_sum(s); if (lane == 0) a.slots[q + t] = s; }
-    bad = block_sum(bad, sh_n);
-    if (threadIdx.x == 0) a.bad[blockIdx.x] = bad;
+}
+
+template <class G, bool ALIGNED>
+__device__ __forceinline__ void load_block(const typename G::type* g, float* x) {
+    const int lane = threadIdx.x & 31;
+    if (ALIGNED) {
+        G::load8(g + PER_LANE * lane, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) x[k] = G::to(g[lane + 32 * k]);
+    }
+}
+
+// `count` blocks of one tensor from element e0 on, the last of them perhaps not whole.
+template <class G, bool ALIGNED>
+__device__ __forceinline__ double squares(const typename G::type* g, int64_t e0, int64_t count, int64_t size, uint32_t& bad) {
+    const int lane = threadIdx.x & 31;
+    double s0 = 0.0, s1 = 0.0;
+    const int64_t whole = min(count, (size - e0) / BLK);
+    g += e0;
+    int64_t k = 0;
+    for (; k + NORM_UNROLL <= whole; k += NORM_UNROLL, g += NORM_UNROLL * BLK) {
+        float x[NORM_UNROLL][PER_LANE];
+#pragma unroll
+        for (int u = 0; u < NORM_UNROLL; ++u) load_block<G, ALIGNED>(g + u * BLK, x[u]);
+#pragma unroll
+        for (int u = 0; u < NORM_UNROLL; ++u) add_squares(x[u], s0, s1, bad);
+    }
+    for (; k < whole; ++k, g += BLK) {
+        float x[PER_LANE];
+        load_block<G, ALIGNED>(g, x);
+        add_squares(x, s0, s1, bad);
+    }
+    if (whole < count) {
+        const int n = (int)(size - e0 - whole * BLK);
+        float x[PER_LANE];
+#pragma unroll
+        for (int j = 0; j < PER_LANE; ++j) x[j] = lane + 32 * j < n ? G::to(g[lane + 32 * j]) : 0.0f;
+        add_squares(x, s0, s1, bad);
+    }
+    return s0 + s1;
+}
+
+template <class G>
+__global__ void __launch_bounds__(32 * WARPS, 4) norm_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ double sh[WARPS], edge_sum[2 * WARPS], stage[NORM_STAGE];
+    __shared__ unsigned long long sh_n[WARPS];
+    __shared__ int edge[2 * WARPS];           // tensors of the warps' first and last sums, which neighbours may share; -1: none
+    __shared__ bool last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c0 = blockIdx.x * a.per_cta, c1 = min(c0 + a.per_cta, a.n_blocks);
+    const int64_t b1 = min(c0 + (warp + 1) * a.per_cta / WARPS, c1);
+    if (threadIdx.x < 2 * WARPS) edge[threadIdx.x] = -1;
+    __syncthreads();
+    uint32_t bad = 0;
+    bool first = true;
+    for (int64_t b = c0 + warp * a.per_cta / WARPS; b < b1;) {
+        const int t = a.owner[b];
+        const Tensor tn = a.tensors[t];
+        const typename G::type* g = static_cast<const typename G::type*>((a.table ? a.table[t] : a.inline_ptr[t]).grad);
+        const int64_t end = min(b1, tn.block0 + (tn.size + BLK - 1) / BLK);
+        const int64_t e0 = (b - tn.block0) * BLK;
+        double s = (uintptr_t)g & G::ALIGN ? squares<G, false>(g, e0, end - b, tn.size, bad) : squares<G, true>(g, e0, end - b, tn.size, bad);
+        s = warp_sum(s);
+        b = end;
+        if (lane == 0) {
+            if (first || b == b1) { const int k = 2 * warp + (first ? 0 : 1); edge[k] = t; edge_sum[k] = s; }
+            else a.slots[blockIdx.x + t] = s;             // begins and ends within this warp's blocks
+        }
+        first = false;
+    }
+    const unsigned long long n_bad = block_sum((unsigned long long)bad, sh_n);       // its barriers also order edge[]
+    if (threadIdx.x == 0) {
+        a.bad[blockIdx.x] = n_bad;
+        int t = -1;
+        double s = 0.0;
+        for (int k = 0; k < 2 * WARPS; ++k) {             // neighbours with the same tensor add up
+            if (edge[k] < 0) continue;
+            if (edge[k] != t) {
+                if (t >= 0) a.slots[blockIdx.x + t] = s;
+                t = edge[k];
+                s = 0.0;
+            }
+            s += edge_sum[k];
+        }
+        if (t >= 0) a.slots[blockIdx.x + t] = s;
+    }
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) last = atomicAdd(&a.sc->norm_ticket, 1u) == gridDim.x - 1;
@@ -321,54 +576,70 @@ __global__ void __launch_bounds__(32 * WARPS) norm_kernel(const __grid_constant_
     __threadfence();
 
     double total = 0.0;
-    for (int t0 = 0; t0 < a.n_tensors; t0 += WARPS) {     // one tensor per warp
-        const int u = t0 + warp;
-        double x = 0.0;
-        if (u < a.n_tensors && a.tensors[u].size > 0) {
-            const int64_t f = a.tensors[u].block0, l = f + (a.tensors[u].size - 1) / BLK;
-            for (int64_t k = f / a.per_warp + u + lane; k <= l / a.per_warp + u; k += 32) x += __ldcg(&a.slots[k]);
-        }
-        x = warp_sum(x);
-        if (u < a.n_tensors && lane == 0) {
-            a.sums[u] = x;
-            if (a.tensor_norms) a.tensor_norms[u] = (float)(sqrt(x) * fabs((double)a.grad_scale));
-        }
+    for (int k = threadIdx.x; k < a.n_slots; k += 32 * WARPS) {
+        const double x = __ldcg(&a.slots[k]);
+        total += x;
+        if (k < NORM_STAGE) stage[k] = x;
     }
-    __syncthreads();
-    for (int u = threadIdx.x; u < a.n_tensors; u += 32 * WARPS) total += a.sums[u];
+    unsigned long long all_bad = 0;
+    for (unsigned k = threadIdx.x; k < gridDim.x; k += 32 * WARPS) all_bad += __ldcg(&a.bad[k]);
     total = block_sum(total, sh);
-    bad = 0;
-    for (unsigned k = threadIdx.x; k < gridDim.x; k += 32 * WARPS) bad += __ldcg(&a.bad[k]);
-    bad = block_sum(bad, sh_n);
+    all_bad = block_sum(all_bad, sh_n);
     if (threadIdx.x == 0) {
         const double norm = sqrt(total) * fabs((double)a.grad_scale);
         double factor = a.grad_scale;
         if (a.max_norm > 0.0f && norm > (double)a.max_norm) factor *= (double)a.max_norm / norm;
         a.info->factor = (float)factor;
         a.info->norm = (float)norm;
-        a.info->nonfinite = bad;
+        a.info->nonfinite = all_bad;
         a.sc->norm_ticket = 0;
+    }
+    if (!a.tensor_norms) return;
+    auto slot = [&](int k) { return k < NORM_STAGE ? stage[k] : __ldcg(&a.slots[k]); };
+    const double scale = fabs((double)a.grad_scale);
+    for (int t0 = warp * 32; t0 < a.n_tensors; t0 += 32 * WARPS) {
+        // a lane per tensor; those with many slots are then added by the whole warp
+        const int t = t0 + lane;
+        int k0 = 0, k1 = 0;
+        if (t < a.n_tensors) {
+            const Tensor tn = a.tensors[t];
+            if (tn.size > 0) {
+                k0 = (int)(tn.block0 / a.per_cta) + t;
+                k1 = (int)((tn.block0 + (tn.size - 1) / BLK) / a.per_cta) + t + 1;
+            }
+        }
+        const bool many = k1 - k0 > 8;
+        double x = 0.0;
+        if (!many) for (int k = k0; k < k1; ++k) x += slot(k);
+        for (uint32_t left = __ballot_sync(0xffffffffu, many); left; left &= left - 1) {
+            const int who = __ffs(left) - 1, f = __shfl_sync(0xffffffffu, k0, who), l = __shfl_sync(0xffffffffu, k1, who);
+            double y = 0.0;
+            for (int k = f + lane; k < l; k += 32) y += slot(k);
+            y = warp_sum(y);
+            if (lane == who) x = y;
+        }
+        if (t < a.n_tensors) a.tensor_norms[t] = (float)(sqrt(x) * scale);
     }
 }
 
 // ---- values of the 8-bit moments, and the tables ---------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ T from_f32(float x);
-template <> __device__ __forceinline__ float from_f32(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
-
-template <typename T>
+template <class T>
 __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp,
-                                                            int64_t n_blocks, T* m_out, T* v_out) {
+                                                            int64_t n_blocks, typename T::type* m_out, typename T::type* v_out) {
     const int lane = threadIdx.x & 31;
     for (int64_t b = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5); b < n_blocks; b += (int64_t)gridDim.x * WARPS) {
         const int m_top = m_exp[b], v_top = v_exp[b];
+        const int64_t at = b * BLK + PER_LANE * lane;
+        float x[PER_LANE];
 #pragma unroll
-        for (int k = 0; k < PER_LANE; ++k) {
-            const int64_t i = b * BLK + lane + 32 * k;
-            const uint32_t c = m[i];
-            const float x = ScaleM::decode(c & 127u, m_top);
-            m_out[i] = from_f32<T>(c & 128u ? -x : x);
-            v_out[i] = from_f32<T>(ScaleV::decode(v[i], v_top));
+        for (int which = 0; which < 2; ++which) {
+            const uint2 c = *reinterpret_cast<const uint2*>((which ? v : m) + at);
+            // the second factor is 1 but for the largest exponents, which one factor cannot hold
+            const int top = which ? v_top : m_top, most = which ? V_TOP_PLAIN : M_TOP_PLAIN, more = top > most ? top - most : 0;
+            if (which) ScaleV::decode8<false>(c, pow2i(top - more - ScaleV::FIELD), x);
+            else ScaleM::decode8<true>(c, pow2i(top - more - ScaleM::FIELD), x);
+            if (more) for (int k = 0; k < PER_LANE; ++k) x[k] *= pow2i(more);
+            T::store8((which ? v_out : m_out) + at, x);
         }
     }
 }
@@ -398,17 +669,17 @@ int width_of(int type) { return type == CO3_F32 ? 4 : 2; }
 }  // namespace
 
 struct co3_adamw {
-    int n_tensors, weight_type, grad_type, copy_type, state_bits, device, num_sms, per_warp, norm_grid;
+    int n_tensors, weight_type, grad_type, copy_type, state_bits, device, num_sms, norm_grid, n_slots;
     double beta1, beta2, eps;
     uint32_t seed;
-    int64_t n_blocks, n_elements;
+    int64_t n_blocks, n_elements, per_cta;
     int64_t* sizes;
     void* slab;                               // one device allocation:
     Tensor* tensors;
     int32_t* owner;
     Pointers* table;                          // only with more than INLINE_TENSORS tensors
     Scalars* sc;
-    double *slots, *sums;
+    double* slots;
     unsigned long long* bad;
     int64_t launches;
 };
@@ -453,9 +724,11 @@ int place_pointers(co3_adamw* h, const void* const* grads, void* const* weights,
     return rc;
 }
 
-template <int BITS, bool W16>
+template <int BITS, class W>
 int launch_step(co3_adamw* h, const StepArgs& a, int grid, cudaStream_t st) {
-    adamw_kernel<BITS, W16><<<grid, 32 * WARPS, 0, st>>>(a);
+    if (h->grad_type == CO3_F32) adamw_kernel<BITS, W, F32><<<grid, 32 * WARPS, 0, st>>>(a);
+    else if (h->grad_type == CO3_BF16) adamw_kernel<BITS, W, Bf16><<<grid, 32 * WARPS, 0, st>>>(a);
+    else adamw_kernel<BITS, W, F16><<<grid, 32 * WARPS, 0, st>>>(a);
     return launched(h, 1);
 }
 
@@ -495,11 +768,11 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
     h->weight_type = cfg->weight_type; h->grad_type = cfg->grad_type; h->copy_type = cfg->copy_type; h->state_bits = cfg->state_bits;
     h->beta1 = cfg->beta1; h->beta2 = cfg->beta2; h->eps = cfg->eps; h->seed = cfg->seed;
     h->n_blocks = blocks; h->n_elements = elements;
-    int64_t per = blocks / NORM_WARPS;
-    h->per_warp = (int)(per < 1 ? 1 : per > 64 ? 64 : per);
-    const int64_t norm_warps = (blocks + h->per_warp - 1) / h->per_warp;
-    h->norm_grid = (int)((norm_warps + WARPS - 1) / WARPS);
+    h->per_cta = (blocks + NORM_CTAS - 1) / NORM_CTAS;
+    if (h->per_cta < WARPS) h->per_cta = WARPS;
+    h->norm_grid = (int)((blocks + h->per_cta - 1) / h->per_cta);
     if (h->norm_grid < 1) h->norm_grid = 1;
+    h->n_slots = h->norm_grid + n;
     h->sizes = (int64_t*)malloc(sizeof(int64_t) * (size_t)n);
     Tensor* host = (Tensor*)calloc((size_t)n, sizeof(Tensor));
     int rc = h->sizes && host ? CO3_OK : CO3_ENOMEM;
@@ -522,18 +795,18 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
         auto part = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
         const size_t o_sc = part(sizeof(Scalars)), o_t = part(sizeof(Tensor) * (size_t)n), o_own = part(4 * (size_t)blocks);
         const size_t o_tab = part(n > INLINE_TENSORS ? sizeof(Pointers) * (size_t)n : 0);
-        const size_t o_slots = part(8 * (size_t)(norm_warps + n)), o_sums = part(8 * (size_t)n), o_bad = part(8 * (size_t)h->norm_grid);
+        const size_t o_slots = part(8 * (size_t)h->n_slots), o_bad = part(8 * (size_t)h->norm_grid);
         if (cudaMalloc(&h->slab, at) != cudaSuccess) { (void)cudaGetLastError(); h->slab = nullptr; rc = CO3_ENOMEM; }
         else {
             char* base = (char*)h->slab;
             h->sc = (Scalars*)(base + o_sc); h->tensors = (Tensor*)(base + o_t); h->owner = (int32_t*)(base + o_own);
             h->table = n > INLINE_TENSORS ? (Pointers*)(base + o_tab) : nullptr;
-            h->slots = (double*)(base + o_slots); h->sums = (double*)(base + o_sums); h->bad = (unsigned long long*)(base + o_bad);
+            h->slots = (double*)(base + o_slots); h->bad = (unsigned long long*)(base + o_bad);
             Scalars s;
             memset(&s, 0, sizeof(s));
             s.pow1 = s.pow2 = 1.0;
             next_scalars(s, h->beta1, h->beta2, h->seed);
-            bool ok = cudaMemcpy(h->sc, &s, sizeof(s), cudaMemcpyHostToDevice) == cudaSuccess &&
+            bool ok = cudaMemset(h->slots, 0, 8 * (size_t)h->n_slots) == cudaSuccess && cudaMemcpy(h->sc, &s, sizeof(s), cudaMemcpyHostToDevice) == cudaSuccess &&
                       cudaMemcpy(h->tensors, host, sizeof(Tensor) * (size_t)n, cudaMemcpyHostToDevice) == cudaSuccess;
             if (ok && blocks) {
                 const int64_t grid = (blocks + 255) / 256;
@@ -565,10 +838,12 @@ extern "C" int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_
     NormArgs a;
     int rc = place_pointers(h, grads, nullptr, nullptr, a.inline_ptr, st);
     if (rc != CO3_OK) return rc;
-    a.tensors = h->tensors; a.owner = h->owner; a.table = h->table; a.n_blocks = h->n_blocks; a.n_tensors = h->n_tensors;
-    a.per_warp = h->per_warp; a.grad_type = h->grad_type; a.grad_scale = grad_scale; a.max_norm = max_norm;
-    a.slots = h->slots; a.sums = h->sums; a.bad = h->bad; a.tensor_norms = tensor_norms; a.info = info; a.sc = h->sc;
-    norm_kernel<<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
+    a.tensors = h->tensors; a.owner = h->owner; a.table = h->table; a.n_blocks = h->n_blocks; a.per_cta = h->per_cta;
+    a.n_tensors = h->n_tensors; a.n_slots = h->n_slots; a.grad_scale = grad_scale; a.max_norm = max_norm;
+    a.slots = h->slots; a.bad = h->bad; a.tensor_norms = tensor_norms; a.info = info; a.sc = h->sc;
+    if (h->grad_type == CO3_F32) norm_kernel<F32><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
+    else if (h->grad_type == CO3_BF16) norm_kernel<Bf16><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
+    else norm_kernel<F16><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
     return launched(h, 1);
 }
 
@@ -590,12 +865,12 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     a.m = state->m; a.v = state->v; a.m_exp = (uint8_t*)state->m_exp; a.v_exp = (uint8_t*)state->v_exp;
     a.info = info; a.d_lr = d_lr; a.sc = h->sc; a.beta1 = h->beta1; a.beta2 = h->beta2;
     a.b1 = (float)h->beta1; a.a1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.a2 = (float)(1.0 - h->beta2);
-    a.eps = (float)h->eps; a.lr = (float)lr; a.seed = h->seed; a.grad_type = h->grad_type; a.copy_type = h->copy_type;
+    a.eps = (float)h->eps; a.lr = (float)lr; a.seed = h->seed; a.copy_type = h->copy_type;
     const int64_t need = (h->n_blocks + WARPS - 1) / WARPS, most = (int64_t)h->num_sms * 8;
     const int grid = (int)(need < 1 ? 1 : need < most ? need : most);
     const bool w16 = h->weight_type == CO3_BF16;
-    if (h->state_bits == 32) return w16 ? launch_step<32, true>(h, a, grid, st) : launch_step<32, false>(h, a, grid, st);
-    return w16 ? launch_step<8, true>(h, a, grid, st) : launch_step<8, false>(h, a, grid, st);
+    if (h->state_bits == 32) return w16 ? launch_step<32, Bf16>(h, a, grid, st) : launch_step<32, F32>(h, a, grid, st);
+    return w16 ? launch_step<8, Bf16>(h, a, grid, st) : launch_step<8, F32>(h, a, grid, st);
 }
 
 extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void* m_values, void* v_values, int32_t value_type, void* cuda_stream) {
@@ -603,15 +878,15 @@ extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void
     if (!on_device(h)) return CO3_EINVAL;
     if (!h->n_blocks) return CO3_OK;
     if (!state->m || !state->v || !state->m_exp || !state->v_exp || (((uintptr_t)state->m | (uintptr_t)state->v) & 31)) return CO3_EINVAL;
-    if (!m_values || !v_values || (((uintptr_t)m_values | (uintptr_t)v_values) & 15)) return CO3_EINVAL;
+    if (!m_values || !v_values || (((uintptr_t)m_values | (uintptr_t)v_values) & 31)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const int64_t need = (h->n_blocks + WARPS - 1) / WARPS, most = (int64_t)h->num_sms * 8;
     const int grid = (int)(need < most ? need : most);
     const uint8_t *m = (const uint8_t*)state->m, *v = (const uint8_t*)state->v;
     if (value_type == CO3_F32)
-        values_kernel<float><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (float*)m_values, (float*)v_values);
+        values_kernel<F32><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (float*)m_values, (float*)v_values);
     else
-        values_kernel<__nv_bfloat16><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (__nv_bfloat16*)m_values, (__nv_bfloat16*)v_values);
+        values_kernel<Bf16><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (__nv_bfloat16*)m_values, (__nv_bfloat16*)v_values);
     return launched(h, 1);
 }
 
