@@ -418,7 +418,7 @@ typedef struct co3_adamw co3_adamw; /* opaque, library-owned */
 
 typedef struct {
     int32_t n_tensors;    /* >= 1                                                                            */
-    const int64_t* sizes; /* host, elements per tensor, each >= 0; at most 2^31 - 1 blocks of 256 in all     */
+    const int64_t* sizes; /* host, elements per tensor, each >= 0; at most 2^31 - 256 blocks of 256 in all   */
     const float* decay;   /* host, decay_l per tensor, or NULL: weight_decay for all                         */
     int32_t weight_type;  /* CO3_F32 or CO3_BF16                                                             */
     int32_t grad_type;    /* CO3_F32, CO3_BF16 or CO3_F16                                                    */

@@ -40,10 +40,11 @@ struct Tensor {
 struct Scalars {
     long long steps;                          // taken so far
     double pow1, pow2;                        // beta1^steps, beta2^steps
-    float inv_c1, rsqrt_c2;                   // 1 / (1 - beta1^(steps+1)), 1 / sqrt(1 - beta2^(steps+1)): the next step's
+    float inv_c1, sqrt_c2;                    // 1 / (1 - beta1^(steps+1)), sqrt(1 - beta2^(steps+1)): the next step's
     uint32_t key;                             // ... and its key of the rounding counters
-    uint32_t ticket, norm_ticket;
-    uint32_t flags;
+    // What thread blocks change as they end lies apart from what others read as they begin: the two dies keep lines of their own.
+    alignas(256) uint32_t ticket;
+    uint32_t norm_ticket, flags;
     unsigned long long skipped_elements, skipped_steps;
 };
 
@@ -56,7 +57,7 @@ __host__ __device__ inline uint32_t mix32(uint32_t x) {
 
 __host__ __device__ inline void next_scalars(Scalars& s, double beta1, double beta2, uint32_t seed) {
     s.inv_c1 = (float)(1.0 / (1.0 - s.pow1 * beta1));
-    s.rsqrt_c2 = (float)(1.0 / sqrt(1.0 - s.pow2 * beta2));
+    s.sqrt_c2 = (float)sqrt(1.0 - s.pow2 * beta2);
     s.key = mix32(mix32(seed) + (uint32_t)(s.steps + 1));
 }
 
@@ -75,7 +76,33 @@ __device__ __forceinline__ float pow2i(int e) {          // 2^e, -149 <= e <= 12
     return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << (e + 149));
 }
 
+// Two 32-bit operations in one instruction, each rounded by itself as the single ones are.
+struct Pair {
+    unsigned long long v;
+    __device__ __forceinline__ Pair() {}
+    explicit __host__ __device__ __forceinline__ Pair(unsigned long long bits) : v(bits) {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 // A type of weights, gradients or copies: one element, and a lane's eight neighbouring ones in one access.
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 u;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    return u;
+}
+__device__ __forceinline__ uint2 load_codes(const void* p) {
+    uint2 u;
+    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(u.x), "=r"(u.y) : "l"(p));
+    return u;
+}
 struct F32 {
     typedef float type;
     static constexpr uintptr_t ALIGN = 31;
@@ -94,7 +121,7 @@ struct Bf16 {
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __bfloat162float(x); }
     static __device__ __forceinline__ void load8(const type* p, float* x) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint4 u = load16(p);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
@@ -111,7 +138,7 @@ struct F16 {
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __half2float(x); }
     static __device__ __forceinline__ void load8(const type* p, float* x) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint4 u = load16(p);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -152,29 +179,44 @@ template <int TOP> struct Scale {
     template <bool SIGNED> static __device__ __forceinline__ void decode8(uint2 c, float up, float* x) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint32_t w = (k < 4 ? c.x : c.y) << (24 - 8 * (k & 3));      // the code on top
-            const uint32_t f = SIGNED ? (uint32_t)((int32_t)w >> 4) & 0x87F00000u : (w >> 4) & 0x0FF00000u;
-            x[k] = __fmul_rn(__uint_as_float(f), up);
+            const uint32_t word = k < 4 ? c.x : c.y;
+            const int left = 24 - 8 * (k & 3);                                 // brings the code on top
+            uint32_t f;
+            if (SIGNED) f = (uint32_t)((int32_t)(word << left) >> 4) & 0x87F00000u;
+            else f = (left ? word << (left - 4) : word >> 4) & 0x0FF00000u;
+            x[k] = __uint_as_float(f);
         }
-    }
-    // r: the counters; the first moment takes bits 0..19, the second 12..31.  The sum is formed four places up, so that the code
-    // ends on top of its word and moves into the packed word with one funnel shift.
-    template <bool SIGNED> static __device__ __forceinline__ uint2 encode8(const float* x, float down, const uint32_t* r) {
-        uint32_t pack[2] = {0, 0};
+        const Pair scale(up, up);
 #pragma unroll
-        for (int k = 7; k >= 0; --k) {
-            float y = __fmul_rn(x[k], down);
-            uint32_t z;
+        for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * scale).get(x[k], x[k + 1]);
+    }
+    // r: the counters; the first moment takes bits 0..19, the second 12..31.  The sum is formed four places up, so that the code is
+    // the upper byte of its word.
+    template <bool SIGNED> static __device__ __forceinline__ uint2 encode8(const float* x, float down, const uint32_t* r) {
+        const Pair scale(down, down);
+        float y[8];
+        uint32_t z[8], pack[2];
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * scale).get(y[k], y[k + 1]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)                                            // (of r >> 8, the last four bits lie below what counts)
+            z[k] = __float_as_uint(y[k]) * 16u + (SIGNED ? (r[k] << 4) & 0x00FFFFF0u : r[k] >> 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            pack[h] = upper_bytes(z + 4 * h);
             if (SIGNED) {
-                z = (__float_as_uint(y) << 4) + ((r[k] << 4) & 0x00FFFFF0u);
-                z = (z & 0x7FFFFFFFu) | (__float_as_uint(y) & 0x80000000u);
-            } else {
-                if (x[k] > 0.0f) y = fmaxf(y, 0x1p-129f);                      // code 1: never to zero
-                z = (__float_as_uint(y) << 4) + (r[k] >> 8);                   // bits 8..11 lie below what counts
+                const uint32_t s[4] = {__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), __float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3])};
+                pack[h] |= upper_bytes(s) & 0x80808080u;
+            } else if ((pack[h] - 0x01010101u) & ~pack[h] & 0x80808080u) {     // some code is zero: a positive value never is
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (!(pack[h] >> (8 * k) & 0xFFu) && x[4 * h + k] > 0.0f) pack[h] |= 1u << (8 * k);
             }
-            pack[k >> 2] = __funnelshift_l(z, pack[k >> 2], 8);
         }
         return make_uint2(pack[0], pack[1]);
+    }
+    static __device__ __forceinline__ uint32_t upper_bytes(const uint32_t* z) {
+        return __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
     }
 };
 using ScaleM = Scale<14>;
@@ -205,14 +247,21 @@ struct StepArgs {
     Scalars* sc;
     double beta1, beta2;
     float b1, a1, b2, a2, eps, lr;
+    unsigned long long b1_pair, a1_pair, b2_pair, a2_pair;   // the first four, each twice
+    unsigned long long minus_zero;            // twice -0: a product plus this is the product, rounded
     uint32_t seed;
-    int copy_type;
+    int copy_type, stretch;
+    bool fast;                                // block_whole's root is precise enough, see co3_adamw_step
     Pointers inline_ptr[INLINE_TENSORS];
 };
 
 struct Step {                                 // what is the same for all elements of a block
-    float factor, rate, rsqrt_c2, decay;
-    uint32_t key;                             // key + place of the block, in the counters' sense
+    float factor, decay;
+    float rate, eps;                          // lr sqrt(1 - beta2^t) / (1 - beta1^t), eps sqrt(1 - beta2^t): the update is rate m / (sqrt(v) + eps)
+};
+
+struct Bases {                                // where a tensor's arrays would begin if it began with block 0
+    uintptr_t weight, grad, copy;
 };
 
 // An element whose second moment is not below this (or is no number) is left as it was.  The bound keeps the exponents
@@ -226,20 +275,23 @@ __device__ __forceinline__ void moments(float& m, float& v, float g, const StepA
     v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.a2));
 }
 
+constexpr int STRETCH = 128;                  // blocks of a thread block at most
+constexpr int STEP_CTAS = 3;                  // thread blocks of the step on an SM
+
 // Root and quotient to two units in the last place: 2^-22 of the update, itself a small part of the weight.
-__device__ __forceinline__ float new_weight(float w, float m, float v, const Step& s, float eps) {
+__device__ __forceinline__ float new_weight(float w, float m, float v, const Step& s) {
     float root;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
-    return w - __fmaf_rn(w, s.decay, __fdividef(m * s.rate, __fmaf_rn(root, s.rsqrt_c2, eps)));
+    return w - __fmaf_rn(w, s.decay, __fdividef(m * s.rate, root + s.eps));
 }
 
 // The general way for one block: any alignment, any count, any values.  Lane i takes the elements i, i + 32, ...
 template <int BITS, class W, class G>
-__device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, const Pointers& p, int64_t b, int64_t e0, int n) {
+__device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, int n, uint8_t* tops) {
     const int lane = threadIdx.x & 31;
-    const int64_t place = b * BLK;
-    typename W::type* pw = static_cast<typename W::type*>(p.weight) + e0;
-    const typename G::type* pg = static_cast<const typename G::type*>(p.grad) + e0;
+    const int64_t place = (int64_t)b * BLK;
+    typename W::type* pw = reinterpret_cast<typename W::type*>(p.weight) + place;
+    const typename G::type* pg = reinterpret_cast<const typename G::type*>(p.grad) + place;
     float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
     uint32_t kept = 0;
 #pragma unroll
@@ -252,9 +304,9 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
             v[k] = i < n ? static_cast<const float*>(a.v)[place + i] : 0.0f;
         } else {
             const uint32_t c = static_cast<const uint8_t*>(a.m)[place + i];
-            m[k] = ScaleM::decode(c & 127u, a.m_exp[b]);
+            m[k] = ScaleM::decode(c & 127u, tops[0]);
             if (c & 128u) m[k] = -m[k];
-            v[k] = ScaleV::decode(static_cast<const uint8_t*>(a.v)[place + i], a.v_exp[b]);
+            v[k] = ScaleV::decode(static_cast<const uint8_t*>(a.v)[place + i], tops[STRETCH]);
             if (i >= n) m[k] = v[k] = 0.0f;
         }
     }
@@ -267,17 +319,17 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
         if (v1 < V_LIMIT) {
             m[k] = m1;
             v[k] = v1;
-            w[k] = new_weight(w[k], m1, v1, s, a.eps);
+            w[k] = new_weight(w[k], m1, v1, s);
             if (i < n) {
-                if (sizeof(typename W::type) == 2) reinterpret_cast<__nv_bfloat16*>(pw)[i] = bf16_stochastic(w[k], counter_bits(s.key, (uint32_t)i) >> 10);
+                if (sizeof(typename W::type) == 2) reinterpret_cast<__nv_bfloat16*>(pw)[i] = bf16_stochastic(w[k], counter_bits(key, (uint32_t)i) >> 10);
                 else reinterpret_cast<float*>(pw)[i] = w[k];
             }
         } else {
             ++kept;                                       // never one of the places past n: their moments are 0
         }
         if (i < n) {
-            if (a.copy_type == CO3_BF16) static_cast<__nv_bfloat16*>(p.copy)[e0 + i] = __float2bfloat16_rn(w[k]);
-            if (a.copy_type == CO3_F16) static_cast<__half*>(p.copy)[e0 + i] = __float2half_rn(w[k]);
+            if (a.copy_type == CO3_BF16) reinterpret_cast<__nv_bfloat16*>(p.copy)[place + i] = __float2bfloat16_rn(w[k]);
+            if (a.copy_type == CO3_F16) reinterpret_cast<__half*>(p.copy)[place + i] = __float2half_rn(w[k]);
             if (BITS == 32) {
                 static_cast<float*>(a.m)[place + i] = m[k];
                 static_cast<float*>(a.v)[place + i] = v[k];
@@ -288,11 +340,12 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
     }
     if (BITS == 8) {
         const int m_top = warp_top(m_max, ScaleM::LEAST), v_top = warp_top(v_max, ScaleV::LEAST);
-        if (lane == 0) { a.m_exp[b] = (uint8_t)m_top; a.v_exp[b] = (uint8_t)v_top; }
+        __syncwarp();
+        if (lane == 0) { tops[0] = (uint8_t)m_top; tops[STRETCH] = (uint8_t)v_top; }
 #pragma unroll
         for (int k = 0; k < PER_LANE; ++k) {
             const int i = lane + 32 * k;
-            const uint32_t r = counter_bits(s.key, (uint32_t)i);
+            const uint32_t r = counter_bits(key, (uint32_t)i);
             uint32_t c = ScaleM::encode(fabsf(m[k]), m_top, r & 0xFFFFFu);
             if (m[k] < 0.0f) c |= 128u;
             if (i < n) static_cast<uint8_t*>(a.m)[place + i] = (uint8_t)c;
@@ -304,65 +357,91 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
     return kept;
 }
 
+__device__ __forceinline__ float root_fast(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float inverse_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
 // The usual way: a whole block whose tensors are aligned.  Lane i takes the elements 8i .. 8i + 7, each array in one access.
 // Returns false, before anything is written, if a value needs the general way.
 template <int BITS, class W, class G>
-__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, const Pointers& p, int64_t b, int64_t e0) {
+__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, uint8_t* tops) {
+    constexpr bool W16 = sizeof(typename W::type) == 2;
     const int lane = threadIdx.x & 31;
-    const int64_t at = b * BLK + PER_LANE * lane;
-    typename W::type* pw = static_cast<typename W::type*>(p.weight) + e0 + PER_LANE * lane;
+    const int64_t at = (int64_t)b * BLK + PER_LANE * lane;
+    typename W::type* pw = reinterpret_cast<typename W::type*>(p.weight) + at;
     float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
-    G::load8(static_cast<const typename G::type*>(p.grad) + e0 + PER_LANE * lane, g);
+    bool other = false;                                   // some value needs the general way
+    G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
     W::load8(pw, w);
     if (BITS == 32) {
         F32::load8(static_cast<const float*>(a.m) + at, m);
         F32::load8(static_cast<const float*>(a.v) + at, v);
     } else {
-        const uint2 cm = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.m) + at);
-        const uint2 cv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.v) + at);
-        const int m_top = a.m_exp[b], v_top = a.v_exp[b];
-        if (m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN) return false;
+        const uint2 cm = load_codes(static_cast<const uint8_t*>(a.m) + at), cv = load_codes(static_cast<const uint8_t*>(a.v) + at);
+        const int m_top = tops[0], v_top = tops[STRETCH];
+        other = m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN;
         ScaleM::decode8<true>(cm, pow2i(m_top - ScaleM::FIELD), m);
         ScaleV::decode8<false>(cv, pow2i(v_top - ScaleV::FIELD), v);
     }
+    // The four products are formed as fused ones that add -0, for ptxas makes a fused one of a packed product and the sum
+    // that takes it, and the moments are rounded after each.
+    const Pair b1(a.b1_pair), a1(a.a1_pair), b2(a.b2_pair), a2(a.a2_pair), zero(a.minus_zero);
+    const Pair factor(s.factor, s.factor), rate(s.rate, s.rate), decay(s.decay, s.decay), eps(s.eps, s.eps), minus(-1.0f, -1.0f);
     uint32_t v_max = 0;
     float m_max = 0.0f;
+    Pair none(0.0f, 0.0f);
 #pragma unroll
-    for (int k = 0; k < PER_LANE; ++k) {
-        moments(m[k], v[k], __fmul_rn(g[k], s.factor), a);
-        v_max = max(v_max, __float_as_uint(v[k]));        // as whole numbers: NaN of either sign is above the limit too
-        if (BITS == 8) m_max = fmaxf(m_max, fabsf(m[k]));
-        w[k] = new_weight(w[k], m[k], v[k], s, a.eps);
+    for (int k = 0; k < PER_LANE; k += 2) {
+        const Pair gf = Pair(g[k], g[k + 1]) * factor;
+        const Pair m1 = fma(Pair(m[k], m[k + 1]), b1, zero) + fma(gf, a1, zero);
+        const Pair v1 = fma(Pair(v[k], v[k + 1]), b2, zero) + fma(gf * gf, a2, zero);
+        m1.get(m[k], m[k + 1]);
+        v1.get(v[k], v[k + 1]);
+        // as whole numbers: NaN of either sign is above the limit too
+        v_max = __vimax3_u32(v_max, __float_as_uint(v[k]), __float_as_uint(v[k + 1]));
+        if (BITS == 8) m_max = fmaxf(fmaxf(m_max, fabsf(m[k])), fabsf(m[k + 1]));
+        const Pair d = Pair(root_fast(v[k]), root_fast(v[k + 1])) + eps;
+        float d0, d1;
+        d.get(d0, d1);
+        const Pair w0(w[k], w[k + 1]), upd = fma(w0, decay, m1 * rate * Pair(inverse_fast(d0), inverse_fast(d1))), w1 = fma(upd, minus, w0);
+        w1.get(w[k], w[k + 1]);
+        if (W16) none = fma(w1, Pair(0.0f, 0.0f), none);  // NaN once a weight is not finite
     }
     int m_top = 0, v_top = 0;
+    if (W16) {
+        float x, y;
+        none.get(x, y);
+        other = other || !(x + y == 0.0f);
+    }
     if (BITS == 8) {
         v_max = __reduce_max_sync(0xffffffffu, v_max);
         v_top = max((int)(v_max >> 23), ScaleV::LEAST);
         m_top = warp_top(m_max, ScaleM::LEAST);
-        if (v_max >= __float_as_uint(V_LIMIT) || m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN) return false;
-    } else if (__any_sync(0xffffffffu, v_max >= __float_as_uint(V_LIMIT))) {
+        other = other || v_max >= __float_as_uint(V_LIMIT) || m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN;
+        if (__any_sync(0xffffffffu, other)) return false;
+    } else if (__any_sync(0xffffffffu, other || v_max >= __float_as_uint(V_LIMIT))) {
         return false;
     }
     uint32_t r[PER_LANE];
-    if (BITS == 8 || sizeof(typename W::type) == 2) {
+    if (BITS == 8 || W16) {
 #pragma unroll
-        for (int k = 0; k < PER_LANE; ++k) r[k] = counter_bits(s.key, (uint32_t)(PER_LANE * lane + k));
+        for (int k = 0; k < PER_LANE; ++k) r[k] = counter_bits(key, (uint32_t)(PER_LANE * lane + k));
     }
-    if (sizeof(typename W::type) == 2) {
-        uint32_t h[PER_LANE];
+    if (W16) {
+        uint32_t h[PER_LANE / 2];
 #pragma unroll
-        for (int k = 0; k < PER_LANE; ++k) h[k] = __bfloat16_as_ushort(bf16_stochastic(w[k], r[k] >> 10));
-        *reinterpret_cast<uint4*>(pw) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        for (int k = 0; k < PER_LANE; k += 2)             // all finite: the sum's upper halves
+            h[k / 2] = __byte_perm(__float_as_uint(w[k]) + ((r[k] << 6) >> 16), __float_as_uint(w[k + 1]) + ((r[k + 1] << 6) >> 16), 0x7632);
+        *reinterpret_cast<uint4*>(pw) = make_uint4(h[0], h[1], h[2], h[3]);
     } else {
         F32::store8(reinterpret_cast<float*>(pw), w);
-        if (a.copy_type == CO3_BF16) Bf16::store8(static_cast<__nv_bfloat16*>(p.copy) + e0 + PER_LANE * lane, w);
-        if (a.copy_type == CO3_F16) F16::store8(static_cast<__half*>(p.copy) + e0 + PER_LANE * lane, w);
+        if (a.copy_type == CO3_BF16) Bf16::store8(reinterpret_cast<__nv_bfloat16*>(p.copy) + at, w);
+        if (a.copy_type == CO3_F16) F16::store8(reinterpret_cast<__half*>(p.copy) + at, w);
     }
     if (BITS == 32) {
         F32::store8(static_cast<float*>(a.m) + at, m);
         F32::store8(static_cast<float*>(a.v) + at, v);
     } else {
-        if (lane == 0) { a.m_exp[b] = (uint8_t)m_top; a.v_exp[b] = (uint8_t)v_top; }
+        if (lane == 0) { tops[0] = (uint8_t)m_top; tops[STRETCH] = (uint8_t)v_top; }
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + at) = ScaleM::encode8<true>(m, pow2i(ScaleM::FIELD - m_top), r);
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + at) = ScaleV::encode8<false>(v, pow2i(ScaleV::FIELD - v_top), r);
     }
@@ -370,30 +449,52 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, co
 }
 
 template <int BITS, class W, class G>
-__global__ void __launch_bounds__(32 * WARPS, 3) adamw_kernel(const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __grid_constant__ StepArgs a) {
+    static_assert(2 * STRETCH <= 32 * WARPS, "a thread for each exponent");
+    __shared__ uint8_t tops[2 * STRETCH];                 // the block exponents of the first moments, then of the second
     const int warp = threadIdx.x >> 5;
-    const float inv_c1 = a.sc->inv_c1;
+    const int64_t begin = (int64_t)blockIdx.x * a.stretch;
+    const int end = (int)min(begin + a.stretch, a.n_blocks), count = end - (int)begin;
+    if (BITS == 8 && threadIdx.x < 2 * STRETCH && (threadIdx.x & (STRETCH - 1)) < count)
+        tops[threadIdx.x] = (threadIdx.x < STRETCH ? a.m_exp : a.v_exp)[begin + (threadIdx.x & (STRETCH - 1))];
+    const float inv_c1 = a.sc->inv_c1, sqrt_c2 = a.sc->sqrt_c2;
     const uint32_t step_key = a.sc->key;
     const bool skip = a.info && a.info->nonfinite != 0;
     const float lr = a.d_lr ? *a.d_lr : a.lr;
     Step s;
     s.factor = a.info ? a.info->factor : 1.0f;
-    s.rate = lr * inv_c1;
-    s.rsqrt_c2 = a.sc->rsqrt_c2;
+    s.rate = lr * (inv_c1 * sqrt_c2);
+    s.eps = a.eps * sqrt_c2;
     __syncthreads();                                      // every thread has read what the last block changes below
     uint32_t kept = 0;
     if (!skip) {
-        for (int64_t b = (int64_t)blockIdx.x * WARPS + warp; b < a.n_blocks; b += (int64_t)gridDim.x * WARPS) {
-            const int t = a.owner[b];
-            const Tensor tn = a.tensors[t];
-            const Pointers p = a.table ? a.table[t] : a.inline_ptr[t];
-            const int64_t e0 = (b - tn.block0) * BLK;
-            const int n = (int)(tn.size - e0 < BLK ? tn.size - e0 : BLK);
-            s.decay = lr * tn.decay;
-            s.key = block_key(step_key, b * BLK);
-            const uintptr_t off = ((uintptr_t)p.weight & W::ALIGN) | ((uintptr_t)p.grad & G::ALIGN) | ((uintptr_t)p.copy & 15);
-            if (n < BLK || off || !block_whole<BITS, W, G>(a, s, p, b, e0)) kept += block_any<BITS, W, G>(a, s, p, b, e0, n);
+        // a stretch of blocks per thread block, one after the other to its warps
+        int end_t = 0, whole_t = 0;                       // of the tensor: block past its last, block past its last usual one
+        Bases p = {0, 0, 0};
+        for (int b = (int)begin + warp; b < end; b += WARPS) {
+            if (b >= end_t) {
+                const int t = a.owner[b];
+                const Tensor tn = a.tensors[t];
+                const Pointers at = a.table ? a.table[t] : a.inline_ptr[t];
+                const uintptr_t e = (uintptr_t)tn.block0 * BLK;
+                p = {(uintptr_t)at.weight - e * sizeof(typename W::type), (uintptr_t)at.grad - e * sizeof(typename G::type), (uintptr_t)at.copy - e * 2};
+                end_t = (int)(tn.block0 + (tn.size + BLK - 1) / BLK);
+                const bool aligned = !(((uintptr_t)at.weight & W::ALIGN) | ((uintptr_t)at.grad & G::ALIGN) | ((uintptr_t)at.copy & 15));
+                whole_t = a.fast && aligned ? (int)(tn.block0 + tn.size / BLK) : 0;
+                s.decay = lr * tn.decay;
+            }
+            const uint32_t key = block_key(step_key, (int64_t)b * BLK);
+            if (b >= whole_t || !block_whole<BITS, W, G>(a, s, key, p, b, tops + (b - (int)begin))) {
+                const Tensor tn = a.tensors[a.owner[b]];
+                const int64_t left = tn.size - (b - tn.block0) * BLK;
+                kept += block_any<BITS, W, G>(a, s, key, p, b, left < BLK ? (int)left : BLK, tops + (b - (int)begin));
+            }
         }
+    }
+    if (BITS == 8 && !skip) {
+        __syncthreads();
+        if (threadIdx.x < 2 * STRETCH && (threadIdx.x & (STRETCH - 1)) < count)
+            (threadIdx.x < STRETCH ? a.m_exp : a.v_exp)[begin + (threadIdx.x & (STRETCH - 1))] = tops[threadIdx.x];
     }
     if (kept) {                                           // rare: elements left as they were
         atomicOr(&a.sc->flags, CO3_FLAG_NONFINITE);
@@ -413,7 +514,7 @@ __global__ void __launch_bounds__(32 * WARPS, 3) adamw_kernel(const __grid_const
                 n.pow2 *= a.beta2;
                 next_scalars(n, a.beta1, a.beta2, a.seed);
                 a.sc->steps = n.steps; a.sc->pow1 = n.pow1; a.sc->pow2 = n.pow2;
-                a.sc->inv_c1 = n.inv_c1; a.sc->rsqrt_c2 = n.rsqrt_c2; a.sc->key = n.key;
+                a.sc->inv_c1 = n.inv_c1; a.sc->sqrt_c2 = n.sqrt_c2; a.sc->key = n.key;
             }
         }
     }
@@ -759,7 +860,7 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
         if (cfg->decay && !(cfg->decay[t] >= 0.0f && cfg->decay[t] < INFINITY)) return CO3_EINVAL;
         blocks += (cfg->sizes[t] + BLK - 1) / BLK;
         elements += cfg->sizes[t];
-        if (blocks > 0x7FFFFFFFLL) return CO3_EINVAL;
+        if (blocks > 0x7FFFFF00LL) return CO3_EINVAL;
     }
     co3_adamw* h = new (std::nothrow) co3_adamw();
     if (!h) return CO3_ENOMEM;
@@ -865,9 +966,19 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     a.m = state->m; a.v = state->v; a.m_exp = (uint8_t*)state->m_exp; a.v_exp = (uint8_t*)state->v_exp;
     a.info = info; a.d_lr = d_lr; a.sc = h->sc; a.beta1 = h->beta1; a.beta2 = h->beta2;
     a.b1 = (float)h->beta1; a.a1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.a2 = (float)(1.0 - h->beta2);
+    auto twice = [](float x) { uint32_t u; memcpy(&u, &x, 4); return (unsigned long long)u << 32 | u; };
+    a.b1_pair = twice(a.b1); a.a1_pair = twice(a.a1); a.b2_pair = twice(a.b2); a.a2_pair = twice(a.a2); a.minus_zero = twice(-0.0f);
     a.eps = (float)h->eps; a.lr = (float)lr; a.seed = h->seed; a.copy_type = h->copy_type;
-    const int64_t need = (h->n_blocks + WARPS - 1) / WARPS, most = (int64_t)h->num_sms * 8;
-    const int grid = (int)(need < 1 ? 1 : need < most ? need : most);
+    // block_whole takes roots of numbers below 2^-126 as 0.  Beside eps that is less than 2^-24 of the denominator if eps is above
+    // 2^24 * 2^-63 / sqrt(1 - beta2) (6e-11 for beta2 = 0.999); a smaller eps takes the general way.
+    a.fast = h->eps * sqrt(1.0 - h->beta2) >= 0x1p-39;
+    // Blocks of one warp: as many as leave every place for a thread block four of them one after the other, so that the SMs end
+    // together, and at most 4 with 32-bit moments (2^28 f32: 1, 2, 4, 8, 16 blocks take 1214, 1115, 1097, 1114, 1125 us), 16 with
+    // 8-bit ones (2^28: 1493, 1186, 1083, 1044, 1023 us): their exponents are bytes, and 128 of them side by side make a line that
+    // no other thread block writes.  (Written block by block, with the dies handing the line to and fro, 4 blocks took 2434 us.)
+    const int64_t per_warp = h->n_blocks / ((int64_t)h->num_sms * STEP_CTAS * WARPS * 4), most = h->state_bits == 8 ? STRETCH / WARPS : 4;
+    a.stretch = (int)(WARPS * (per_warp < 1 ? 1 : per_warp > most ? most : per_warp));
+    const int grid = h->n_blocks ? (int)((h->n_blocks + a.stretch - 1) / a.stretch) : 1;
     const bool w16 = h->weight_type == CO3_BF16;
     if (h->state_bits == 32) return w16 ? launch_step<32, Bf16>(h, a, grid, st) : launch_step<32, F32>(h, a, grid, st);
     return w16 ? launch_step<8, Bf16>(h, a, grid, st) : launch_step<8, F32>(h, a, grid, st);
