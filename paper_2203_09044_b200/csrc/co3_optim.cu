@@ -103,8 +103,28 @@ __device__ __forceinline__ uint2 load_codes(const void* p) {
     asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(u.x), "=r"(u.y) : "l"(p));
     return u;
 }
+// The same accesses to shared memory that cp.async has filled.
+__device__ __forceinline__ uint4 stage16(uint32_t at) {
+    uint4 u;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at));
+    return u;
+}
+__device__ __forceinline__ uint2 stage8(uint32_t at) {
+    uint2 u;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(u.x), "=r"(u.y) : "r"(at));
+    return u;
+}
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory");
+}
 struct F32 {
     typedef float type;
+    static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
+        const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k]);
+    }
     static constexpr uintptr_t ALIGN = 31;
     static __device__ __forceinline__ float to(float x) { return x; }
     static __device__ __forceinline__ void load8(const float* p, float* x) {
@@ -120,9 +140,9 @@ struct Bf16 {
     typedef __nv_bfloat16 type;
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __bfloat162float(x); }
-    static __device__ __forceinline__ void load8(const type* p, float* x) {
-        const uint4 u = load16(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    static __device__ __forceinline__ void load8(const type* p, float* x) { const uint4 u = load16(p); unpack(&u, x); }
+    static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
+        const uint32_t w[4] = {u->x, u->y, u->z, u->w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
     }
@@ -137,9 +157,9 @@ struct F16 {
     typedef __half type;
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __half2float(x); }
-    static __device__ __forceinline__ void load8(const type* p, float* x) {
-        const uint4 u = load16(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    static __device__ __forceinline__ void load8(const type* p, float* x) { const uint4 u = load16(p); unpack(&u, x); }
+    static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
+        const uint32_t w[4] = {u->x, u->y, u->z, u->w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
@@ -168,6 +188,10 @@ template <int TOP> struct Scale {
     static __device__ __forceinline__ float up2() { return pow2i(127 - TOP); }
     static __device__ __forceinline__ float down1(int top) { return pow2i(127 - top); }
     static __device__ __forceinline__ float down2() { return pow2i(TOP - 127); }
+    // ... and as one, for stored exponents up to PLAIN (and 2^(TOP - top))
+    static constexpr int PLAIN = 126 + TOP;
+    static __device__ __forceinline__ float up(int top) { return __uint_as_float((uint32_t)(top + (127 - TOP)) << 23); }
+    static __device__ __forceinline__ float down(int top) { return __uint_as_float((uint32_t)(TOP + 127 - top) << 23); }
     static __device__ __forceinline__ float decode(uint32_t code, int top) {
         return __fmul_rn(__fmul_rn(__uint_as_float(code << 20), up2()), up1(top));
     }
@@ -267,8 +291,6 @@ struct Bases {                                // where a tensor's arrays would b
 // An element whose second moment is not below this (or is no number) is left as it was.  The bound keeps the exponents
 // of 8-bit moments, and first moments with them, far from the end of the range.
 constexpr float V_LIMIT = 0x1p126f;
-// Up to these stored exponents the two factors of a scale can be multiplied beforehand.
-constexpr int M_TOP_PLAIN = 127 + ScaleM::FIELD, V_TOP_PLAIN = 127 + ScaleV::FIELD;
 
 __device__ __forceinline__ void moments(float& m, float& v, float g, const StepArgs& a) {
     m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.a1));
@@ -360,27 +382,62 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
 __device__ __forceinline__ float root_fast(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float inverse_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+// With 8-bit moments a block is little to load and much to compute: its loads are started one block ahead, into shared memory, where
+// they take no registers.  A copy of the warp is 512 bytes in a row (with 32 bytes a lane in two copies of 16 each, sectors would
+// be fetched twice), so lanes read what others copied and the warp meets before and after.
+template <class W, class G> struct Stage {
+    static constexpr int W_BYTES = sizeof(typename W::type) * BLK, G_BYTES = sizeof(typename G::type) * BLK, BYTES = W_BYTES + G_BYTES + 2 * BLK;
+    uint32_t base;                            // of the warp: gradient, weights, codes of the two moments
+    __device__ __forceinline__ void start(const StepArgs& a, const Bases& p, int b) const {
+        const int lane = threadIdx.x & 31;
+        const int64_t at = (int64_t)b * BLK;
+        const char* g = reinterpret_cast<const char*>(p.grad) + at * (int)sizeof(typename G::type) + 16 * lane;
+        const char* w = reinterpret_cast<const char*>(p.weight) + at * (int)sizeof(typename W::type) + 16 * lane;
+        const uint32_t to = base + 16 * lane, codes = base + G_BYTES + W_BYTES + 8 * lane;
+#pragma unroll
+        for (int k = 0; k < G_BYTES; k += 512) copy_async<16>(to + k, g + k);
+#pragma unroll
+        for (int k = 0; k < W_BYTES; k += 512) copy_async<16>(to + G_BYTES + k, w + k);
+        copy_async<8>(codes, static_cast<const uint8_t*>(a.m) + at + 8 * lane);
+        copy_async<8>(codes + BLK, static_cast<const uint8_t*>(a.v) + at + 8 * lane);
+    }
+    __device__ __forceinline__ void take(float* g, float* w, uint2& m, uint2& v) const {
+        const int lane = threadIdx.x & 31;
+        constexpr int g_lane = G_BYTES / 32, w_lane = W_BYTES / 32;
+        uint4 u[2];
+#pragma unroll
+        for (int k = 0; k < g_lane; k += 16) u[k / 16] = stage16(base + g_lane * lane + k);
+        G::unpack(u, g);
+#pragma unroll
+        for (int k = 0; k < w_lane; k += 16) u[k / 16] = stage16(base + G_BYTES + w_lane * lane + k);
+        W::unpack(u, w);
+        m = stage8(base + G_BYTES + W_BYTES + 8 * lane);
+        v = stage8(base + G_BYTES + W_BYTES + BLK + 8 * lane);
+    }
+};
+
 // The usual way: a whole block whose tensors are aligned.  Lane i takes the elements 8i .. 8i + 7, each array in one access.
 // Returns false, before anything is written, if a value needs the general way.
 template <int BITS, class W, class G>
-__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, uint8_t* tops) {
+__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, const Stage<W, G>& stage, uint8_t* tops) {
     constexpr bool W16 = sizeof(typename W::type) == 2;
     const int lane = threadIdx.x & 31;
     const int64_t at = (int64_t)b * BLK + PER_LANE * lane;
     typename W::type* pw = reinterpret_cast<typename W::type*>(p.weight) + at;
     float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
     bool other = false;                                   // some value needs the general way
-    G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
-    W::load8(pw, w);
     if (BITS == 32) {
+        G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
+        W::load8(pw, w);
         F32::load8(static_cast<const float*>(a.m) + at, m);
         F32::load8(static_cast<const float*>(a.v) + at, v);
     } else {
-        const uint2 cm = load_codes(static_cast<const uint8_t*>(a.m) + at), cv = load_codes(static_cast<const uint8_t*>(a.v) + at);
+        uint2 cm, cv;
+        stage.take(g, w, cm, cv);
         const int m_top = tops[0], v_top = tops[STRETCH];
-        other = m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN;
-        ScaleM::decode8<true>(cm, pow2i(m_top - ScaleM::FIELD), m);
-        ScaleV::decode8<false>(cv, pow2i(v_top - ScaleV::FIELD), v);
+        other = m_top > ScaleM::PLAIN || v_top > ScaleV::PLAIN;
+        ScaleM::decode8<true>(cm, ScaleM::up(m_top), m);
+        ScaleV::decode8<false>(cv, ScaleV::up(v_top), v);
     }
     // The four products are formed as fused ones that add -0, for ptxas makes a fused one of a packed product and the sum
     // that takes it, and the moments are rounded after each.
@@ -416,7 +473,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
         v_max = __reduce_max_sync(0xffffffffu, v_max);
         v_top = max((int)(v_max >> 23), ScaleV::LEAST);
         m_top = warp_top(m_max, ScaleM::LEAST);
-        other = other || v_max >= __float_as_uint(V_LIMIT) || m_top > M_TOP_PLAIN || v_top > V_TOP_PLAIN;
+        other = other || v_max >= __float_as_uint(V_LIMIT) || m_top > ScaleM::PLAIN || v_top > ScaleV::PLAIN;
         if (__any_sync(0xffffffffu, other)) return false;
     } else if (__any_sync(0xffffffffu, other || v_max >= __float_as_uint(V_LIMIT))) {
         return false;
@@ -442,59 +499,84 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
         F32::store8(static_cast<float*>(a.v) + at, v);
     } else {
         if (lane == 0) { tops[0] = (uint8_t)m_top; tops[STRETCH] = (uint8_t)v_top; }
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + at) = ScaleM::encode8<true>(m, pow2i(ScaleM::FIELD - m_top), r);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + at) = ScaleV::encode8<false>(v, pow2i(ScaleV::FIELD - v_top), r);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.m) + at) = ScaleM::encode8<true>(m, ScaleM::down(m_top), r);
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + at) = ScaleV::encode8<false>(v, ScaleV::down(v_top), r);
     }
     return true;
 }
 
 template <int BITS, class W, class G>
 __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __grid_constant__ StepArgs a) {
-    static_assert(2 * STRETCH <= 32 * WARPS, "a thread for each exponent");
     __shared__ uint8_t tops[2 * STRETCH];                 // the block exponents of the first moments, then of the second
+    extern __shared__ __align__(16) char stages[];        // two of each warp, taken in turn
     const int warp = threadIdx.x >> 5;
     const int64_t begin = (int64_t)blockIdx.x * a.stretch;
     const int end = (int)min(begin + a.stretch, a.n_blocks), count = end - (int)begin;
-    if (BITS == 8 && threadIdx.x < 2 * STRETCH && (threadIdx.x & (STRETCH - 1)) < count)
-        tops[threadIdx.x] = (threadIdx.x < STRETCH ? a.m_exp : a.v_exp)[begin + (threadIdx.x & (STRETCH - 1))];
-    const float inv_c1 = a.sc->inv_c1, sqrt_c2 = a.sc->sqrt_c2;
-    const uint32_t step_key = a.sc->key;
     const bool skip = a.info && a.info->nonfinite != 0;
     const float lr = a.d_lr ? *a.d_lr : a.lr;
     Step s;
+    int end_t = 0, whole_t = 0;                           // of the tensor: block past its last, block past its last usual one
+    Bases p = {0, 0, 0};
+    auto look_up = [&](int b) {
+        const int t = a.owner[b];
+        const Tensor tn = a.tensors[t];
+        const Pointers at = a.table ? a.table[t] : a.inline_ptr[t];
+        const uintptr_t e = (uintptr_t)tn.block0 * BLK;
+        p = {(uintptr_t)at.weight - e * sizeof(typename W::type), (uintptr_t)at.grad - e * sizeof(typename G::type), (uintptr_t)at.copy - e * 2};
+        end_t = (int)(tn.block0 + (tn.size + BLK - 1) / BLK);
+        const bool aligned = !(((uintptr_t)at.weight & W::ALIGN) | ((uintptr_t)at.grad & G::ALIGN) | ((uintptr_t)at.copy & 15));
+        whole_t = a.fast && aligned ? (int)(tn.block0 + tn.size / BLK) : 0;
+        s.decay = lr * tn.decay;
+    };
+    // a stretch of blocks per thread block, one after the other to its warps
+    int b = (int)begin + warp;
+    if (b < end) look_up(b);
+    Stage<W, G> stage = {(uint32_t)__cvta_generic_to_shared(stages) + 2 * warp * Stage<W, G>::BYTES};
+    uint32_t to_other = Stage<W, G>::BYTES;
+    bool have = false;                                    // block b is on its way to `stage`
+    if (BITS == 8) {
+        have = b < min(end, whole_t) && !skip;
+        if (have) stage.start(a, p, b);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        for (int i = threadIdx.x; i < 2 * STRETCH; i += 32 * WARPS)
+            if ((i & (STRETCH - 1)) < count) tops[i] = (i < STRETCH ? a.m_exp : a.v_exp)[begin + (i & (STRETCH - 1))];
+    }
+    const float inv_c1 = a.sc->inv_c1, sqrt_c2 = a.sc->sqrt_c2;
+    const uint32_t step_key = a.sc->key;
     s.factor = a.info ? a.info->factor : 1.0f;
     s.rate = lr * (inv_c1 * sqrt_c2);
     s.eps = a.eps * sqrt_c2;
     __syncthreads();                                      // every thread has read what the last block changes below
     uint32_t kept = 0;
     if (!skip) {
-        // a stretch of blocks per thread block, one after the other to its warps
-        int end_t = 0, whole_t = 0;                       // of the tensor: block past its last, block past its last usual one
-        Bases p = {0, 0, 0};
-        for (int b = (int)begin + warp; b < end; b += WARPS) {
-            if (b >= end_t) {
-                const int t = a.owner[b];
-                const Tensor tn = a.tensors[t];
-                const Pointers at = a.table ? a.table[t] : a.inline_ptr[t];
-                const uintptr_t e = (uintptr_t)tn.block0 * BLK;
-                p = {(uintptr_t)at.weight - e * sizeof(typename W::type), (uintptr_t)at.grad - e * sizeof(typename G::type), (uintptr_t)at.copy - e * 2};
-                end_t = (int)(tn.block0 + (tn.size + BLK - 1) / BLK);
-                const bool aligned = !(((uintptr_t)at.weight & W::ALIGN) | ((uintptr_t)at.grad & G::ALIGN) | ((uintptr_t)at.copy & 15));
-                whole_t = a.fast && aligned ? (int)(tn.block0 + tn.size / BLK) : 0;
-                s.decay = lr * tn.decay;
-            }
+        for (; b < end; b += WARPS) {
+            if (b >= end_t) look_up(b);
             const uint32_t key = block_key(step_key, (int64_t)b * BLK);
-            if (b >= whole_t || !block_whole<BITS, W, G>(a, s, key, p, b, tops + (b - (int)begin))) {
+            if (BITS == 8) {
+                if (!have && b < whole_t) {
+                    stage.start(a, p, b);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                }
+                have = b + WARPS < min(end, whole_t);
+                if (have) Stage<W, G>{stage.base + to_other}.start(a, p, b + WARPS);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                __syncwarp();
+            }
+            if (b >= whole_t || !block_whole<BITS, W, G>(a, s, key, p, b, stage, tops + (b - (int)begin))) {
                 const Tensor tn = a.tensors[a.owner[b]];
                 const int64_t left = tn.size - (b - tn.block0) * BLK;
                 kept += block_any<BITS, W, G>(a, s, key, p, b, left < BLK ? (int)left : BLK, tops + (b - (int)begin));
             }
+            __syncwarp();                                 // every lane has taken its part before it is overwritten
+            stage.base += to_other;
+            to_other = 0u - to_other;
         }
     }
     if (BITS == 8 && !skip) {
         __syncthreads();
-        if (threadIdx.x < 2 * STRETCH && (threadIdx.x & (STRETCH - 1)) < count)
-            (threadIdx.x < STRETCH ? a.m_exp : a.v_exp)[begin + (threadIdx.x & (STRETCH - 1))] = tops[threadIdx.x];
+        for (int i = threadIdx.x; i < 2 * STRETCH; i += 32 * WARPS)
+            if ((i & (STRETCH - 1)) < count) (i < STRETCH ? a.m_exp : a.v_exp)[begin + (i & (STRETCH - 1))] = tops[i];
     }
     if (kept) {                                           // rare: elements left as they were
         atomicOr(&a.sc->flags, CO3_FLAG_NONFINITE);
@@ -734,9 +816,9 @@ __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, co
         float x[PER_LANE];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const uint2 c = *reinterpret_cast<const uint2*>((which ? v : m) + at);
+            const uint2 c = load_codes((which ? v : m) + at);
             // the second factor is 1 but for the largest exponents, which one factor cannot hold
-            const int top = which ? v_top : m_top, most = which ? V_TOP_PLAIN : M_TOP_PLAIN, more = top > most ? top - most : 0;
+            const int top = which ? v_top : m_top, most = which ? ScaleV::PLAIN : ScaleM::PLAIN, more = top > most ? top - most : 0;
             if (which) ScaleV::decode8<false>(c, pow2i(top - more - ScaleV::FIELD), x);
             else ScaleM::decode8<true>(c, pow2i(top - more - ScaleM::FIELD), x);
             if (more) for (int k = 0; k < PER_LANE; ++k) x[k] *= pow2i(more);
@@ -825,12 +907,19 @@ int place_pointers(co3_adamw* h, const void* const* grads, void* const* weights,
     return rc;
 }
 
+template <int BITS, class W, class G>
+int launch_step_of(co3_adamw* h, const StepArgs& a, int grid, cudaStream_t st) {
+    constexpr int shared = BITS == 8 ? 2 * WARPS * Stage<W, G>::BYTES : 0;
+    static_assert(shared <= 48 * 1024, "more needs to be asked for");
+    adamw_kernel<BITS, W, G><<<grid, 32 * WARPS, shared, st>>>(a);
+    return launched(h, 1);
+}
+
 template <int BITS, class W>
 int launch_step(co3_adamw* h, const StepArgs& a, int grid, cudaStream_t st) {
-    if (h->grad_type == CO3_F32) adamw_kernel<BITS, W, F32><<<grid, 32 * WARPS, 0, st>>>(a);
-    else if (h->grad_type == CO3_BF16) adamw_kernel<BITS, W, Bf16><<<grid, 32 * WARPS, 0, st>>>(a);
-    else adamw_kernel<BITS, W, F16><<<grid, 32 * WARPS, 0, st>>>(a);
-    return launched(h, 1);
+    if (h->grad_type == CO3_F32) return launch_step_of<BITS, W, F32>(h, a, grid, st);
+    if (h->grad_type == CO3_BF16) return launch_step_of<BITS, W, Bf16>(h, a, grid, st);
+    return launch_step_of<BITS, W, F16>(h, a, grid, st);
 }
 
 }  // namespace
