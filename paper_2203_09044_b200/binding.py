@@ -5,6 +5,7 @@ library has not been built (python -m paper_2203_09044_b200.build, or __graft_en
 loading raises.  torch is used for device memory and streams only.
 """
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -562,9 +563,14 @@ def hdr_from_numpy(hdr3, device="cuda"):
 
 
 # ---- optimizer: gradient norm and AdamW over many tensors ---------------------------------------------------------
+_type_codes = {}
+
+
 def _type_code(dtype):
-    import torch
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(dtype)
+    if not _type_codes:
+        import torch
+        _type_codes.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _type_codes.get(dtype)
     if code is None:
         raise TypeError(f"float32, bfloat16 or float16 expected, got {dtype}")
     return code
@@ -603,6 +609,7 @@ class TensorList:
             if order is not None and n and _order(t) != order[i]:
                 raise ValueError(f"{what} {i}: its elements lie in another order than those of its weights")
         self.pointers = (C.c_void_p * len(sizes))(*[t.data_ptr() if n else None for t, n in zip(self.tensors, sizes)])
+        self.address, self.sizes, self.dtype = C.addressof(self.pointers), sizes, dtype
 
 
 class GradNorm:
@@ -630,8 +637,9 @@ class GradNorm:
         rc = lib().co3_adamw_create(C.byref(h), C.byref(cfg))
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_create")
-        self.handle = h
+        self.handle, self._lib = h, lib()
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._current_stream = functools.partial(torch._C._cuda_getCurrentRawStream, self.device.index)   # torch.cuda.current_stream's handle
         nb = C.c_int64()
         lib().co3_adamw_sizes(h, C.byref(nb), None)
         self.n_blocks = nb.value
@@ -647,33 +655,33 @@ class GradNorm:
         except Exception:
             pass
 
-    def _stream(self, stream, *tensors):
-        if stream is None:
-            return self.torch.cuda.current_stream(self.device).cuda_stream
-        for t in tensors:                     # the allocator must not hand their memory on while that stream uses it
+    @staticmethod
+    def _record(stream, tensors):
+        """The allocator must not hand the tensors' memory on while that stream uses it."""
+        for t in tensors:
             if t is not None:
                 t.record_stream(stream)
         return stream.cuda_stream
 
     def bind_grads(self, grads):
-        """Check the gradient tensors and keep their pointers, for programs whose gradients stay where they are."""
+        """Check the gradient tensors and keep their pointers, for programs whose gradients stay where they are.  (What another
+        optimizer's bind_grads returned is checked again.)"""
+        if type(grads) is TensorList:
+            grads = grads.tensors
         return TensorList(grads, self.sizes, self.grad_dtype, self.device, "gradients", self._order)
-
-    def _grads(self, grads):
-        return grads if type(grads) is TensorList else self.bind_grads(grads)
 
     def grad_norm(self, grads, info=None, max_norm=0.0, grad_scale=1.0, tensor_norms=None, stream=None):
         """grads: the tensors, or what bind_grads returned.  info: 4 float32 on the device, written and returned: factor, norm,
         and in the last two the count of non-finite elements as one int64 (`info[2:].view(torch.int64)`)."""
-        g = self._grads(grads)
+        g = grads if type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype else self.bind_grads(grads)
         if info is None:
             info = self.torch.empty(4, dtype=self.torch.float32, device=self.device)
         _check(info, self.torch.float32, 4, self.device, "info")
         if tensor_norms is not None:
             _check(tensor_norms, self.torch.float32, len(self.sizes), self.device, "tensor_norms")
-        s = self._stream(stream, info, tensor_norms, *(g.tensors if stream is not None else ()))
-        rc = lib().co3_grad_norm(self.handle, g.pointers, grad_scale, max_norm,
-                                 None if tensor_norms is None else tensor_norms.data_ptr(), info.data_ptr(), s)
+        s = self._current_stream() if stream is None else self._record(stream, [info, tensor_norms, *g.tensors])
+        rc = self._lib.co3_grad_norm(self.handle, g.address, grad_scale, max_norm,
+                                     None if tensor_norms is None else tensor_norms.data_ptr(), info.data_ptr(), s)
         if rc != OK:
             raise Co3Error(rc, "co3_grad_norm")
         return info
@@ -726,12 +734,13 @@ class AdamW(GradNorm):
             _check(t, kind, int(np.prod(shape)), self.device, k)
             setattr(self, k, t)
         self._state = AdamwState(*[getattr(self, k).data_ptr() if k in names else None for k in ("m", "v", "m_exp", "v_exp")])
-        self._state_p = C.byref(self._state)
+        self._state_p = C.addressof(self._state)
+        self._weights, self._copies = self.params.address, None if self.copies is None else self.copies.address
 
     def step(self, grads, info=None, lr=None, stream=None):
         """One step.  info: what grad_norm returned (its factor multiplies the gradients, and nothing is changed if it counted
         non-finite elements).  lr: a number, or one float32 on the device, in place of the optimizer's."""
-        g = self._grads(grads)
+        g = grads if type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype else self.bind_grads(grads)
         d_lr = None
         if lr is None:
             lr = self.lr
@@ -740,24 +749,28 @@ class AdamW(GradNorm):
             d_lr, lr = lr, 0.0
         if info is not None:
             _check(info, self.torch.float32, 4, self.device, "info")
-        s = self._stream(stream, info, d_lr, *(self._all(g) if stream is not None else ()))
-        rc = lib().co3_adamw_step(self.handle, self.params.pointers, g.pointers, None if self.copies is None else self.copies.pointers,
-                                  self._state_p, lr, None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
+        s = self._current_stream() if stream is None else self._record(stream, [info, d_lr, *self._all(g)])
+        rc = self._lib.co3_adamw_step(self.handle, self._weights, g.address, self._copies, self._state_p, lr,
+                                      None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_step")
 
     def _all(self, g):
-        state = [getattr(self, k) for k in ("m", "v", "m_exp", "v_exp") if hasattr(self, k)]
+        state = [self.m, self.v] if self.state_bits == 32 else [self.m, self.v, self.m_exp, self.v_exp]
         return g.tensors + self.params.tensors + (self.copies.tensors if self.copies else []) + state
 
     def state_values(self, m_out=None, v_out=None, stream=None):
         """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""
         if m_out is None or v_out is None:
             m_out, v_out = (self.torch.empty((self.n_blocks, STATE_BLOCK), dtype=self.torch.bfloat16, device=self.device) for _ in range(2))
-        for t, what in ((m_out, "m_out"), (v_out, "v_out")):
-            _check(t, m_out.dtype, self.n_blocks * STATE_BLOCK, self.device, what)
-        s = self._stream(stream, m_out, v_out, *([self.m, self.v, self.m_exp, self.v_exp] if stream is not None and self.state_bits == 8 else ()))
-        rc = lib().co3_adamw_values(self.handle, self._state_p, m_out.data_ptr(), v_out.data_ptr(), _type_code(m_out.dtype), s)
+        n, kind = self.n_blocks * STATE_BLOCK, m_out.dtype
+        _check(m_out, kind, n, self.device, "m_out")
+        _check(v_out, kind, n, self.device, "v_out")
+        if stream is None:
+            s = self._current_stream()
+        else:
+            s = self._record(stream, [m_out, v_out, *([self.m, self.v, self.m_exp, self.v_exp] if self.state_bits == 8 else [])])
+        rc = self._lib.co3_adamw_values(self.handle, self._state_p, m_out.data_ptr(), v_out.data_ptr(), _type_code(kind), s)
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_values")
         return m_out, v_out

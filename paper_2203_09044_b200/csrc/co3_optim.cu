@@ -780,9 +780,10 @@ __global__ void __launch_bounds__(32 * WARPS, 4) norm_kernel(const __grid_consta
     if (!a.tensor_norms) return;
     auto slot = [&](int k) { return k < NORM_STAGE ? stage[k] : __ldcg(&a.slots[k]); };
     const double scale = fabs((double)a.grad_scale);
-    for (int t0 = warp * 32; t0 < a.n_tensors; t0 += 32 * WARPS) {
-        // a lane per tensor; those with many slots are then added by the whole warp
-        const int t = t0 + lane;
+    for (int t0 = warp; t0 < a.n_tensors; t0 += 32 * WARPS) {
+        // a lane per tensor; those with many slots are then added by the whole warp (neighbours, which may both have many, to
+        // different warps)
+        const int t = t0 + lane * WARPS;
         int k0 = 0, k1 = 0;
         if (t < a.n_tensors) {
             const Tensor tn = a.tensors[t];
@@ -1061,12 +1062,20 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     // block_whole takes roots of numbers below 2^-126 as 0.  Beside eps that is less than 2^-24 of the denominator if eps is above
     // 2^24 * 2^-63 / sqrt(1 - beta2) (6e-11 for beta2 = 0.999); a smaller eps takes the general way.
     a.fast = h->eps * sqrt(1.0 - h->beta2) >= 0x1p-39;
-    // Blocks of one warp: as many as leave every place for a thread block four of them one after the other, so that the SMs end
-    // together, and at most 4 with 32-bit moments (2^28 f32: 1, 2, 4, 8, 16 blocks take 1214, 1115, 1097, 1114, 1125 us), 16 with
-    // 8-bit ones (2^28: 1493, 1186, 1083, 1044, 1023 us): their exponents are bytes, and 128 of them side by side make a line that
-    // no other thread block writes.  (Written block by block, with the dies handing the line to and fro, 4 blocks took 2434 us.)
-    const int64_t per_warp = h->n_blocks / ((int64_t)h->num_sms * STEP_CTAS * WARPS * 4), most = h->state_bits == 8 ? STRETCH / WARPS : 4;
-    a.stretch = (int)(WARPS * (per_warp < 1 ? 1 : per_warp > most ? most : per_warp));
+    // Blocks of one thread block.  32-bit moments: one warp takes as many as leave every place for a thread block four of them one
+    // after the other, so that the SMs end together, and at most 4 (2^28 f32: 1, 2, 4, 8, 16 take 1214, 1115, 1097, 1114, 1125 us).
+    // 8-bit moments: whole rounds over all places, of at most 128 blocks (11.2M f32: 24 blocks in four and a bit rounds 39.4 us, 99
+    // in one 36.9; 2^28: 8, 16, 32, 64, 128 blocks 1493, 1186, 1083, 1044, 1023 us).  Their exponents are bytes side by side, and
+    // a line of them that thread blocks on both dies write has each of them wait for the other.
+    const int64_t places = (int64_t)h->num_sms * STEP_CTAS;
+    if (h->state_bits == 8) {
+        const int64_t rounds = (h->n_blocks + places * STRETCH - 1) / (places * STRETCH);
+        const int64_t each = rounds ? (h->n_blocks + places * rounds - 1) / (places * rounds) : 0;
+        a.stretch = (int)(each < WARPS ? WARPS : each);
+    } else {
+        const int64_t per_warp = h->n_blocks / (places * WARPS * 4);
+        a.stretch = (int)(WARPS * (per_warp < 1 ? 1 : per_warp > 4 ? 4 : per_warp));
+    }
     const int grid = h->n_blocks ? (int)((h->n_blocks + a.stretch - 1) / a.stretch) : 1;
     const bool w16 = h->weight_type == CO3_BF16;
     if (h->state_bits == 32) return w16 ? launch_step<32, Bf16>(h, a, grid, st) : launch_step<32, F32>(h, a, grid, st);

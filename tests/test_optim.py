@@ -581,3 +581,18 @@ def test_no_elements_at_all(binding, bits):
     assert info[:2].tolist() == [1.0, 0.0]
     opt.step([p, p], info)
     assert opt.steps() == 1 and opt.n_blocks == 0
+
+
+@pytest.mark.gpu
+def test_bound_gradients_of_another_optimizer_are_checked_again(binding):
+    b = binding
+    p, q = [torch.ones(300, device="cuda")], [torch.ones(5000, device="cuda")]
+    small, large = b.AdamW(p), b.AdamW(q)
+    bound = small.bind_grads([torch.ones(300, device="cuda")])
+    small.step(bound)
+    with pytest.raises(ValueError, match="5000 elements"):
+        large.step(bound)
+    with pytest.raises(ValueError, match="bfloat16"):
+        b.AdamW(p, grad_dtype=torch.bfloat16).grad_norm(bound)
+    b.AdamW([torch.ones(300, device="cuda")]).step(bound)          # fits: used as it is
+    assert large.steps() == 0
