@@ -19,10 +19,10 @@ constexpr int BLK = 256;                      // elements of a block
 constexpr int WARPS = 8;                      // warps of a thread block
 constexpr int PER_LANE = BLK / 32;
 constexpr int INLINE_TENSORS = 128;           // pointers of so many tensors travel with the launch itself
-constexpr int TABLE_TENSORS = 1300;           // ... and of so many with one launch of the kernel that fills the device table
+constexpr int TABLE_FEW = 400, TABLE_MANY = 1300;   // ... and of so many with one launch of the kernel that fills the device table
 constexpr int MAX_TENSORS = 1 << 20;
-constexpr int NORM_CTAS = 592;                // thread blocks of the norm at most: four on each of 148 SMs, whatever the device,
-                                              // so that a sum does not depend on where it is formed
+constexpr int NORM_PER_SM = 3;                // thread blocks of the norm on an SM (2^26 f32: 3 take 44 us, 4 with fewer registers 46)
+constexpr int NORM_CTAS = NORM_PER_SM * 148;  // ... and in all at most, whatever the device, so that a sum does not depend on it
 
 struct Pointers {
     const void* grad;
@@ -46,6 +46,7 @@ struct Scalars {
     alignas(256) uint32_t ticket;
     uint32_t norm_ticket, flags;
     unsigned long long skipped_elements, skipped_steps;
+    unsigned long long nonfinite;             // of the gradients that the norm is reading
 };
 
 // Published multiply-and-shift mixing of 32 bits (two odd constants): any input bit reaches every output bit.
@@ -75,6 +76,11 @@ __device__ __forceinline__ uint32_t block_key(uint32_t key, int64_t place) {
 __device__ __forceinline__ float pow2i(int e) {          // 2^e, -149 <= e <= 127
     return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << (e + 149));
 }
+
+// A kernel of this file may start while the one before it on the stream still runs.  It then reads what was fixed when the handle
+// was made, and waits for the end of the other, and for its writes, before anything else.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Two 32-bit operations in one instruction, each rounded by itself as the single ones are.
 struct Pair {
@@ -127,6 +133,12 @@ struct F32 {
     }
     static constexpr uintptr_t ALIGN = 31;
     static __device__ __forceinline__ float to(float x) { return x; }
+    struct Raw { float x[8]; };                           // eight elements as they lie in memory
+    static __device__ __forceinline__ Raw load_raw(const float* p) { Raw r; load8(p, r.x); return r; }
+    static __device__ __forceinline__ void unpack_raw(const Raw& r, float* x) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = r.x[k];
+    }
     static __device__ __forceinline__ void load8(const float* p, float* x) {
         asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
@@ -140,7 +152,10 @@ struct Bf16 {
     typedef __nv_bfloat16 type;
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __bfloat162float(x); }
-    static __device__ __forceinline__ void load8(const type* p, float* x) { const uint4 u = load16(p); unpack(&u, x); }
+    typedef uint4 Raw;
+    static __device__ __forceinline__ Raw load_raw(const type* p) { return load16(p); }
+    static __device__ __forceinline__ void unpack_raw(const Raw& u, float* x) { unpack(&u, x); }
+    static __device__ __forceinline__ void load8(const type* p, float* x) { unpack_raw(load_raw(p), x); }
     static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
         const uint32_t w[4] = {u->x, u->y, u->z, u->w};
 #pragma unroll
@@ -157,7 +172,10 @@ struct F16 {
     typedef __half type;
     static constexpr uintptr_t ALIGN = 15;
     static __device__ __forceinline__ float to(type x) { return __half2float(x); }
-    static __device__ __forceinline__ void load8(const type* p, float* x) { const uint4 u = load16(p); unpack(&u, x); }
+    typedef uint4 Raw;
+    static __device__ __forceinline__ Raw load_raw(const type* p) { return load16(p); }
+    static __device__ __forceinline__ void unpack_raw(const Raw& u, float* x) { unpack(&u, x); }
+    static __device__ __forceinline__ void load8(const type* p, float* x) { unpack_raw(load_raw(p), x); }
     static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
         const uint32_t w[4] = {u->x, u->y, u->z, u->w};
 #pragma unroll
@@ -512,25 +530,30 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __gr
     const int warp = threadIdx.x >> 5;
     const int64_t begin = (int64_t)blockIdx.x * a.stretch;
     const int end = (int)min(begin + a.stretch, a.n_blocks), count = end - (int)begin;
-    const bool skip = a.info && a.info->nonfinite != 0;
-    const float lr = a.d_lr ? *a.d_lr : a.lr;
     Step s;
+    float tensor_decay = 0.0f;
     int end_t = 0, whole_t = 0;                           // of the tensor: block past its last, block past its last usual one
     Bases p = {0, 0, 0};
-    auto look_up = [&](int b) {
-        const int t = a.owner[b];
-        const Tensor tn = a.tensors[t];
+    int t = 0;
+    Tensor tn = {0, 0, 0.0f, 0};
+    auto find = [&](int b) { t = a.owner[b]; tn = a.tensors[t]; };
+    auto enter = [&] {
         const Pointers at = a.table ? a.table[t] : a.inline_ptr[t];
         const uintptr_t e = (uintptr_t)tn.block0 * BLK;
         p = {(uintptr_t)at.weight - e * sizeof(typename W::type), (uintptr_t)at.grad - e * sizeof(typename G::type), (uintptr_t)at.copy - e * 2};
         end_t = (int)(tn.block0 + (tn.size + BLK - 1) / BLK);
         const bool aligned = !(((uintptr_t)at.weight & W::ALIGN) | ((uintptr_t)at.grad & G::ALIGN) | ((uintptr_t)at.copy & 15));
         whole_t = a.fast && aligned ? (int)(tn.block0 + tn.size / BLK) : 0;
-        s.decay = lr * tn.decay;
+        tensor_decay = tn.decay;
     };
     // a stretch of blocks per thread block, one after the other to its warps
     int b = (int)begin + warp;
-    if (b < end) look_up(b);
+    let_next_start();
+    if (b < end) find(b);
+    wait_for_previous();
+    if (b < end) enter();
+    const bool skip = a.info && a.info->nonfinite != 0;
+    const float lr = a.d_lr ? *a.d_lr : a.lr;
     Stage<W, G> stage = {(uint32_t)__cvta_generic_to_shared(stages) + 2 * warp * Stage<W, G>::BYTES};
     uint32_t to_other = Stage<W, G>::BYTES;
     bool have = false;                                    // block b is on its way to `stage`
@@ -550,7 +573,8 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __gr
     uint32_t kept = 0;
     if (!skip) {
         for (; b < end; b += WARPS) {
-            if (b >= end_t) look_up(b);
+            if (b >= end_t) { find(b); enter(); }
+            s.decay = lr * tensor_decay;
             const uint32_t key = block_key(step_key, (int64_t)b * BLK);
             if (BITS == 8) {
                 if (!have && b < whole_t) {
@@ -603,10 +627,11 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __gr
 }
 
 // ---- gradient norm ------------------------------------------------------------------------------------------------------
-// Thread block c takes the blocks c*K .. c*K + K-1, warp w an eighth of them in a row, and leaves one partial sum for every
-// tensor that it meets, at slot c + tensor: going on to the next thread block or to the next tensor moves at least one slot on,
-// so the slots are all different, and those of a tensor lie side by side.  Slots that nothing maps to stay zero.  The thread
-// block that finishes last adds them up, always in the same order.
+// Thread block c takes the blocks c*K .. c*K + K-1 and leaves one partial sum for every tensor that it meets, at slot c + tensor:
+// going on to the next thread block or to the next tensor moves at least one slot on, so the slots are all different, and those of
+// a tensor lie side by side.  Slots that nothing maps to stay zero.  The thread block that finishes last adds them up, always in
+// the same order.  Within a thread block, all warps share the blocks of a large piece of a tensor, in turn, so that together they
+// read one stretch of memory (a stretch of its own for each warp: 94 us for 2^28 bf16, against 86); small pieces go to one warp each.
 struct NormArgs {
     const Tensor* tensors;
     const int32_t* owner;
@@ -615,15 +640,15 @@ struct NormArgs {
     int n_tensors, n_slots;
     float grad_scale, max_norm;
     double* slots;
-    unsigned long long* bad;                  // per thread block
     float* tensor_norms;
     co3_grad_info* info;
     Scalars* sc;
     Pointers inline_ptr[INLINE_TENSORS];
 };
 
-constexpr int NORM_UNROLL = 4;                // blocks whose loads a warp has in flight
-constexpr int NORM_STAGE = 2048;              // slots that the last thread block brings into shared memory
+template <class G> constexpr int NORM_UNROLL = sizeof(typename G::type) == 2 ? 6 : 3;    // blocks whose loads a warp has in flight
+constexpr int NORM_SHARED = 32;               // pieces of tensors that the warps of a thread block share, at most
+constexpr int NORM_STAGE = 1024;              // slots that the last thread block brings into shared memory
 
 template <typename T>
 __device__ __forceinline__ T warp_sum(T x) {
@@ -644,12 +669,22 @@ __device__ __forceinline__ T block_sum(T x, T* sh) {      // same value in every
     return s;
 }
 
-// The square of a 32-bit float is exact in 64 bits: no range is lost, and the sum rounds at 2^-53.
+// The square of a 32-bit float is exact in 64 bits: no range is lost, and the sum rounds at 2^-53.  The conversions (16 a clock on an
+// SM) would bind with 16-bit elements: the squares of those are exact in 32 bits too, so that two of them are added there, with
+// one rounding, where all of a lane's eight are of a size that leaves their squares in range.
+template <class G>
 __device__ __forceinline__ void add_squares(const float* x, double& s0, double& s1, uint32_t& bad) {
     uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < PER_LANE; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-    if (top < 0x7F800000u) {
+    for (int k = 0; k < PER_LANE; k += 2) top = __vimax3_u32(top, __float_as_uint(x[k]) & 0x7FFFFFFFu, __float_as_uint(x[k + 1]) & 0x7FFFFFFFu);
+    if (sizeof(typename G::type) == 2 && top - 0x26800000u < 0x37000000u) {     // 2^-50 <= top < 2^60
+#pragma unroll
+        for (int k = 0; k < PER_LANE; k += 4) {
+            s0 += (double)(x[k] * x[k] + x[k + 1] * x[k + 1]);
+            s1 += (double)(x[k + 2] * x[k + 2] + x[k + 3] * x[k + 3]);
+        }
+    } else if (top < 0x7F800000u) {
+        if (sizeof(typename G::type) == 2 && top == 0) return;
 #pragma unroll
         for (int k = 0; k < PER_LANE; k += 2) {
             const double d0 = (double)x[k], d1 = (double)x[k + 1];
@@ -666,139 +701,166 @@ __device__ __forceinline__ void add_squares(const float* x, double& s0, double& 
     }
 }
 
-template <class G, bool ALIGNED>
-__device__ __forceinline__ void load_block(const typename G::type* g, float* x) {
-    const int lane = threadIdx.x & 31;
-    if (ALIGNED) {
-        G::load8(g + PER_LANE * lane, x);
-    } else {
+// A lane's part of a block, eight elements side by side or 32 apart.
+template <class G, bool ALIGNED> struct Part {
+    typename G::Raw raw;
+    __device__ __forceinline__ void load(const typename G::type* g) { raw = G::load_raw(g + PER_LANE * (threadIdx.x & 31)); }
+    __device__ __forceinline__ void get(float* x) const { G::unpack_raw(raw, x); }
+};
+template <class G> struct Part<G, false> {
+    typename G::type raw[PER_LANE];
+    __device__ __forceinline__ void load(const typename G::type* g) {
 #pragma unroll
-        for (int k = 0; k < PER_LANE; ++k) x[k] = G::to(g[lane + 32 * k]);
+        for (int k = 0; k < PER_LANE; ++k) raw[k] = g[(threadIdx.x & 31) + 32 * k];
     }
-}
+    __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+        for (int k = 0; k < PER_LANE; ++k) x[k] = G::to(raw[k]);
+    }
+};
 
-// `count` blocks of one tensor from element e0 on, the last of them perhaps not whole.
+// The blocks of a tensor from `first` to below `end`, or every turns-th group of U of them.
 template <class G, bool ALIGNED>
-__device__ __forceinline__ double squares(const typename G::type* g, int64_t e0, int64_t count, int64_t size, uint32_t& bad) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ double squares(const typename G::type* g, int64_t first, int64_t end, int turns, int64_t size, uint32_t& bad) {
+    constexpr int U = ALIGNED ? NORM_UNROLL<G> : 2;       // 16-bit elements one by one take a register each
     double s0 = 0.0, s1 = 0.0;
-    const int64_t whole = min(count, (size - e0) / BLK);
-    g += e0;
-    int64_t k = 0;
-    for (; k + NORM_UNROLL <= whole; k += NORM_UNROLL, g += NORM_UNROLL * BLK) {
-        float x[NORM_UNROLL][PER_LANE];
+    float x[PER_LANE];
+    const int64_t whole = min(end, size / BLK);
+    first += (turns > 1 ? (threadIdx.x >> 5) * U : 0);
+    g += first * BLK;
+    const int stride = U * turns;
+    for (int left = (int)(whole - first); left > 0; left -= stride, g += (int64_t)stride * BLK) {
+        Part<G, ALIGNED> part[U];
 #pragma unroll
-        for (int u = 0; u < NORM_UNROLL; ++u) load_block<G, ALIGNED>(g + u * BLK, x[u]);
+        for (int u = 0; u < U; ++u) if (u < left) part[u].load(g + u * BLK);
 #pragma unroll
-        for (int u = 0; u < NORM_UNROLL; ++u) add_squares(x[u], s0, s1, bad);
-    }
-    for (; k < whole; ++k, g += BLK) {
-        float x[PER_LANE];
-        load_block<G, ALIGNED>(g, x);
-        add_squares(x, s0, s1, bad);
-    }
-    if (whole < count) {
-        const int n = (int)(size - e0 - whole * BLK);
-        float x[PER_LANE];
-#pragma unroll
-        for (int j = 0; j < PER_LANE; ++j) x[j] = lane + 32 * j < n ? G::to(g[lane + 32 * j]) : 0.0f;
-        add_squares(x, s0, s1, bad);
+        for (int u = 0; u < U; ++u) if (u < left) { part[u].get(x); add_squares<G>(x, s0, s1, bad); }
     }
     return s0 + s1;
 }
 
+// A tensor's last block, not whole.
 template <class G>
-__global__ void __launch_bounds__(32 * WARPS, 4) norm_kernel(const __grid_constant__ NormArgs a) {
-    __shared__ double sh[WARPS], edge_sum[2 * WARPS], stage[NORM_STAGE];
-    __shared__ unsigned long long sh_n[WARPS];
-    __shared__ int edge[2 * WARPS];           // tensors of the warps' first and last sums, which neighbours may share; -1: none
+__device__ __forceinline__ double squares_end(const typename G::type* g, int64_t size, uint32_t& bad) {
+    const int lane = threadIdx.x & 31, n = (int)(size % BLK);
+    double s0 = 0.0, s1 = 0.0;
+    float x[PER_LANE];
+    g += size - n;
+#pragma unroll
+    for (int j = 0; j < PER_LANE; ++j) x[j] = lane + 32 * j < n ? G::to(g[lane + 32 * j]) : 0.0f;
+    add_squares<G>(x, s0, s1, bad);
+    return s0 + s1;
+}
+
+template <class G>
+__global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ double sh[WARPS], stage[NORM_STAGE], shared_sum[NORM_SHARED][WARPS];
+    __shared__ int shared_tensor[NORM_SHARED];
     __shared__ bool last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c0 = blockIdx.x * a.per_cta, c1 = min(c0 + a.per_cta, a.n_blocks);
-    const int64_t b1 = min(c0 + (warp + 1) * a.per_cta / WARPS, c1);
-    if (threadIdx.x < 2 * WARPS) edge[threadIdx.x] = -1;
-    __syncthreads();
+    const int large = max(WARPS, (int)(a.per_cta / NORM_SHARED) + 1);           // so that at most NORM_SHARED pieces are large
     uint32_t bad = 0;
+    int n_shared = 0, n_small = 0;
+    int base = c0 < c1 ? a.owner[c0] : 0;
+    bool more = c0 < c1;
+    let_next_start();
     bool first = true;
-    for (int64_t b = c0 + warp * a.per_cta / WARPS; b < b1;) {
-        const int t = a.owner[b];
-        const Tensor tn = a.tensors[t];
-        const typename G::type* g = static_cast<const typename G::type*>((a.table ? a.table[t] : a.inline_ptr[t]).grad);
-        const int64_t end = min(b1, tn.block0 + (tn.size + BLK - 1) / BLK);
-        const int64_t e0 = (b - tn.block0) * BLK;
-        double s = (uintptr_t)g & G::ALIGN ? squares<G, false>(g, e0, end - b, tn.size, bad) : squares<G, true>(g, e0, end - b, tn.size, bad);
-        s = warp_sum(s);
-        b = end;
-        if (lane == 0) {
-            if (first || b == b1) { const int k = 2 * warp + (first ? 0 : 1); edge[k] = t; edge_sum[k] = s; }
-            else a.slots[blockIdx.x + t] = s;             // begins and ends within this warp's blocks
-        }
+    while (more || first) {
+        // 32 tensors at a time, one to a lane
+        int64_t block0 = 0, size = 0;
+        if (more && base + lane < a.n_tensors) { block0 = a.tensors[base + lane].block0; size = a.tensors[base + lane].size; }
+        if (first) wait_for_previous();
         first = false;
-    }
-    const unsigned long long n_bad = block_sum((unsigned long long)bad, sh_n);       // its barriers also order edge[]
-    if (threadIdx.x == 0) {
-        a.bad[blockIdx.x] = n_bad;
-        int t = -1;
-        double s = 0.0;
-        for (int k = 0; k < 2 * WARPS; ++k) {             // neighbours with the same tensor add up
-            if (edge[k] < 0) continue;
-            if (edge[k] != t) {
-                if (t >= 0) a.slots[blockIdx.x + t] = s;
-                t = edge[k];
-                s = 0.0;
+        const int64_t f = max(block0, c0), e = min(block0 + (size + BLK - 1) / BLK, c1);
+        uint32_t pieces = __ballot_sync(0xffffffffu, more && size > 0 && f < e);
+        for (; pieces; pieces &= pieces - 1) {
+            const int who = __ffs(pieces) - 1, t = base + who;
+            const int64_t b0 = __shfl_sync(0xffffffffu, block0, who), n = __shfl_sync(0xffffffffu, size, who);
+            const int64_t from = __shfl_sync(0xffffffffu, f, who) - b0, to = __shfl_sync(0xffffffffu, e, who) - b0;
+            const bool share = to - from >= large;
+            if (!share && (n_small++ & (WARPS - 1)) != warp) continue;
+            int64_t at = from, end = to;
+            int turns = 1;
+            if (share) {
+                if (to - from >= 8 * WARPS) turns = WARPS;
+                else { at = from + (to - from) * warp / WARPS; end = from + (to - from) * (warp + 1) / WARPS; }
             }
-            s += edge_sum[k];
+            const typename G::type* g = static_cast<const typename G::type*>((a.table ? a.table[t] : a.inline_ptr[t]).grad);
+            double s = (uintptr_t)g & G::ALIGN ? squares<G, false>(g, at, end, turns, n, bad) : squares<G, true>(g, at, end, turns, n, bad);
+            if (to * BLK > n && (!share || warp == WARPS - 1)) s += squares_end<G>(g, n, bad);
+            s = warp_sum(s);
+            if (lane == 0) {
+                if (share) { shared_sum[n_shared][warp] = s; shared_tensor[n_shared] = t; }
+                else a.slots[blockIdx.x + t] = s;
+            }
+            n_shared += share;
         }
-        if (t >= 0) a.slots[blockIdx.x + t] = s;
+        // done once a tensor reaches beyond this thread block's blocks, or none is left
+        more = more && !__any_sync(0xffffffffu, size > 0 && block0 + (size + BLK - 1) / BLK >= c1) && base + 32 < a.n_tensors;
+        base += 32;
     }
-    __threadfence();
+    if (bad) atomicAdd(&a.sc->nonfinite, (unsigned long long)bad);             // rare
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(&a.sc->norm_ticket, 1u) == gridDim.x - 1;
+    if (threadIdx.x < n_shared) {
+        double s = 0.0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) s += shared_sum[threadIdx.x][w];
+        a.slots[blockIdx.x + shared_tensor[threadIdx.x]] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();                                  // of the whole block's writes, which the barrier put before it
+        last = atomicAdd(&a.sc->norm_ticket, 1u) == gridDim.x - 1;
+        __threadfence();
+    }
     __syncthreads();
     if (!last) return;
-    __threadfence();
 
+    // The sums, and where each tensor's lie, on their way together.
     double total = 0.0;
     for (int k = threadIdx.x; k < a.n_slots; k += 32 * WARPS) {
         const double x = __ldcg(&a.slots[k]);
         total += x;
         if (k < NORM_STAGE) stage[k] = x;
     }
-    unsigned long long all_bad = 0;
-    for (unsigned k = threadIdx.x; k < gridDim.x; k += 32 * WARPS) all_bad += __ldcg(&a.bad[k]);
+    auto range = [&](int t) {
+        const Tensor tn = a.tensors[t];
+        int2 k = {0, 0};
+        if (tn.size > 0) {
+            k.x = (int)(tn.block0 / a.per_cta) + t;
+            k.y = (int)((tn.block0 + (tn.size - 1) / BLK) / a.per_cta) + t + 1;
+        }
+        return k;
+    };
+    const int mine = lane * WARPS + warp;                 // the tensors of a warp lie apart: neighbours may both have many slots
+    int2 k = {0, 0};
+    if (a.tensor_norms && mine < a.n_tensors) k = range(mine);
     total = block_sum(total, sh);
-    all_bad = block_sum(all_bad, sh_n);
     if (threadIdx.x == 0) {
         const double norm = sqrt(total) * fabs((double)a.grad_scale);
         double factor = a.grad_scale;
         if (a.max_norm > 0.0f && norm > (double)a.max_norm) factor *= (double)a.max_norm / norm;
         a.info->factor = (float)factor;
         a.info->norm = (float)norm;
-        a.info->nonfinite = all_bad;
+        a.info->nonfinite = __ldcg(&a.sc->nonfinite);
+        a.sc->nonfinite = 0;
         a.sc->norm_ticket = 0;
     }
     if (!a.tensor_norms) return;
-    auto slot = [&](int k) { return k < NORM_STAGE ? stage[k] : __ldcg(&a.slots[k]); };
+    auto slot = [&](int i) { return i < NORM_STAGE ? stage[i] : __ldcg(&a.slots[i]); };
     const double scale = fabs((double)a.grad_scale);
-    for (int t0 = warp; t0 < a.n_tensors; t0 += 32 * WARPS) {
-        // a lane per tensor; those with many slots are then added by the whole warp (neighbours, which may both have many, to
-        // different warps)
-        const int t = t0 + lane * WARPS;
-        int k0 = 0, k1 = 0;
-        if (t < a.n_tensors) {
-            const Tensor tn = a.tensors[t];
-            if (tn.size > 0) {
-                k0 = (int)(tn.block0 / a.per_cta) + t;
-                k1 = (int)((tn.block0 + (tn.size - 1) / BLK) / a.per_cta) + t + 1;
-            }
-        }
-        const bool many = k1 - k0 > 8;
+    for (int t0 = 0; t0 < a.n_tensors; t0 += 32 * WARPS) {
+        // a lane per tensor; those with many slots are then added by the whole warp
+        const int t = t0 + mine;
+        if (t0) k = t < a.n_tensors ? range(t) : int2{0, 0};
+        const bool many = k.y - k.x > 8;
         double x = 0.0;
-        if (!many) for (int k = k0; k < k1; ++k) x += slot(k);
+        if (!many) for (int i = k.x; i < k.y; ++i) x += slot(i);
         for (uint32_t left = __ballot_sync(0xffffffffu, many); left; left &= left - 1) {
-            const int who = __ffs(left) - 1, f = __shfl_sync(0xffffffffu, k0, who), l = __shfl_sync(0xffffffffu, k1, who);
+            const int who = __ffs(left) - 1, f = __shfl_sync(0xffffffffu, k.x, who), l = __shfl_sync(0xffffffffu, k.y, who);
             double y = 0.0;
-            for (int k = f + lane; k < l; k += 32) y += slot(k);
+            for (int i = f + lane; i < l; i += 32) y += slot(i);
             y = warp_sum(y);
             if (lane == who) x = y;
         }
@@ -811,6 +873,8 @@ template <class T>
 __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp,
                                                             int64_t n_blocks, typename T::type* m_out, typename T::type* v_out) {
     const int lane = threadIdx.x & 31;
+    let_next_start();
+    wait_for_previous();
     for (int64_t b = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5); b < n_blocks; b += (int64_t)gridDim.x * WARPS) {
         const int m_top = m_exp[b], v_top = v_exp[b];
         const int64_t at = b * BLK + PER_LANE * lane;
@@ -839,12 +903,14 @@ __global__ void owner_kernel(const Tensor* tensors, int n_tensors, int32_t* owne
     }
 }
 
-struct TableArgs {
-    Pointers ptr[TABLE_TENSORS];
+template <int N> struct TableArgs {
+    Pointers ptr[N];
 };
 
-__global__ void table_kernel(const __grid_constant__ TableArgs a, Pointers* table, int count) {
+template <int N> __global__ void table_kernel(const __grid_constant__ TableArgs<N> a, Pointers* table, int count) {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    let_next_start();
+    wait_for_previous();
     if (i < count) table[i] = a.ptr[i];
 }
 
@@ -864,15 +930,26 @@ struct co3_adamw {
     Pointers* table;                          // only with more than INLINE_TENSORS tensors
     Scalars* sc;
     double* slots;
-    unsigned long long* bad;
     int64_t launches;
 };
 
 namespace {
 
-int launched(co3_adamw* h, int n) {
-    if (cudaGetLastError() != cudaSuccess) return CO3_ECUDA;
-    h->launches += n;
+// See let_next_start.
+template <class... P, class... A>
+int launch(co3_adamw* h, void (*kernel)(P...), int grid, int threads, int shared, cudaStream_t st, const A&... args) {
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)shared;
+    cfg.stream = st;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
+    h->launches += 1;
     return CO3_OK;
 }
 
@@ -895,14 +972,16 @@ int place_pointers(co3_adamw* h, const void* const* grads, void* const* weights,
         for (int t = 0; t < h->n_tensors; ++t) in_args[t] = one(t);
         return CO3_OK;
     }
-    TableArgs* args = (TableArgs*)malloc(sizeof(TableArgs));
+    TableArgs<TABLE_MANY>* args = (TableArgs<TABLE_MANY>*)malloc(sizeof(TableArgs<TABLE_MANY>));
     if (!args) return CO3_ENOMEM;
     int rc = CO3_OK;
-    for (int t0 = 0; t0 < h->n_tensors && rc == CO3_OK; t0 += TABLE_TENSORS) {
-        const int count = h->n_tensors - t0 < TABLE_TENSORS ? h->n_tensors - t0 : TABLE_TENSORS;
+    for (int t0 = 0; t0 < h->n_tensors && rc == CO3_OK; t0 += TABLE_MANY) {
+        const int count = h->n_tensors - t0 < TABLE_MANY ? h->n_tensors - t0 : TABLE_MANY;
         for (int i = 0; i < count; ++i) args->ptr[i] = one(t0 + i);
-        table_kernel<<<(count + 255) / 256, 256, 0, st>>>(*args, h->table + t0, count);
-        rc = launched(h, 1);
+        if (count <= TABLE_FEW)               // the arguments of a launch are copied whole
+            rc = launch(h, table_kernel<TABLE_FEW>, (count + 255) / 256, 256, 0, st, *(const TableArgs<TABLE_FEW>*)args, h->table + t0, count);
+        else
+            rc = launch(h, table_kernel<TABLE_MANY>, (count + 255) / 256, 256, 0, st, *args, h->table + t0, count);
     }
     free(args);
     return rc;
@@ -912,8 +991,7 @@ template <int BITS, class W, class G>
 int launch_step_of(co3_adamw* h, const StepArgs& a, int grid, cudaStream_t st) {
     constexpr int shared = BITS == 8 ? 2 * WARPS * Stage<W, G>::BYTES : 0;
     static_assert(shared <= 48 * 1024, "more needs to be asked for");
-    adamw_kernel<BITS, W, G><<<grid, 32 * WARPS, shared, st>>>(a);
-    return launched(h, 1);
+    return launch(h, adamw_kernel<BITS, W, G>, grid, 32 * WARPS, shared, st, a);
 }
 
 template <int BITS, class W>
@@ -986,13 +1064,13 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
         auto part = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
         const size_t o_sc = part(sizeof(Scalars)), o_t = part(sizeof(Tensor) * (size_t)n), o_own = part(4 * (size_t)blocks);
         const size_t o_tab = part(n > INLINE_TENSORS ? sizeof(Pointers) * (size_t)n : 0);
-        const size_t o_slots = part(8 * (size_t)h->n_slots), o_bad = part(8 * (size_t)h->norm_grid);
+        const size_t o_slots = part(8 * (size_t)h->n_slots);
         if (cudaMalloc(&h->slab, at) != cudaSuccess) { (void)cudaGetLastError(); h->slab = nullptr; rc = CO3_ENOMEM; }
         else {
             char* base = (char*)h->slab;
             h->sc = (Scalars*)(base + o_sc); h->tensors = (Tensor*)(base + o_t); h->owner = (int32_t*)(base + o_own);
             h->table = n > INLINE_TENSORS ? (Pointers*)(base + o_tab) : nullptr;
-            h->slots = (double*)(base + o_slots); h->bad = (unsigned long long*)(base + o_bad);
+            h->slots = (double*)(base + o_slots);
             Scalars s;
             memset(&s, 0, sizeof(s));
             s.pow1 = s.pow2 = 1.0;
@@ -1031,11 +1109,11 @@ extern "C" int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_
     if (rc != CO3_OK) return rc;
     a.tensors = h->tensors; a.owner = h->owner; a.table = h->table; a.n_blocks = h->n_blocks; a.per_cta = h->per_cta;
     a.n_tensors = h->n_tensors; a.n_slots = h->n_slots; a.grad_scale = grad_scale; a.max_norm = max_norm;
-    a.slots = h->slots; a.bad = h->bad; a.tensor_norms = tensor_norms; a.info = info; a.sc = h->sc;
-    if (h->grad_type == CO3_F32) norm_kernel<F32><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
-    else if (h->grad_type == CO3_BF16) norm_kernel<Bf16><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
-    else norm_kernel<F16><<<h->norm_grid, 32 * WARPS, 0, st>>>(a);
-    return launched(h, 1);
+    a.slots = h->slots; a.tensor_norms = tensor_norms; a.info = info; a.sc = h->sc;
+    const int threads = 32 * WARPS;
+    if (h->grad_type == CO3_F32) return launch(h, norm_kernel<F32>, h->norm_grid, threads, 0, st, a);
+    if (h->grad_type == CO3_BF16) return launch(h, norm_kernel<Bf16>, h->norm_grid, threads, 0, st, a);
+    return launch(h, norm_kernel<F16>, h->norm_grid, threads, 0, st, a);
 }
 
 extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* const* grads, void* const* copies, const co3_adamw_state* state,
@@ -1093,10 +1171,10 @@ extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void
     const int grid = (int)(need < most ? need : most);
     const uint8_t *m = (const uint8_t*)state->m, *v = (const uint8_t*)state->v;
     if (value_type == CO3_F32)
-        values_kernel<F32><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (float*)m_values, (float*)v_values);
-    else
-        values_kernel<Bf16><<<grid, 32 * WARPS, 0, st>>>(m, v, state->m_exp, state->v_exp, h->n_blocks, (__nv_bfloat16*)m_values, (__nv_bfloat16*)v_values);
-    return launched(h, 1);
+        return launch(h, values_kernel<F32>, grid, 32 * WARPS, 0, st, m, v, (const uint8_t*)state->m_exp, (const uint8_t*)state->v_exp, h->n_blocks,
+                      (float*)m_values, (float*)v_values);
+    return launch(h, values_kernel<Bf16>, grid, 32 * WARPS, 0, st, m, v, (const uint8_t*)state->m_exp, (const uint8_t*)state->v_exp, h->n_blocks,
+                  (__nv_bfloat16*)m_values, (__nv_bfloat16*)v_values);
 }
 
 extern "C" int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped_elements, uint64_t* skipped_steps, int32_t clear) {
