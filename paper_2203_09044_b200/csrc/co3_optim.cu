@@ -249,11 +249,12 @@ template <int TOP> struct Scale {
             if (SIGNED) {
                 const uint32_t s[4] = {__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), __float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3])};
                 pack[h] |= upper_bytes(s) & 0x80808080u;
-            } else if ((pack[h] - 0x01010101u) & ~pack[h] & 0x80808080u) {     // some code is zero: a positive value never is
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (!(pack[h] >> (8 * k) & 0xFFu) && x[4 * h + k] > 0.0f) pack[h] |= 1u << (8 * k);
             }
+        }
+        if (!SIGNED && ((((pack[0] - 0x01010101u) & ~pack[0]) | ((pack[1] - 0x01010101u) & ~pack[1])) & 0x80808080u)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)                                        // some code is zero: a positive value never is
+                if (!(pack[k / 4] >> (8 * (k & 3)) & 0xFFu) && x[k] > 0.0f) pack[k / 4] |= 1u << (8 * (k & 3));
         }
         return make_uint2(pack[0], pack[1]);
     }
@@ -316,7 +317,7 @@ __device__ __forceinline__ void moments(float& m, float& v, float g, const StepA
 }
 
 constexpr int STRETCH = 128;                  // blocks of a thread block at most
-constexpr int STEP_CTAS = 3;                  // thread blocks of the step on an SM
+template <int BITS> constexpr int STEP_CTAS = BITS == 8 ? 4 : 3;                  // thread blocks of the step on an SM
 
 // Root and quotient to two units in the last place: 2^-22 of the update, itself a small part of the weight.
 __device__ __forceinline__ float new_weight(float w, float m, float v, const Step& s) {
@@ -504,8 +505,8 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     if (W16) {
         uint32_t h[PER_LANE / 2];
 #pragma unroll
-        for (int k = 0; k < PER_LANE; k += 2)             // all finite: the sum's upper halves
-            h[k / 2] = __byte_perm(__float_as_uint(w[k]) + ((r[k] << 6) >> 16), __float_as_uint(w[k + 1]) + ((r[k + 1] << 6) >> 16), 0x7632);
+        for (int k = 0; k < PER_LANE; k += 2)             // all finite: the sum's upper halves (bits 10..25 of the counter by a product: 3 us of 218)
+            h[k / 2] = __byte_perm(__float_as_uint(w[k]) + __umulhi(r[k] << 6, 0x10000u), __float_as_uint(w[k + 1]) + __umulhi(r[k + 1] << 6, 0x10000u), 0x7632);
         *reinterpret_cast<uint4*>(pw) = make_uint4(h[0], h[1], h[2], h[3]);
     } else {
         F32::store8(reinterpret_cast<float*>(pw), w);
@@ -524,10 +525,10 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
 }
 
 template <int BITS, class W, class G>
-__global__ void __launch_bounds__(32 * WARPS, STEP_CTAS) adamw_kernel(const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(const __grid_constant__ StepArgs a) {
     __shared__ uint8_t tops[2 * STRETCH];                 // the block exponents of the first moments, then of the second
     extern __shared__ __align__(16) char stages[];        // two of each warp, taken in turn
-    const int warp = threadIdx.x >> 5;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);     // so that addresses are formed once for the warp
     const int64_t begin = (int64_t)blockIdx.x * a.stretch;
     const int end = (int)min(begin + a.stretch, a.n_blocks), count = end - (int)begin;
     Step s;
@@ -1145,7 +1146,7 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     // 8-bit moments: whole rounds over all places, of at most 128 blocks (11.2M f32: 24 blocks in four and a bit rounds 39.4 us, 99
     // in one 36.9; 2^28: 8, 16, 32, 64, 128 blocks 1493, 1186, 1083, 1044, 1023 us).  Their exponents are bytes side by side, and
     // a line of them that thread blocks on both dies write has each of them wait for the other.
-    const int64_t places = (int64_t)h->num_sms * STEP_CTAS;
+    const int64_t places = (int64_t)h->num_sms * (h->state_bits == 8 ? STEP_CTAS<8> : STEP_CTAS<32>);
     if (h->state_bits == 8) {
         const int64_t rounds = (h->n_blocks + places * STRETCH - 1) / (places * STRETCH);
         const int64_t each = rounds ? (h->n_blocks + places * rounds - 1) / (places * rounds) : 0;
