@@ -18,7 +18,9 @@ namespace {
 constexpr int BLK = 256;                      // elements of a block
 constexpr int WARPS = 8;                      // warps of a thread block
 constexpr int PER_LANE = BLK / 32;
+constexpr int VALUES_PAIRS = 2;               // pairs of blocks that a warp of the values' kernel has in flight
 constexpr int INLINE_TENSORS = 128;           // pointers of so many tensors travel with the launch itself
+constexpr int INLINE_GRADS = 384;             // ... of the norm, which takes one for each
 constexpr int TABLE_FEW = 400, TABLE_MANY = 1300;   // ... and of so many with one launch of the kernel that fills the device table
 constexpr int MAX_TENSORS = 1 << 20;
 constexpr int NORM_PER_SM = 3;                // thread blocks of the norm on an SM (2^26 f32: 3 take 44 us, 4 with fewer registers 46)
@@ -104,11 +106,6 @@ __device__ __forceinline__ uint4 load16(const void* p) {
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
     return u;
 }
-__device__ __forceinline__ uint2 load_codes(const void* p) {
-    uint2 u;
-    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(u.x), "=r"(u.y) : "l"(p));
-    return u;
-}
 // The same accesses to shared memory that cp.async has filled.
 __device__ __forceinline__ uint4 stage16(uint32_t at) {
     uint4 u;
@@ -143,6 +140,7 @@ struct F32 {
         asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
     }
+    static __device__ __forceinline__ void store16(float* p, const float* x) { store8(p, x); store8(p + 8, x + 8); }
     static __device__ __forceinline__ void store8(float* p, const float* x) {
         asm volatile("st.global.v8.f32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
                      :: "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "l"(p) : "memory");
@@ -166,6 +164,11 @@ struct Bf16 {
 #pragma unroll
         for (int k = 0; k < 4; ++k) h[k] = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
         return *reinterpret_cast<const uint4*>(h);
+    }
+    static __device__ __forceinline__ void store16(type* p, const float* x) {
+        const uint4 u = pack(x), w = pack(x + 8);
+        asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                     :: "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w), "l"(p) : "memory");
     }
     static __device__ __forceinline__ void store8(type* p, const float* x) { *reinterpret_cast<uint4*>(p) = pack(x); }
 };
@@ -201,7 +204,6 @@ struct F16 {
 // exponent bits, no sign (32 octaves: sixteen of its square root).  Scaled so that its grid lies at the lower end of the
 // 32-bit floats, a code IS the upper bits of the float, subnormal codes included, and both directions are a product and a shift.
 template <int TOP> struct Scale {
-    static constexpr int FIELD = TOP;
     static constexpr int LEAST = TOP + 3;                // smallest stored exponent: the grid stays within normal floats
     // 2^(top - TOP), as two factors since their product can leave the range
     static __device__ __forceinline__ float up1(int top) { return pow2i(top - 127); }
@@ -716,7 +718,7 @@ struct NormArgs {
     float* tensor_norms;
     co3_grad_info* info;
     Scalars* sc;
-    Pointers inline_ptr[INLINE_TENSORS];
+    const void* inline_grad[INLINE_GRADS];
 };
 
 template <class G> constexpr int NORM_UNROLL = sizeof(typename G::type) == 2 ? 6 : 3;    // blocks whose loads a warp has in flight
@@ -859,7 +861,7 @@ __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __g
                 if (to - from >= 8 * WARPS) turns = WARPS;
                 else { at = from + (to - from) * warp / WARPS; end = from + (to - from) * (warp + 1) / WARPS; }
             }
-            const typename G::type* g = static_cast<const typename G::type*>((a.table ? a.table[t] : a.inline_ptr[t]).grad);
+            const typename G::type* g = static_cast<const typename G::type*>(a.table ? a.table[t].grad : a.inline_grad[t]);
             double s = (uintptr_t)g & G::ALIGN ? squares<G, false>(g, at, end, turns, n, bad) : squares<G, true>(g, at, end, turns, n, bad);
             if (to * BLK > n && (!share || warp == WARPS - 1)) s += squares_end<G>(g, n, bad);
             s = warp_sum(s);
@@ -942,25 +944,47 @@ __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __g
 }
 
 // ---- values of the 8-bit moments, and the tables ---------------------------------------------------------------------------
+// A warp takes pairs of blocks, sixteen codes of a block to a lane, and stores 32 bytes at a time (124M: 111 us, 6.7 TB/s; one block
+// and 16 bytes at a time 125 us).  Thread blocks begin at the end of the arrays, where the step ended: its last codes are still in the
+// cache (step and values of 124M: 323 us, 332 the other way round).
+template <class T, bool SECOND>
+__device__ __forceinline__ void values16(uint4 c, int top, typename T::type* out) {
+    // the second factor is 1 but for the largest exponents, which one factor cannot hold
+    const int most = SECOND ? ScaleV::PLAIN : ScaleM::PLAIN, more = top > most ? top - most : 0;
+    const float up = SECOND ? ScaleV::up(top - more) : ScaleM::up(top - more);
+    float x[16];
+    if (SECOND) { ScaleV::decode8<false>(make_uint2(c.x, c.y), up, x); ScaleV::decode8<false>(make_uint2(c.z, c.w), up, x + 8); }
+    else { ScaleM::decode8<true>(make_uint2(c.x, c.y), up, x); ScaleM::decode8<true>(make_uint2(c.z, c.w), up, x + 8); }
+    if (more) for (int k = 0; k < 16; ++k) x[k] *= pow2i(more);
+    T::store16(out, x);
+}
+
 template <class T>
 __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp,
                                                             int64_t n_blocks, typename T::type* m_out, typename T::type* v_out) {
     const int lane = threadIdx.x & 31;
+    const int64_t cta = (int64_t)(gridDim.x - 1 - blockIdx.x);
+    const int64_t b0 = 2 * VALUES_PAIRS * (cta * WARPS + (threadIdx.x >> 5)) + (lane >> 4);
     let_next_start();
     wait_for_previous();
-    for (int64_t b = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5); b < n_blocks; b += (int64_t)gridDim.x * WARPS) {
-        const int m_top = m_exp[b], v_top = v_exp[b];
-        const int64_t at = b * BLK + PER_LANE * lane;
-        float x[PER_LANE];
+    uint4 cm[VALUES_PAIRS], cv[VALUES_PAIRS];
+    int m_top[VALUES_PAIRS], v_top[VALUES_PAIRS];
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint2 c = load_codes((which ? v : m) + at);
-            // the second factor is 1 but for the largest exponents, which one factor cannot hold
-            const int top = which ? v_top : m_top, most = which ? ScaleV::PLAIN : ScaleM::PLAIN, more = top > most ? top - most : 0;
-            if (which) ScaleV::decode8<false>(c, pow2i(top - more - ScaleV::FIELD), x);
-            else ScaleM::decode8<true>(c, pow2i(top - more - ScaleM::FIELD), x);
-            if (more) for (int k = 0; k < PER_LANE; ++k) x[k] *= pow2i(more);
-            T::store8((which ? v_out : m_out) + at, x);
+    for (int u = 0; u < VALUES_PAIRS; ++u) {
+        const int64_t b = b0 + 2 * u;
+        if (b < n_blocks) {
+            cm[u] = load16(m + b * BLK + 16 * (lane & 15));
+            cv[u] = load16(v + b * BLK + 16 * (lane & 15));
+            m_top[u] = m_exp[b];
+            v_top[u] = v_exp[b];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < VALUES_PAIRS; ++u) {
+        const int64_t b = b0 + 2 * u;
+        if (b < n_blocks) {
+            values16<T, false>(cm[u], m_top[u], m_out + b * BLK + 16 * (lane & 15));
+            values16<T, true>(cv[u], v_top[u], v_out + b * BLK + 16 * (lane & 15));
         }
     }
 }
@@ -1032,19 +1056,20 @@ bool on_device(const co3_adamw* h) {
     return dev == h->device;
 }
 
-// The pointers of the call, in the launch's own arguments or in the device table.  weights == null: gradients only.
-int place_pointers(co3_adamw* h, const void* const* grads, void* const* weights, void* const* copies, Pointers* in_args, cudaStream_t st) {
+// Whether all pointers are there and aligned as their types.  weights == null: gradients only.
+bool pointers_fine(const co3_adamw* h, const void* const* grads, void* const* weights, void* const* copies) {
     for (int t = 0; t < h->n_tensors; ++t) {
         if (h->sizes[t] == 0) continue;
-        if (!grads[t] || ((uintptr_t)grads[t] & (uintptr_t)(width_of(h->grad_type) - 1))) return CO3_EINVAL;
-        if (weights && (!weights[t] || ((uintptr_t)weights[t] & (uintptr_t)(width_of(h->weight_type) - 1)))) return CO3_EINVAL;
-        if (copies && (!copies[t] || ((uintptr_t)copies[t] & 1))) return CO3_EINVAL;
+        if (!grads[t] || ((uintptr_t)grads[t] & (uintptr_t)(width_of(h->grad_type) - 1))) return false;
+        if (weights && (!weights[t] || ((uintptr_t)weights[t] & (uintptr_t)(width_of(h->weight_type) - 1)))) return false;
+        if (copies && (!copies[t] || ((uintptr_t)copies[t] & 1))) return false;
     }
+    return true;
+}
+
+// The pointers of the call to the device table.
+int fill_table(co3_adamw* h, const void* const* grads, void* const* weights, void* const* copies, cudaStream_t st) {
     auto one = [&](int t) { return Pointers{grads[t], weights ? weights[t] : nullptr, copies ? copies[t] : nullptr}; };
-    if (h->n_tensors <= INLINE_TENSORS) {
-        for (int t = 0; t < h->n_tensors; ++t) in_args[t] = one(t);
-        return CO3_OK;
-    }
     TableArgs<TABLE_MANY>* args = (TableArgs<TABLE_MANY>*)malloc(sizeof(TableArgs<TABLE_MANY>));
     if (!args) return CO3_ENOMEM;
     int rc = CO3_OK;
@@ -1184,10 +1209,17 @@ extern "C" int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_
     if (!(fabsf(grad_scale) < INFINITY) || !(max_norm < INFINITY)) return CO3_EINVAL;
     if (!on_device(h)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (!pointers_fine(h, grads, nullptr, nullptr)) return CO3_EINVAL;
     NormArgs a;
-    int rc = place_pointers(h, grads, nullptr, nullptr, a.inline_ptr, st);
-    if (rc != CO3_OK) return rc;
-    a.tensors = h->tensors; a.owner = h->owner; a.table = h->table; a.n_blocks = h->n_blocks; a.per_cta = h->per_cta;
+    a.table = nullptr;
+    if (h->n_tensors <= INLINE_GRADS) {
+        for (int t = 0; t < h->n_tensors; ++t) a.inline_grad[t] = grads[t];
+    } else {
+        a.table = h->table;
+        const int rc = fill_table(h, grads, nullptr, nullptr, st);
+        if (rc != CO3_OK) return rc;
+    }
+    a.tensors = h->tensors; a.owner = h->owner; a.n_blocks = h->n_blocks; a.per_cta = h->per_cta;
     a.n_tensors = h->n_tensors; a.n_slots = h->n_slots; a.grad_scale = grad_scale; a.max_norm = max_norm;
     a.slots = h->slots; a.tensor_norms = tensor_norms; a.info = info; a.sc = h->sc;
     const int threads = 32 * WARPS;
@@ -1207,10 +1239,16 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     }
     if (!on_device(h)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (!pointers_fine(h, grads, weights, copies)) return CO3_EINVAL;
     StepArgs a;
-    int rc = place_pointers(h, grads, weights, copies, a.inline_ptr, st);
-    if (rc != CO3_OK) return rc;
-    a.tensors = h->tensors; a.owner = h->owner; a.table = h->table; a.n_blocks = h->n_blocks;
+    a.table = h->table;
+    if (!h->table) {
+        for (int t = 0; t < h->n_tensors; ++t) a.inline_ptr[t] = Pointers{grads[t], weights[t], copies ? copies[t] : nullptr};
+    } else {
+        const int rc = fill_table(h, grads, weights, copies, st);
+        if (rc != CO3_OK) return rc;
+    }
+    a.tensors = h->tensors; a.owner = h->owner; a.n_blocks = h->n_blocks;
     a.m = state->m; a.v = state->v; a.m_exp = (uint8_t*)state->m_exp; a.v_exp = (uint8_t*)state->v_exp;
     a.info = info; a.d_lr = d_lr; a.sc = h->sc; a.beta1 = h->beta1; a.beta2 = h->beta2;
     a.b1 = (float)h->beta1; a.a1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.a2 = (float)(1.0 - h->beta2);
@@ -1254,8 +1292,7 @@ extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void
     if (!state->m || !state->v || !state->m_exp || !state->v_exp || (((uintptr_t)state->m | (uintptr_t)state->v) & 31)) return CO3_EINVAL;
     if (!m_values || !v_values || (((uintptr_t)m_values | (uintptr_t)v_values) & 31)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int64_t need = (h->n_blocks + WARPS - 1) / WARPS, most = (int64_t)h->num_sms * 8;
-    const int grid = (int)(need < most ? need : most);
+    const int grid = (int)((h->n_blocks + 2 * VALUES_PAIRS * WARPS - 1) / (2 * VALUES_PAIRS * WARPS));
     const uint8_t *m = (const uint8_t*)state->m, *v = (const uint8_t*)state->v;
     if (value_type == CO3_F32)
         return launch(h, values_kernel<F32>, grid, 32 * WARPS, 0, st, m, v, (const uint8_t*)state->m_exp, (const uint8_t*)state->v_exp, h->n_blocks,
