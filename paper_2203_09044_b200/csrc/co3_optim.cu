@@ -84,7 +84,8 @@ __device__ __forceinline__ float pow2i(int e) {          // 2^e, -149 <= e <= 12
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Two 32-bit operations in one instruction, each rounded by itself as the single ones are.
+// Two 32-bit operations in one instruction.  (A product whose result goes into a sum may come out as one fused operation, with one
+// rounding; where that matters it is written as a fused one itself.)
 struct Pair {
     unsigned long long v;
     __device__ __forceinline__ Pair() {}
@@ -100,7 +101,6 @@ __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
     return r;
 }
 
-// A type of weights, gradients or copies: one element, and a lane's eight neighbouring ones in one access.
 __device__ __forceinline__ uint4 load16(const void* p) {
     uint4 u;
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
@@ -121,6 +121,8 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
 }
+// A type of weights, gradients or copies: one element, and a lane's eight neighbouring ones, in one access if the array begins on a
+// multiple of ALIGN + 1 bytes.
 struct F32 {
     typedef float type;
     static __device__ __forceinline__ void unpack(const uint4* u, float* x) {
@@ -394,7 +396,7 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
             const int i = lane + 32 * k;
             const uint32_t r = counter_bits(key, (uint32_t)i);
             uint32_t c = ScaleM::encode(fabsf(m[k]), m_top, r & 0xFFFFFu);
-            if (m[k] < 0.0f) c |= 128u;
+            c |= __float_as_uint(m[k]) >> 24 & 128u;
             if (i < n) static_cast<uint8_t*>(a.m)[place + i] = (uint8_t)c;
             c = ScaleV::encode(v[k], v_top, r >> 12);
             if (c == 0 && v[k] > 0.0f) c = 1;
@@ -945,8 +947,7 @@ __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __g
 
 // ---- values of the 8-bit moments, and the tables ---------------------------------------------------------------------------
 // A warp takes pairs of blocks, sixteen codes of a block to a lane, and stores 32 bytes at a time (124M: 111 us, 6.7 TB/s; one block
-// and 16 bytes at a time 125 us).  Thread blocks begin at the end of the arrays, where the step ended: its last codes are still in the
-// cache (step and values of 124M: 323 us, 332 the other way round).
+// and 16 bytes at a time 125 us).
 template <class T, bool SECOND>
 __device__ __forceinline__ void values16(uint4 c, int top, typename T::type* out) {
     // the second factor is 1 but for the largest exponents, which one factor cannot hold
@@ -963,8 +964,7 @@ template <class T>
 __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp,
                                                             int64_t n_blocks, typename T::type* m_out, typename T::type* v_out) {
     const int lane = threadIdx.x & 31;
-    const int64_t cta = (int64_t)(gridDim.x - 1 - blockIdx.x);
-    const int64_t b0 = 2 * VALUES_PAIRS * (cta * WARPS + (threadIdx.x >> 5)) + (lane >> 4);
+    const int64_t b0 = 2 * VALUES_PAIRS * ((int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5)) + (lane >> 4);
     let_next_start();
     wait_for_previous();
     uint4 cm[VALUES_PAIRS], cv[VALUES_PAIRS];

@@ -596,3 +596,154 @@ def test_bound_gradients_of_another_optimizer_are_checked_again(binding):
         b.AdamW(p, grad_dtype=torch.bfloat16).grad_norm(bound)
     b.AdamW([torch.ones(300, device="cuda")]).step(bound)          # fits: used as it is
     assert large.steps() == 0
+
+
+# ---- mixtures, neighbours in memory, calls in a row ---------------------------------------------------------------------------------
+def _mixture(n, top, seed):
+    rng = np.random.default_rng(seed)
+    return [int(x) for x in np.exp(rng.uniform(0.0, math.log(top), n)).astype(np.int64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,top,off", [(3000, 40_000, 0), (500, 300_000, 1), (40, 4_000_000, 0), (385, 2000, 0), (384, 2000, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_mixtures(binding, n, top, off, dtype):
+    """Tensors of very different sizes: pieces that all warps of a thread block share, that one takes, that several thread blocks have."""
+    sizes = _mixture(n, top, n + off)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    row = (torch.randn(sum(sizes) + off, generator=gen, device="cuda") * 0.01).to(DT[dtype])[off:]
+    grads = list(row.split(sizes))
+    opt = binding.GradNorm(sizes, DT[dtype])
+    norms = torch.empty(n, device="cuda")
+    info = opt.grad_norm(grads, max_norm=0.5, tensor_norms=norms)
+    want = torch.stack([g.double().pow(2).sum().sqrt() for g in grads])
+    assert ((norms.double() - want).abs() <= 2.0 ** -23 * want).all()
+    total = row.double().pow(2).sum().sqrt().item()
+    assert abs(info[1].item() - total) <= 2.0 ** -23 * total
+    for _ in range(3):
+        again = opt.grad_norm(grads, max_norm=0.5)
+        assert torch.equal(again.view(torch.int32), info.view(torch.int32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("off", [0, 1, 2])
+@pytest.mark.parametrize("weight,grad,copy", [("f32", "bf16", "bf16"), ("bf16", "bf16", None), ("f32", "f32", None)])
+def test_places_between_tensors_are_left_alone(binding, bits, off, weight, grad, copy):
+    sizes = [1, 700, 256, 5, 1024, 3000]
+    gaps = [3, 2, 8, 1, 16, 5]
+
+    def spread(dtype, fill):
+        buf = torch.full((off + sum(sizes) + sum(gaps) + 64,), fill, device="cuda", dtype=dtype)
+        at, views = off, []
+        mask = torch.ones_like(buf, dtype=torch.bool)
+        for n, gap in zip(sizes, gaps):
+            views.append(buf[at:at + n])
+            mask[at:at + n] = False
+            at += n + gap
+        return buf, views, mask
+    w, ws, w_mask = spread(DT[weight], 0.375)
+    g, gs, _ = spread(DT[grad], float("nan"))
+    for x in gs:
+        x.copy_(torch.randn(x.numel(), device="cuda"))
+    c, cs, c_mask = spread(DT[copy], 0.625) if copy else (None, None, None)
+    opt = binding.AdamW(ws, grad_dtype=DT[grad], copies=cs, state_bits=bits, lr=0.1)
+    used = torch.zeros(opt.n_blocks * 256, dtype=torch.bool, device="cuda")
+    for i in range(len(sizes)):
+        a = opt.moments_of(i)[0]
+        start = (a.data_ptr() - opt.m.data_ptr()) // a.element_size()
+        used[start:start + sizes[i]] = True
+    sentinel = 77 if bits == 8 else 77.0
+    opt.m.view(-1)[~used] = sentinel
+    opt.v.view(-1)[~used] = sentinel
+    info = opt.grad_norm(gs)                                  # the NaN between the gradients are not counted
+    assert info[2:].view(torch.int64).item() == 0
+    opt.step(gs, info)
+    opt.step(gs)
+    assert (w[w_mask] == 0.375).all() and all((x != 0.375).all() for x in ws)
+    assert c is None or (c[c_mask] == 0.625).all()
+    assert (opt.m.view(-1)[~used] == sentinel).all() and (opt.v.view(-1)[~used] == sentinel).all()
+    assert opt.status() == (0, 0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("n,top", [(2, 5000), (300, 3000), (30, 200_000)])
+def test_calls_in_a_row_wait_for_one_another(binding, bits, n, top):
+    """Each kernel may start before the one ahead of it has ended.  Gradients that change between the calls, norm, step and values one
+    after the other without a pause give the bits of the same calls with a wait after each."""
+    sizes = _mixture(n, top, n)
+
+    def loop(wait):
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        row = torch.randn(sum(sizes), generator=gen, device="cuda")
+        base = torch.randn(sum(sizes), generator=gen, device="cuda") * 1e-3
+        grad = torch.empty_like(base)
+        opt = binding.AdamW(list(row.split(sizes)), state_bits=bits, seed=4)
+        bound, info = opt.bind_grads(list(grad.split(sizes))), torch.zeros(4, device="cuda")
+        norms = torch.empty(n, device="cuda")
+        kept = torch.zeros((), dtype=torch.float64, device="cuda")
+        sync = torch.cuda.synchronize if wait else (lambda: None)
+        for t in range(60):
+            torch.mul(base, 1.0 + 0.1 * t, out=grad)
+            sync()
+            opt.grad_norm(bound, info, max_norm=0.5, tensor_norms=norms)
+            sync()
+            opt.step(bound, info)
+            sync()
+            if bits == 8:
+                m, v = opt.state_values()
+                sync()
+                kept += m.double().abs().sum() + norms.double().sum()
+            opt.step(bound, info)
+            sync()
+            opt.grad_norm(bound, info)
+            sync()
+            kept += info[1].double()
+        return row, opt.m.clone(), opt.v.clone(), kept
+    a, b = loop(True), loop(False)
+    assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3])) and abs(a[3].item() / b[3].item() - 1) < 1e-12
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_weights_that_are_not_finite_change_no_others(binding, bits, off):
+    """An infinite weight times its decay, taken from itself, is no number by the formula; stochastic rounding must not make one of it."""
+    for dtype in (torch.float32, torch.bfloat16):
+        w = torch.randn(2000 + off, device="cuda").to(dtype)[off:]
+        bad = [0, 255, 256, 700, 1999]
+        w[bad] = torch.tensor([float("nan"), float("inf"), -float("inf"), float("nan"), float("inf")], device="cuda", dtype=dtype)
+        opt = binding.AdamW([w], grad_dtype=torch.float32, state_bits=bits, weight_decay=0.1, lr=1e-3)
+        for _ in range(3):
+            opt.step([torch.randn(2000, device="cuda")])
+        fine = torch.isfinite(w)
+        assert not fine[bad].any() and int(fine.sum()) == 1995 and opt.status() == (0, 0, 0)
+
+
+@pytest.mark.gpu
+def test_against_torch_s_optimizer_in_64_bits(binding):
+    """torch.optim.AdamW on 64-bit copies of the same weights and gradients, 20 steps with two decays."""
+    gen = torch.Generator().manual_seed(11)
+    sizes = [3000, 17, 512]
+    p = make(sizes, torch.float32, gen)
+    q = [x.double().clone().requires_grad_() for x in p]
+    theirs = torch.optim.AdamW([{"params": q[:2], "weight_decay": 0.1}, {"params": q[2:], "weight_decay": 0.0}], lr=1e-2, betas=(0.9, 0.99))
+    ours = binding.AdamW(p, lr=1e-2, betas=(0.9, 0.99), weight_decay=[0.1, 0.1, 0.0])
+    for t in range(1, 21):
+        g = make(sizes, torch.float32, gen)
+        for x, y in zip(q, g):
+            x.grad = y.double()
+        theirs.step()
+        ours.step(g)
+        for x, y in zip(p, q):
+            # one step's bound (updates below 10 lr) for each step so far
+            assert (x.double() - y.detach()).abs().max() <= t * (2.0 ** -23 * y.detach().abs().max() + 2.0 ** -19 * 0.1)
+
+
+@pytest.mark.gpu
+def test_training_loop_learns_with_either_kind_of_moments(binding):
+    from paper_2203_09044_b200 import train_step
+    l32 = train_step.run(iterations=80, n_users=3, d=60_000, state_bits=32)
+    l8 = train_step.run(iterations=80, n_users=3, d=60_000, state_bits=8)
+    assert l32[0] == l8[0] and l32[-1] < 0.2 * l32[0] and l8[-1] < 0.2 * l8[0]
