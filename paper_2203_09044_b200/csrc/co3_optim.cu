@@ -18,7 +18,6 @@ namespace {
 constexpr int BLK = 256;                      // elements of a block
 constexpr int WARPS = 8;                      // warps of a thread block
 constexpr int PER_LANE = BLK / 32;
-constexpr int VALUES_PAIRS = 2;               // pairs of blocks that a warp of the values' kernel has in flight
 constexpr int INLINE_TENSORS = 128;           // pointers of so many tensors travel with the launch itself
 constexpr int INLINE_GRADS = 384;             // ... of the norm, which takes one for each
 constexpr int TABLE_FEW = 400, TABLE_MANY = 1300;   // ... and of so many with one launch of the kernel that fills the device table
@@ -82,6 +81,12 @@ __device__ __forceinline__ float pow2i(int e) {          // 2^e, -149 <= e <= 12
 // A kernel of this file may start while the one before it on the stream still runs.  It then reads what was fixed when the handle
 // was made, and waits for the end of the other, and for its writes, before anything else.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// One more on a ticket, after all that the thread block has written or read before its last barrier, and before what follows.
+__device__ __forceinline__ uint32_t take_ticket(uint32_t* ticket) {
+    uint32_t old;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(ticket) : "memory");
+    return old;
+}
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Two 32-bit operations in one instruction.  (A product whose result goes into a sum may come out as one fused operation, with one
@@ -684,8 +689,7 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(cons
         atomicAdd(&a.sc->skipped_elements, (unsigned long long)kept);
     }
     if (threadIdx.x == 0) {                               // the last block to come here prepares the next step
-        __threadfence();
-        if (atomicAdd(&a.sc->ticket, 1u) == gridDim.x - 1) {
+        if (take_ticket(&a.sc->ticket) == gridDim.x - 1) {
             a.sc->ticket = 0;
             if (skip) {
                 atomicOr(&a.sc->flags, CO3_FLAG_NONFINITE);
@@ -886,11 +890,7 @@ __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __g
         a.slots[blockIdx.x + shared_tensor[threadIdx.x]] = s;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();                                  // of the whole block's writes, which the barrier put before it
-        last = atomicAdd(&a.sc->norm_ticket, 1u) == gridDim.x - 1;
-        __threadfence();
-    }
+    if (threadIdx.x == 0) last = take_ticket(&a.sc->norm_ticket) == gridDim.x - 1;
     __syncthreads();
     if (!last) return;
 
@@ -946,7 +946,7 @@ __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __g
 }
 
 // ---- values of the 8-bit moments, and the tables ---------------------------------------------------------------------------
-// A warp takes pairs of blocks, sixteen codes of a block to a lane, and stores 32 bytes at a time (124M: 111 us, 6.7 TB/s; one block
+// A warp takes two blocks, sixteen codes of a block to a lane, and stores 32 bytes at a time (124M: 111 us, 6.7 TB/s; one block
 // and 16 bytes at a time 125 us).
 template <class T, bool SECOND>
 __device__ __forceinline__ void values16(uint4 c, int top, typename T::type* out) {
@@ -964,29 +964,14 @@ template <class T>
 __global__ void __launch_bounds__(32 * WARPS) values_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* m_exp, const uint8_t* v_exp,
                                                             int64_t n_blocks, typename T::type* m_out, typename T::type* v_out) {
     const int lane = threadIdx.x & 31;
-    const int64_t b0 = 2 * VALUES_PAIRS * ((int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5)) + (lane >> 4);
+    const int64_t b = 2 * ((int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5)) + (lane >> 4), at = b * BLK + 16 * (lane & 15);
     let_next_start();
     wait_for_previous();
-    uint4 cm[VALUES_PAIRS], cv[VALUES_PAIRS];
-    int m_top[VALUES_PAIRS], v_top[VALUES_PAIRS];
-#pragma unroll
-    for (int u = 0; u < VALUES_PAIRS; ++u) {
-        const int64_t b = b0 + 2 * u;
-        if (b < n_blocks) {
-            cm[u] = load16(m + b * BLK + 16 * (lane & 15));
-            cv[u] = load16(v + b * BLK + 16 * (lane & 15));
-            m_top[u] = m_exp[b];
-            v_top[u] = v_exp[b];
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < VALUES_PAIRS; ++u) {
-        const int64_t b = b0 + 2 * u;
-        if (b < n_blocks) {
-            values16<T, false>(cm[u], m_top[u], m_out + b * BLK + 16 * (lane & 15));
-            values16<T, true>(cv[u], v_top[u], v_out + b * BLK + 16 * (lane & 15));
-        }
-    }
+    if (b >= n_blocks) return;
+    const uint4 cm = load16(m + at), cv = load16(v + at);
+    const int m_top = m_exp[b], v_top = v_exp[b];
+    values16<T, false>(cm, m_top, m_out + at);
+    values16<T, true>(cv, v_top, v_out + at);
 }
 
 __global__ void owner_kernel(const Tensor* tensors, int n_tensors, int32_t* owner, int64_t n_blocks) {
@@ -1292,7 +1277,7 @@ extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void
     if (!state->m || !state->v || !state->m_exp || !state->v_exp || (((uintptr_t)state->m | (uintptr_t)state->v) & 31)) return CO3_EINVAL;
     if (!m_values || !v_values || (((uintptr_t)m_values | (uintptr_t)v_values) & 31)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int grid = (int)((h->n_blocks + 2 * VALUES_PAIRS * WARPS - 1) / (2 * VALUES_PAIRS * WARPS));
+    const int grid = (int)((h->n_blocks + 2 * WARPS - 1) / (2 * WARPS));
     const uint8_t *m = (const uint8_t*)state->m, *v = (const uint8_t*)state->v;
     if (value_type == CO3_F32)
         return launch(h, values_kernel<F32>, grid, 32 * WARPS, 0, st, m, v, (const uint8_t*)state->m_exp, (const uint8_t*)state->v_exp, h->n_blocks,
