@@ -18,7 +18,7 @@ namespace {
 constexpr int BLK = 256;                      // elements of a block
 constexpr int WARPS = 8;                      // warps of a thread block
 constexpr int PER_LANE = BLK / 32;
-constexpr int INLINE_TENSORS = 128;           // pointers of so many tensors travel with the launch itself
+constexpr int INLINE_TENSORS = 64;            // pointers of so many tensors travel with the launch itself
 constexpr int INLINE_GRADS = 384;             // ... of the norm, which takes one for each
 constexpr int TABLE_FEW = 400, TABLE_MANY = 1300;   // ... and of so many with one launch of the kernel that fills the device table
 constexpr int MAX_TENSORS = 1 << 20;
