@@ -243,8 +243,27 @@ template <int TOP> struct Scale {
 #pragma unroll
         for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * scale).get(x[k], x[k + 1]);
     }
-    // r: the counters; the first moment takes bits 0..19, the second 12..31.  The sum is formed four places up, so that the code is
-    // the upper byte of its word.
+    // Eight codes as floats that lack their block's scale, which is multiplied into the constant that they meet: the first moments' as
+    // the e4m3 numbers that they are (but for the code that is no number there and never made here), the second's as upper bits.
+    static __device__ __forceinline__ void first8(uint2 c, float* x) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)((k < 4 ? c.x : c.y) >> (8 * (k & 3)))));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            x[k] = f.x; x[k + 1] = f.y;
+        }
+    }
+    static __device__ __forceinline__ float first_scale(int top) { return __uint_as_float((uint32_t)(top - 7) << 23); }   // e4m3 has field 14 at 2^7
+    static __device__ __forceinline__ void second8(uint2 c, float* x) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t word = k < 4 ? c.x : c.y;
+            const int left = 20 - 8 * (k & 3);
+            x[k] = __uint_as_float((left >= 0 ? word << (left & 31) : word >> 4) & 0x0FF00000u);
+        }
+    }
+    // r: the counters; the first moment takes bits 0..19, the second 12..31.
     template <bool SIGNED> static __device__ __forceinline__ uint2 encode8(const float* x, float down, const uint32_t* r) {
         const Pair scale(down, down);
         float y[8];
@@ -252,14 +271,15 @@ template <int TOP> struct Scale {
 #pragma unroll
         for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * scale).get(y[k], y[k + 1]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)                                            // (of r >> 8, the last four bits lie below what counts)
-            z[k] = __float_as_uint(y[k]) * 16u + (SIGNED ? (r[k] << 4) & 0x00FFFFF0u : r[k] >> 8);
+        for (int k = 0; k < 8; ++k) z[k] = __float_as_uint(y[k]) + (SIGNED ? r[k] & 0xFFFFFu : r[k] >> 12);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            pack[h] = upper_bytes(z + 4 * h);
+        for (int h = 0; h < 2; ++h) {                                          // upper halves: the code in bits 4 .. 11, the sign on top
+            const uint32_t a = __byte_perm(z[4 * h], z[4 * h + 1], 0x7632), b = __byte_perm(z[4 * h + 2], z[4 * h + 3], 0x7632);
+            pack[h] = __byte_perm(a >> 4, b >> 4, 0x6420);
             if (SIGNED) {
-                const uint32_t s[4] = {__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), __float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3])};
-                pack[h] |= upper_bytes(s) & 0x80808080u;
+                uint32_t signs;                                                // of four, each through a whole byte
+                asm("prmt.b32 %0, %1, %2, 0xFDB9;" : "=r"(signs) : "r"(a), "r"(b));
+                pack[h] = (pack[h] & 0x7F7F7F7Fu) | (signs & 0x80808080u);
             }
         }
         if (!SIGNED && ((((pack[0] - 0x01010101u) & ~pack[0]) | ((pack[1] - 0x01010101u) & ~pack[1])) & 0x80808080u)) {
@@ -268,9 +288,6 @@ template <int TOP> struct Scale {
                 if (!(pack[k / 4] >> (8 * (k & 3)) & 0xFFu) && x[k] > 0.0f) pack[k / 4] |= 1u << (8 * (k & 3));
         }
         return make_uint2(pack[0], pack[1]);
-    }
-    static __device__ __forceinline__ uint32_t upper_bytes(const uint32_t* z) {
-        return __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
     }
 };
 using ScaleM = Scale<14>;
@@ -305,7 +322,7 @@ struct StepArgs {
     unsigned long long minus_zero;            // twice -0: a product plus this is the product, rounded
     uint32_t seed;
     int copy_type, stretch;
-    bool fast;                                // block_whole's root is precise enough, see co3_adamw_step
+    bool fast;                                // block_whole is as precise as block_any, see co3_adamw_step
     Pointers inline_ptr[INLINE_TENSORS];
 };
 
@@ -501,6 +518,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     typename W::type* pw = reinterpret_cast<typename W::type*>(p.weight) + at;
     float g[PER_LANE], w[PER_LANE], m[PER_LANE], v[PER_LANE];
     bool other = false;                                   // some value needs the general way
+    float b1m = 0.0f, b2v = 0.0f;                         // beta1 and beta2 times the scales of 8-bit moments
     if (BITS == 32) {
         G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
         W::load8(pw, w);
@@ -511,12 +529,15 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
         stage.take(p, g, w, cm, cv);
         const int m_top = tops[0], v_top = tops[STRETCH];
         other = m_top > ScaleM::PLAIN || v_top > ScaleV::PLAIN;
-        ScaleM::decode8<true>(cm, ScaleM::up(m_top), m);
-        ScaleV::decode8<false>(cv, ScaleV::up(v_top), v);
+        ScaleM::first8(cm, m);
+        ScaleV::second8(cv, v);
+        b1m = a.b1 * ScaleM::first_scale(m_top);          // exact: see `fast` in co3_adamw_step
+        b2v = a.b2 * ScaleV::up(v_top);
     }
     // The four products are formed as fused ones that add -0, for ptxas makes a fused one of a packed product and the sum
     // that takes it, and the moments are rounded after each.
-    const Pair b1(a.b1_pair), a1(a.a1_pair), b2(a.b2_pair), a2(a.a2_pair), zero(a.minus_zero);
+    const Pair b1 = BITS == 8 ? Pair(b1m, b1m) : Pair(a.b1_pair), b2 = BITS == 8 ? Pair(b2v, b2v) : Pair(a.b2_pair);
+    const Pair a1(a.a1_pair), a2(a.a2_pair), zero(a.minus_zero);
     const Pair factor(s.factor, s.factor), rate(s.rate, s.rate), decay(s.decay, s.decay), eps(s.eps, s.eps), minus(-1.0f, -1.0f);
     uint32_t v_max = 0;
     float m_max = 0.0f;
@@ -530,7 +551,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
         v1.get(v[k], v[k + 1]);
         // as whole numbers: NaN of either sign is above the limit too
         v_max = __vimax3_u32(v_max, __float_as_uint(v[k]), __float_as_uint(v[k + 1]));
-        if (BITS == 8) m_max = fmaxf(fmaxf(m_max, fabsf(m[k])), fabsf(m[k + 1]));
+        if (BITS == 8) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m_max) : "f"(m_max), "f"(m[k]), "f"(m[k + 1]));
         const Pair d = Pair(root_fast(v[k]), root_fast(v[k + 1])) + eps;
         float d0, d1;
         d.get(d0, d1);
@@ -1242,7 +1263,8 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     a.eps = (float)h->eps; a.lr = (float)lr; a.seed = h->seed; a.copy_type = h->copy_type;
     // block_whole takes roots of numbers below 2^-126 as 0.  Beside eps that is less than 2^-24 of the denominator if eps is above
     // 2^24 * 2^-63 / sqrt(1 - beta2) (6e-11 for beta2 = 0.999); a smaller eps takes the general way.
-    a.fast = h->eps * sqrt(1.0 - h->beta2) >= 0x1p-39;
+    // The scale of 8-bit moments (2^-117 at least) times beta1 has to stay a normal number.
+    a.fast = h->eps * sqrt(1.0 - h->beta2) >= 0x1p-39 && (h->state_bits == 32 || h->beta1 == 0.0 || h->beta1 >= 0x1p-9);
     // Blocks of one thread block.  32-bit moments: one warp takes as many as leave every place for a thread block four of them one
     // after the other, so that the SMs end together, and at most 4 (2^28 f32: 1, 2, 4, 8, 16 take 1214, 1115, 1097, 1114, 1125 us).
     // 8-bit moments: whole rounds over all places, of at most 128 blocks (11.2M f32: 24 blocks in four and a bit rounds 39.4 us, 99

@@ -284,7 +284,7 @@ def test_step_over_types_and_alignments(binding, weight, grad, copy, bits, off):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
-@pytest.mark.parametrize("betas", [(0.0, 0.0), (0.9, 0.95), (0.0, 0.999), (0.5, 0.0)])
+@pytest.mark.parametrize("betas", [(0.0, 0.0), (0.9, 0.95), (0.0, 0.999), (0.5, 0.0), (1e-3, 0.9), (2.0 ** -9, 1e-6)])
 @pytest.mark.parametrize("eps", [0.0, 1e-8, 1.0])
 def test_step_over_constants(binding, bits, betas, eps):
     run_steps(binding, [1000, 5], bits, betas=betas, eps=eps)
@@ -748,3 +748,29 @@ def test_training_loop_learns_with_either_kind_of_moments(binding):
     l32 = train_step.run(iterations=80, n_users=3, d=60_000, state_bits=32)
     l8 = train_step.run(iterations=80, n_users=3, d=60_000, state_bits=8)
     assert l32[0] == l8[0] and l32[-1] < 0.2 * l32[0] and l8[-1] < 0.2 * l8[0]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off", [0, 1])
+def test_every_code_is_read_by_the_formula(binding, off):
+    """Moments of 8 bits that no step of this library has made: all 256 codes in each block, with exponents from the least to the
+    largest, values and a step on from them."""
+    n, seed = 256 * 12, 5
+    tops_m = np.array([17, 18, 100, 120, 127, 139, 140, 141, 150, 17, 30, 113], np.uint8)
+    tops_v = np.array([33, 34, 90, 120, 127, 155, 156, 157, 170, 33, 40, 100], np.uint8)
+    rng = np.random.default_rng(1)
+    code_m = np.stack([rng.permutation(256) for _ in range(12)]).astype(np.uint8)
+    code_v = np.stack([rng.permutation(256) for _ in range(12)]).astype(np.uint8)
+    state = dict(m=torch.from_numpy(code_m).cuda(), v=torch.from_numpy(code_v).cuda(), m_exp=torch.from_numpy(tops_m).cuda(), v_exp=torch.from_numpy(tops_v).cuda())
+    gen = torch.Generator().manual_seed(3)
+    p, g = make([n], torch.float32, gen, off), make([n], torch.float32, gen, off)
+    opt = binding.AdamW(p, state_bits=8, seed=seed, state=state, weight_decay=0.0, lr=0.0)
+    ref = Reference(as_f32(p), np.zeros(1), 8, 0.0, (0.9, 0.999), 1e-8, seed, False)
+    ref.mc, ref.mt, ref.vc, ref.vt = code_m.copy(), tops_m.copy(), code_v.copy(), tops_v.copy()
+    m, v = (x.double().cpu().numpy() for x in opt.state_values(*(torch.empty((12, 256), device="cuda") for _ in range(2))))
+    assert np.array_equal(m, decode_ref(code_m, tops_m, M_FIELD, True)) and np.array_equal(v, decode_ref(code_v, tops_v, V_FIELD, False))
+    opt.step(g)
+    ref.step(as_f32(g))
+    assert ref.kept == 0 and opt.status() == (0, 0, 0)
+    for got, want in ((opt.m_exp, ref.mt), (opt.v_exp, ref.vt), (opt.m, ref.mc), (opt.v, ref.vc)):
+        assert np.array_equal(got.cpu().numpy(), want)
