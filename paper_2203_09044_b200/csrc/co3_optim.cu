@@ -617,6 +617,12 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     return true;
 }
 
+// The step.  Every element is read and written once; the moments' products and sums are the formula's in its order, so that no other
+// order of blocks, and neither way through a block, changes a bit of them.
+// 32-bit moments: 28 bytes an element (f32) against 40 instructions, so memory binds: 2^28 f32 in 1091 us, 6.9 TB/s, and 124M with bf16
+// gradient and copy in 519 us, 6.7 TB/s, both above the copy rate of 6.55.  11.2M in 62 tensors: 52 us (5.9 TB/s; it begins and ends).
+// 8-bit moments: 16 bytes (f32) or 10 (bf16) against 49 instructions, which leave the issue slots 83% busy: 2^28 f32 weights with bf16
+// gradient and copy in 667 us, 6.4 TB/s; 124M bf16 in 199 us, 6.25 TB/s, and more under the power limit, which takes clocks away.
 template <int BITS, class W, class G, bool ANY>
 __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(const __grid_constant__ StepArgs a) {
     __shared__ uint8_t tops[2 * STRETCH];                 // the block exponents of the first moments, then of the second
@@ -854,6 +860,9 @@ __device__ __forceinline__ double squares_end(const typename G::type* g, int64_t
     return s0 + s1;
 }
 
+// Reads every gradient once.  2^28 bf16 in 87 us, 6.2 TB/s (in 290 tensors of very different sizes, each with its norm, 96 us);
+// 2^26 f32 in 44 us; 11.2M f32 in 13 us, of which the bytes explain 7: the rest is the chain of the last sums (barrier, ticket,
+// slots, barrier) after the last load, and the begin of the first.
 template <class G>
 __global__ void __launch_bounds__(32 * WARPS, NORM_PER_SM) norm_kernel(const __grid_constant__ NormArgs a) {
     __shared__ double sh[WARPS], stage[NORM_STAGE], shared_sum[NORM_SHARED][WARPS];
