@@ -441,6 +441,7 @@ typedef struct {          /* device, 16-byte aligned: written by co3_grad_norm (
     uint64_t nonfinite;
 } co3_grad_info;
 
+/* On the current device.  Allocates, and waits for the little work that fills the tables (not to be called during a capture). */
 int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg);
 void co3_adamw_destroy(co3_adamw* h);
 int co3_adamw_sizes(const co3_adamw* h, int64_t* n_blocks, int64_t* n_elements);
@@ -465,7 +466,8 @@ int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void* m_values,
                      void* cuda_stream);
 
 /* Synchronising calls: sticky flags with the counts of elements and steps left out (clear != 0 resets all three);
- * steps taken, to be stored beside the moments and set again when a run is resumed. */
+ * steps taken, to be stored beside the moments and set again when a run is resumed, which then goes on with the same
+ * bits (after more than 2^26 steps: the bias corrections to 64-bit precision). */
 int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped_elements, uint64_t* skipped_steps, int32_t clear);
 int co3_adamw_steps_export(co3_adamw* h, int64_t* steps);
 int co3_adamw_steps_import(co3_adamw* h, int64_t steps);

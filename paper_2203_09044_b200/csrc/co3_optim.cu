@@ -1345,8 +1345,14 @@ extern "C" int co3_adamw_steps_import(co3_adamw* h, int64_t steps) {
     Scalars s;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, h->sc, sizeof(s), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     s.steps = steps;
-    s.pow1 = pow(h->beta1, (double)steps);
-    s.pow2 = pow(h->beta2, (double)steps);
+    // the products that the steps themselves would have left, to the bit; after very many (0.1 s of them here) the powers
+    s.pow1 = s.pow2 = 1.0;
+    if (steps <= (int64_t)1 << 26) {
+        for (int64_t i = 0; i < steps && (s.pow1 != 0.0 || s.pow2 != 0.0); ++i) { s.pow1 *= h->beta1; s.pow2 *= h->beta2; }
+    } else {
+        s.pow1 = pow(h->beta1, (double)steps);
+        s.pow2 = pow(h->beta2, (double)steps);
+    }
     next_scalars(s, h->beta1, h->beta2, h->seed);
     if (cudaMemcpy(h->sc, &s, sizeof(s), cudaMemcpyHostToDevice) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     return CO3_OK;

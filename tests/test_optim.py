@@ -434,6 +434,17 @@ def test_resumed_run_gives_the_same_bits(binding):
     for g in data[3:]:
         oc.step(g)
     assert all(torch.equal(x, y) for x, y in zip(a, b)) and torch.equal(oa.m, oc.m) and torch.equal(oa.v_exp, oc.v_exp)
+    # far into a run: one optimizer that took the steps, one that is told so
+    w = [torch.ones(64, device="cuda") for _ in range(2)]
+    z, g = [torch.zeros(64, device="cuda")], [torch.full((64,), 0.5, device="cuda")]
+    od, oe = binding.AdamW([w[0]], weight_decay=0.0), binding.AdamW([w[1]], weight_decay=0.0)
+    bound = od.bind_grads(z)
+    for _ in range(3000):
+        od.step(bound)
+    oe.set_steps(3000)
+    od.step(g)
+    oe.step(g)
+    assert od.steps() == oe.steps() == 3001 and torch.equal(w[0], w[1]) and not torch.equal(w[0], torch.ones_like(w[0]))
     m, v = oc.moments_of(1)
     assert m.numel() == v.numel() == 30 and m.data_ptr() == oc.m.data_ptr() + 1024
 
