@@ -124,7 +124,7 @@ __device__ __forceinline__ uint2 stage8(uint32_t at) {
 }
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory");
 }
 // A type of weights, gradients or copies: one element, and a lane's eight neighbouring ones, in one access if the array begins on a
 // multiple of ALIGN + 1 bytes.
@@ -334,7 +334,8 @@ struct Step {                                 // what is the same for all elemen
 enum Begin { ON_16, ON_4, ON_2 };             // the bytes that an array's beginning is a multiple of
 struct Bases {                                // where a tensor's arrays would begin if it began with block 0
     uintptr_t weight, grad, copy;
-    Begin weight_begin, grad_begin, copy_begin;
+    Begin weight_begin, copy_begin;           // for stores; ON_16 for whole accesses
+    int weight_shift, grad_shift;             // for loads: bytes past a multiple of 16
 };
 
 // An element whose second moment is not below this (or is no number) is left as it was.  The bound keeps the exponents
@@ -434,49 +435,52 @@ __device__ __forceinline__ float inverse_fast(float x) { float y; asm("rcp.appro
 // With 8-bit moments a block is little to load and much to compute: its loads are started one block ahead, into shared memory, where
 // they take no registers.  A copy of the warp is 512 bytes in a row (with 32 bytes a lane in two copies of 16 each, sectors would
 // be fetched twice), so lanes read what others copied and the warp meets before and after.
-// Weights and gradients that do not begin on 16 bytes come word by word (67M bf16: 152 us, 305 the general way); if an odd 16-bit
-// element comes first, from the one before it on, and are shifted when they are read.
+// Weights and gradients that do not begin on 16 bytes come with what else lies in their first and last 16 (which the tensor's first
+// and last blocks, without neighbours in the tensor, leave to the general way), and are moved to their places when they are read.
 template <class W, class G, bool ANY> struct Stage {      // ANY: arrays may begin anywhere
     static constexpr int W_BYTES = sizeof(typename W::type) * BLK, G_BYTES = sizeof(typename G::type) * BLK;
     static constexpr int W_AT = G_BYTES + 16, M_AT = W_AT + W_BYTES + 16, BYTES = M_AT + 2 * BLK;
-    uint32_t base;                            // of the warp: gradient, weights (each with room for one word more), codes of the two moments
-    template <int N> static __device__ __forceinline__ void bring(uint32_t to, const char* from, Begin begin) {
+    uint32_t base;                            // of the warp: gradient, weights (each with room for 16 bytes more), codes of the two moments
+    template <int N> static __device__ __forceinline__ void bring(uint32_t to, const char* from, int shift) {
         const int lane = threadIdx.x & 31;
-        if (!ANY || begin == ON_16) {
+        if (ANY) from -= shift;
 #pragma unroll
-            for (int k = 0; k < N; k += 512) copy_async<16>(to + 16 * lane + k, from + 16 * lane + k);
-        } else {
-            if (begin == ON_2) from -= 2;
-#pragma unroll
-            for (int k = 0; k < N; k += 128) copy_async<4>(to + 4 * lane + k, from + 4 * lane + k);
-            if (begin == ON_2 && lane == 0) copy_async<4>(to + N, from + N);
-        }
+        for (int k = 0; k < N; k += 512) copy_async<16>(to + 16 * lane + k, from + 16 * lane + k);
+        if (ANY && shift && lane == 0) copy_async<16>(to + N, from + N);
     }
     __device__ __forceinline__ void start(const StepArgs& a, const Bases& p, int b) const {
         const int lane = threadIdx.x & 31;
         const int64_t at = (int64_t)b * BLK;
-        bring<G_BYTES>(base, reinterpret_cast<const char*>(p.grad) + at * (int)sizeof(typename G::type), p.grad_begin);
-        bring<W_BYTES>(base + W_AT, reinterpret_cast<const char*>(p.weight) + at * (int)sizeof(typename W::type), p.weight_begin);
+        bring<G_BYTES>(base, reinterpret_cast<const char*>(p.grad) + at * (int)sizeof(typename G::type), p.grad_shift);
+        bring<W_BYTES>(base + W_AT, reinterpret_cast<const char*>(p.weight) + at * (int)sizeof(typename W::type), p.weight_shift);
         copy_async<8>(base + M_AT + 8 * lane, static_cast<const uint8_t*>(a.m) + at + 8 * lane);
         copy_async<8>(base + M_AT + BLK + 8 * lane, static_cast<const uint8_t*>(a.v) + at + 8 * lane);
     }
-    template <class T> static __device__ __forceinline__ void eight(uint32_t from, Begin begin, float* x) {
-        constexpr int n = 8 * sizeof(typename T::type);
-        from += n * (threadIdx.x & 31);
-        uint4 u[2];
+    template <class T> static __device__ __forceinline__ void eight(uint32_t from, int shift, float* x) {
+        constexpr int n = sizeof(typename T::type) / 2;                        // times 16 bytes
+        from += 16 * n * (threadIdx.x & 31);
+        uint4 u[n];
 #pragma unroll
-        for (int k = 0; k < n; k += 16) u[k / 16] = stage16(from + k);
-        if (ANY && n == 16 && begin == ON_2) {
-            uint32_t w;
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(from + 16));
-            u[0] = make_uint4(__byte_perm(u[0].x, u[0].y, 0x5432), __byte_perm(u[0].y, u[0].z, 0x5432), __byte_perm(u[0].z, u[0].w, 0x5432), __byte_perm(u[0].w, w, 0x5432));
+        for (int k = 0; k < n; ++k) u[k] = stage16(from + 16 * k);
+        if (ANY && shift) {
+            const uint4 more = stage16(from + 16 * n);
+            uint32_t w[4 * n + 4], z[4 * n + 1];
+            memcpy(w, u, 16 * n);
+            memcpy(w + 4 * n, &more, 16);
+            const int words = shift >> 2;                                      // the same in the whole warp
+            if (words == 0) { for (int k = 0; k <= 4 * n; ++k) z[k] = w[k]; }
+            else if (words == 1) { for (int k = 0; k <= 4 * n; ++k) z[k] = w[k + 1]; }
+            else if (words == 2) { for (int k = 0; k <= 4 * n; ++k) z[k] = w[k + 2]; }
+            else { for (int k = 0; k <= 4 * n; ++k) z[k] = w[k + 3]; }
+            if (n == 1 && (shift & 2)) { for (int k = 0; k < 4; ++k) z[k] = __byte_perm(z[k], z[k + 1], 0x5432); }
+            memcpy(u, z, 16 * n);
         }
         T::unpack(u, x);
     }
     __device__ __forceinline__ void take(const Bases& p, float* g, float* w, uint2& m, uint2& v) const {
         const int lane = threadIdx.x & 31;
-        eight<G>(base, p.grad_begin, g);
-        eight<W>(base + W_AT, p.weight_begin, w);
+        eight<G>(base, p.grad_shift, g);
+        eight<W>(base + W_AT, p.weight_shift, w);
         m = stage8(base + M_AT + 8 * lane);
         v = stage8(base + M_AT + BLK + 8 * lane);
     }
@@ -634,7 +638,7 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(cons
     float tensor_decay = 0.0f;
     // of the tensor: block past its last, and its blocks that can go the usual way, from `usual` to below `past`
     int end_t = 0, usual = 0, past = 0;
-    Bases p = {0, 0, 0, ON_16, ON_16, ON_16};
+    Bases p = {0, 0, 0, ON_16, ON_16, 0, 0};
     int t = 0;
     Tensor tn = {0, 0, 0.0f, 0};
     auto find = [&](int b) { t = a.owner[b]; tn = a.tensors[t]; };
@@ -643,14 +647,14 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(cons
         const uintptr_t e = (uintptr_t)tn.block0 * BLK;
         auto begin_of = [](const void* q, uintptr_t least) { return !((uintptr_t)q & least) ? ON_16 : !((uintptr_t)q & 3) ? ON_4 : ON_2; };
         p = {(uintptr_t)at.weight - e * sizeof(typename W::type), (uintptr_t)at.grad - e * sizeof(typename G::type), (uintptr_t)at.copy - e * 2,
-             begin_of(at.weight, W::ALIGN), begin_of(at.grad, BITS == 8 ? 15 : G::ALIGN), begin_of(at.copy, 15)};
+             begin_of(at.weight, W::ALIGN), begin_of(at.copy, 15), (int)((uintptr_t)at.weight & 15), (int)((uintptr_t)at.grad & 15)};
         end_t = (int)(tn.block0 + (tn.size + BLK - 1) / BLK);
         usual = (int)tn.block0;
         past = (int)(tn.block0 + tn.size / BLK);
-        const bool aligned = p.weight_begin == ON_16 && p.grad_begin == ON_16 && p.copy_begin == ON_16;
-        if (ANY && (p.weight_begin == ON_2 || p.grad_begin == ON_2)) {   // needs an element before and one after
+        const bool aligned = p.weight_begin == ON_16 && p.copy_begin == ON_16 && !((uintptr_t)at.grad & (BITS == 8 ? 15 : G::ALIGN));
+        if (ANY && (p.weight_shift || p.grad_shift)) {    // needs the tensor's neighbouring elements, up to 16 bytes of them
             usual += 1;
-            past -= tn.size % BLK == 0;
+            past -= tn.size % BLK < 8;
         }
         if (!a.fast || (!ANY && !aligned)) past = 0;
         tensor_decay = tn.decay;
@@ -1102,7 +1106,7 @@ int fill_table(co3_adamw* h, const void* const* grads, void* const* weights, voi
 
 template <int BITS, class W, class G>
 int launch_step_of(co3_adamw* h, const StepArgs& a, bool aligned, int grid, cudaStream_t st) {
-    // The 8-bit kernel that takes arrays from any beginning costs a tenth more on those that need none of it (124M bf16: 233 us, 209).
+    // The 8-bit kernel that takes arrays from any beginning costs a tenth more on those that need none of it (67M bf16: 129 us, 116).
     // With 32-bit moments only whole aligned blocks go the usual way, and the general way is near (11.2M f32: 59 us, 53).
     if constexpr (BITS == 8)
         if (!aligned) {
