@@ -432,15 +432,17 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
 __device__ __forceinline__ float root_fast(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float inverse_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+template <int BITS, bool ANY> constexpr bool STAGED = BITS == 8 || ANY;
 // With 8-bit moments a block is little to load and much to compute: its loads are started one block ahead, into shared memory, where
-// they take no registers.  A copy of the warp is 512 bytes in a row (with 32 bytes a lane in two copies of 16 each, sectors would
+// they take no registers.  With 32-bit ones weights and gradients go this way where they do not begin on 16 bytes (67M bf16: 235 us,
+// 288 element by element).  A copy of the warp is 512 bytes in a row (with 32 bytes a lane in two copies of 16 each, sectors would
 // be fetched twice), so lanes read what others copied and the warp meets before and after.
 // Weights and gradients that do not begin on 16 bytes come with what else lies in their first and last 16 (which the tensor's first
 // and last blocks, without neighbours in the tensor, leave to the general way), and are moved to their places when they are read.
-template <class W, class G, bool ANY> struct Stage {      // ANY: arrays may begin anywhere
+template <int BITS, class W, class G, bool ANY> struct Stage {      // ANY: arrays may begin anywhere
     static constexpr int W_BYTES = sizeof(typename W::type) * BLK, G_BYTES = sizeof(typename G::type) * BLK;
-    static constexpr int W_AT = G_BYTES + 16, M_AT = W_AT + W_BYTES + 16, BYTES = M_AT + 2 * BLK;
-    uint32_t base;                            // of the warp: gradient, weights (each with room for 16 bytes more), codes of the two moments
+    static constexpr int W_AT = G_BYTES + 16, M_AT = W_AT + W_BYTES + 16, BYTES = M_AT + (BITS == 8 ? 2 * BLK : 0);
+    uint32_t base;                            // of the warp: gradient, weights (each with room for 16 bytes more), codes of 8-bit moments
     template <int N> static __device__ __forceinline__ void bring(uint32_t to, const char* from, int shift) {
         const int lane = threadIdx.x & 31;
         if (ANY) from -= shift;
@@ -453,8 +455,10 @@ template <class W, class G, bool ANY> struct Stage {      // ANY: arrays may beg
         const int64_t at = (int64_t)b * BLK;
         bring<G_BYTES>(base, reinterpret_cast<const char*>(p.grad) + at * (int)sizeof(typename G::type), p.grad_shift);
         bring<W_BYTES>(base + W_AT, reinterpret_cast<const char*>(p.weight) + at * (int)sizeof(typename W::type), p.weight_shift);
-        copy_async<8>(base + M_AT + 8 * lane, static_cast<const uint8_t*>(a.m) + at + 8 * lane);
-        copy_async<8>(base + M_AT + BLK + 8 * lane, static_cast<const uint8_t*>(a.v) + at + 8 * lane);
+        if (BITS == 8) {
+            copy_async<8>(base + M_AT + 8 * lane, static_cast<const uint8_t*>(a.m) + at + 8 * lane);
+            copy_async<8>(base + M_AT + BLK + 8 * lane, static_cast<const uint8_t*>(a.v) + at + 8 * lane);
+        }
     }
     template <class T> static __device__ __forceinline__ void eight(uint32_t from, int shift, float* x) {
         constexpr int n = sizeof(typename T::type) / 2;                        // times 16 bytes
@@ -477,13 +481,11 @@ template <class W, class G, bool ANY> struct Stage {      // ANY: arrays may beg
         }
         T::unpack(u, x);
     }
-    __device__ __forceinline__ void take(const Bases& p, float* g, float* w, uint2& m, uint2& v) const {
-        const int lane = threadIdx.x & 31;
+    __device__ __forceinline__ void take(const Bases& p, float* g, float* w) const {
         eight<G>(base, p.grad_shift, g);
         eight<W>(base + W_AT, p.weight_shift, w);
-        m = stage8(base + M_AT + 8 * lane);
-        v = stage8(base + M_AT + BLK + 8 * lane);
     }
+    __device__ __forceinline__ uint2 codes(int which) const { return stage8(base + M_AT + which * BLK + 8 * (threadIdx.x & 31)); }
     // A lane's eight 32-bit (u[0], u[1]) or 16-bit (u[0]) elements to an array that does not begin on 16 bytes, by way of `part`, which
     // the warp has read.
     template <int N> static __device__ __forceinline__ void send(uint32_t part, const uint4* u, char* to, Begin begin) {
@@ -511,11 +513,10 @@ template <class W, class G, bool ANY> struct Stage {      // ANY: arrays may beg
     }
 };
 
-// The usual way: a whole block, whose tensors are aligned if the moments have 32 bits.  Lane i takes the elements 8i .. 8i + 7, each
-// array in one access.
+// The usual way: a whole block.  Lane i takes the elements 8i .. 8i + 7, each aligned array in one access.
 // Returns false, before anything is written, if a value needs the general way.
 template <int BITS, class W, class G, bool ANY>
-__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, const Stage<W, G, ANY>& stage, uint8_t* tops) {
+__device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, uint32_t key, const Bases& p, int b, const Stage<BITS, W, G, ANY>& stage, uint8_t* tops) {
     constexpr bool W16 = sizeof(typename W::type) == 2;
     const int lane = threadIdx.x & 31;
     const int64_t at = (int64_t)b * BLK + PER_LANE * lane;
@@ -524,13 +525,17 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     bool other = false;                                   // some value needs the general way
     float b1m = 0.0f, b2v = 0.0f;                         // beta1 and beta2 times the scales of 8-bit moments
     if (BITS == 32) {
-        G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
-        W::load8(pw, w);
         F32::load8(static_cast<const float*>(a.m) + at, m);
         F32::load8(static_cast<const float*>(a.v) + at, v);
+    }
+    if (!STAGED<BITS, ANY>) {
+        G::load8(reinterpret_cast<const typename G::type*>(p.grad) + at, g);
+        W::load8(pw, w);
     } else {
-        uint2 cm, cv;
-        stage.take(p, g, w, cm, cv);
+        stage.take(p, g, w);
+    }
+    if (BITS == 8) {
+        const uint2 cm = stage.codes(0), cv = stage.codes(1);
         const int m_top = tops[0], v_top = tops[STRETCH];
         other = m_top > ScaleM::PLAIN || v_top > ScaleV::PLAIN;
         ScaleM::first8(cm, m);
@@ -590,7 +595,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
             h[k / 2] = __byte_perm(__float_as_uint(w[k]) + __umulhi(r[k] << 6, 0x10000u), __float_as_uint(w[k + 1]) + __umulhi(r[k + 1] << 6, 0x10000u), 0x7632);
         const uint4 u = make_uint4(h[0], h[1], h[2], h[3]);
         if (!ANY || p.weight_begin == ON_16) *reinterpret_cast<uint4*>(pw) = u;
-        else Stage<W, G, ANY>::template send<2 * BLK>(stage.base + Stage<W, G, ANY>::W_AT, &u, reinterpret_cast<char*>(pw - PER_LANE * lane), p.weight_begin);
+        else Stage<BITS, W, G, ANY>::template send<2 * BLK>(stage.base + Stage<BITS, W, G, ANY>::W_AT, &u, reinterpret_cast<char*>(pw - PER_LANE * lane), p.weight_begin);
     } else {
         // (eight floats in two accesses of 16 bytes where 32 in one are not possible would write each sector twice)
         if (!ANY || p.weight_begin == ON_16) {
@@ -598,7 +603,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
         } else {
             uint4 u[2];
             memcpy(u, w, sizeof(u));
-            Stage<W, G, ANY>::template send<4 * BLK>(stage.base + Stage<W, G, ANY>::W_AT, u, reinterpret_cast<char*>(pw - PER_LANE * lane), p.weight_begin);
+            Stage<BITS, W, G, ANY>::template send<4 * BLK>(stage.base + Stage<BITS, W, G, ANY>::W_AT, u, reinterpret_cast<char*>(pw - PER_LANE * lane), p.weight_begin);
         }
         if (a.copy_type != CO3_NONE) {
             if (!ANY || p.copy_begin == ON_16) {
@@ -606,7 +611,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
                 else F16::store8(reinterpret_cast<__half*>(p.copy) + at, w);
             } else {
                 const uint4 u = a.copy_type == CO3_BF16 ? Bf16::pack(w) : F16::pack(w);
-                Stage<W, G, ANY>::template send<2 * BLK>(stage.base + Stage<W, G, ANY>::W_AT, &u, reinterpret_cast<char*>(p.copy) + (int64_t)b * (2 * BLK), p.copy_begin);
+                Stage<BITS, W, G, ANY>::template send<2 * BLK>(stage.base + Stage<BITS, W, G, ANY>::W_AT, &u, reinterpret_cast<char*>(p.copy) + (int64_t)b * (2 * BLK), p.copy_begin);
             }
         }
     }
@@ -667,13 +672,15 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(cons
     if (b < end) enter();
     const bool skip = a.info && a.info->nonfinite != 0;
     const float lr = a.d_lr ? *a.d_lr : a.lr;
-    Stage<W, G, ANY> stage = {(uint32_t)__cvta_generic_to_shared(stages) + 2 * warp * Stage<W, G, ANY>::BYTES};
-    uint32_t to_other = Stage<W, G, ANY>::BYTES;
+    Stage<BITS, W, G, ANY> stage = {(uint32_t)__cvta_generic_to_shared(stages) + 2 * warp * Stage<BITS, W, G, ANY>::BYTES};
+    uint32_t to_other = Stage<BITS, W, G, ANY>::BYTES;
     bool have = false;                                    // block b is on its way to `stage`
-    if (BITS == 8) {
+    if (STAGED<BITS, ANY>) {
         have = b >= usual && b < min(end, past) && !skip;
         if (have) stage.start(a, p, b);
         asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (BITS == 8) {
         for (int i = threadIdx.x; i < 2 * STRETCH; i += 32 * WARPS)
             if ((i & (STRETCH - 1)) < count) tops[i] = (i < STRETCH ? a.m_exp : a.v_exp)[begin + (i & (STRETCH - 1))];
     }
@@ -689,13 +696,13 @@ __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(cons
             if (b >= end_t) { find(b); enter(); }
             s.decay = lr * tensor_decay;
             const uint32_t key = block_key(step_key, (int64_t)b * BLK);
-            if (BITS == 8) {
+            if (STAGED<BITS, ANY>) {
                 if (!have && b >= usual && b < past) {
                     stage.start(a, p, b);
                     asm volatile("cp.async.commit_group;" ::: "memory");
                 }
                 have = b + WARPS >= usual && b + WARPS < min(end, past);
-                if (have) Stage<W, G, ANY>{stage.base + to_other}.start(a, p, b + WARPS);
+                if (have) Stage<BITS, W, G, ANY>{stage.base + to_other}.start(a, p, b + WARPS);
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncwarp();
@@ -1106,15 +1113,14 @@ int fill_table(co3_adamw* h, const void* const* grads, void* const* weights, voi
 
 template <int BITS, class W, class G>
 int launch_step_of(co3_adamw* h, const StepArgs& a, bool aligned, int grid, cudaStream_t st) {
-    // The 8-bit kernel that takes arrays from any beginning costs a tenth more on those that need none of it (67M bf16: 129 us, 116).
-    // With 32-bit moments only whole aligned blocks go the usual way, and the general way is near (11.2M f32: 59 us, 53).
-    if constexpr (BITS == 8)
-        if (!aligned) {
-            constexpr int shared = 2 * WARPS * Stage<W, G, true>::BYTES;
-            static_assert(shared + 2 * STRETCH <= 48 * 1024, "more needs to be asked for");
-            return launch(h, adamw_kernel<BITS, W, G, true>, grid, 32 * WARPS, shared, st, a);
-        }
-    constexpr int shared = BITS == 8 ? 2 * WARPS * Stage<W, G, false>::BYTES : 0;
+    // The kernel that takes arrays from any beginning, on ones that need it and ones that do not, against the other one (67M elements):
+    // 8-bit moments, bf16 138 and 129 us against 111, f32 173 and 167 against 166; 32-bit ones, bf16 235 against 225, f32 284 against 277.
+    if (!aligned) {
+        constexpr int shared = 2 * WARPS * Stage<BITS, W, G, true>::BYTES;
+        static_assert(shared + 2 * STRETCH <= 48 * 1024, "more needs to be asked for");
+        return launch(h, adamw_kernel<BITS, W, G, true>, grid, 32 * WARPS, shared, st, a);
+    }
+    constexpr int shared = BITS == 8 ? 2 * WARPS * Stage<BITS, W, G, false>::BYTES : 0;
     return launch(h, adamw_kernel<BITS, W, G, false>, grid, 32 * WARPS, shared, st, a);
 }
 
@@ -1294,13 +1300,15 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     }
     const int grid = h->n_blocks ? (int)((h->n_blocks + a.stretch - 1) / a.stretch) : 1;
     const bool w16 = h->weight_type == CO3_BF16;
-    uintptr_t weight_bits = 0, other_bits = 0;
+    uintptr_t weight_bits = 0, grad_bits = 0, copy_bits = 0;
     for (int t = 0; t < h->n_tensors; ++t)
         if (h->sizes[t] >= BLK) {
             weight_bits |= (uintptr_t)weights[t];
-            other_bits |= (uintptr_t)grads[t] | (copies ? (uintptr_t)copies[t] : 0);
+            grad_bits |= (uintptr_t)grads[t];
+            if (copies) copy_bits |= (uintptr_t)copies[t];
         }
-    const bool aligned = !(weight_bits & (w16 ? Bf16::ALIGN : F32::ALIGN)) && !(other_bits & 15);
+    const uintptr_t grad_align = h->state_bits == 32 && h->grad_type == CO3_F32 ? F32::ALIGN : 15;    // 8-bit: copied 16 bytes at a time
+    const bool aligned = !(weight_bits & (w16 ? Bf16::ALIGN : F32::ALIGN)) && !(grad_bits & grad_align) && !(copy_bits & 15);
     if (h->state_bits == 32) return w16 ? launch_step<32, Bf16>(h, a, aligned, grid, st) : launch_step<32, F32>(h, a, aligned, grid, st);
     return w16 ? launch_step<8, Bf16>(h, a, aligned, grid, st) : launch_step<8, F32>(h, a, aligned, grid, st);
 }
