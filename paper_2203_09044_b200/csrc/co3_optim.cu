@@ -536,7 +536,7 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     }
     if (BITS == 8) {
         const uint2 cm = stage.codes(0), cv = stage.codes(1);
-        const int m_top = tops[0], v_top = tops[STRETCH];
+        const int m_top = max((int)tops[0], ScaleM::LEAST), v_top = tops[STRETCH];       // (0 before the first step)
         other = m_top > ScaleM::PLAIN || v_top > ScaleV::PLAIN;
         ScaleM::first8(cm, m);
         ScaleV::second8(cv, v);

@@ -785,3 +785,16 @@ def test_every_code_is_read_by_the_formula(binding, off):
     assert ref.kept == 0 and opt.status() == (0, 0, 0)
     for got, want in ((opt.m_exp, ref.mt), (opt.v_exp, ref.vt), (opt.m, ref.mc), (opt.v, ref.vc)):
         assert np.array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_negative_zeros_leave_fresh_moments_at_zero(binding, bits):
+    """In whole blocks and in a part of one the same bits: a sum of +0 and -0 is +0."""
+    p, g = torch.randn(600, device="cuda"), torch.full((600,), -0.0, device="cuda")
+    before = p.clone()
+    opt = binding.AdamW([p], state_bits=bits, weight_decay=0.0)
+    for _ in range(2):
+        opt.step([g])
+    assert not opt.m.view(torch.int32 if bits == 32 else torch.uint8).any() and not opt.v.view(torch.int32 if bits == 32 else torch.uint8).any()
+    assert torch.equal(p, before)
