@@ -1082,6 +1082,12 @@ bool on_device(const co3_adamw* h) {
     return dev == h->device;
 }
 
+// To the device, and there when the call returns.  A copy from pageable memory alone may still be on its way then, and streams that do
+// not wait for the null stream (PyTorch's) would not wait for it.
+bool to_device(void* to, const void* from, size_t bytes) {
+    return cudaMemcpy(to, from, bytes, cudaMemcpyHostToDevice) == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
+}
+
 // Whether all pointers are there and aligned as their types.  weights == null: gradients only.
 bool pointers_fine(const co3_adamw* h, const void* const* grads, void* const* weights, void* const* copies) {
     for (int t = 0; t < h->n_tensors; ++t) {
@@ -1210,8 +1216,9 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
             if (ok && blocks) {
                 const int64_t grid = (blocks + 255) / 256;
                 owner_kernel<<<(int)(grid < 4096 ? grid : 4096), 256>>>(h->tensors, n, h->owner, blocks);
-                ok = cudaGetLastError() == cudaSuccess && cudaStreamSynchronize(nullptr) == cudaSuccess;
+                ok = cudaGetLastError() == cudaSuccess;
             }
+            ok = ok && cudaStreamSynchronize(nullptr) == cudaSuccess;
             if (!ok) { (void)cudaGetLastError(); rc = CO3_ECUDA; }
         }
     }
@@ -1339,7 +1346,7 @@ extern "C" int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped
     if (clear) {
         s.flags = 0;
         s.skipped_elements = s.skipped_steps = 0;
-        if (cudaMemcpy(h->sc, &s, sizeof(s), cudaMemcpyHostToDevice) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
+        if (!to_device(h->sc, &s, sizeof(s))) { (void)cudaGetLastError(); return CO3_ECUDA; }
     }
     return CO3_OK;
 }
@@ -1366,7 +1373,7 @@ extern "C" int co3_adamw_steps_import(co3_adamw* h, int64_t steps) {
         s.pow2 = pow(h->beta2, (double)steps);
     }
     next_scalars(s, h->beta1, h->beta2, h->seed);
-    if (cudaMemcpy(h->sc, &s, sizeof(s), cudaMemcpyHostToDevice) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
+    if (!to_device(h->sc, &s, sizeof(s))) { (void)cudaGetLastError(); return CO3_ECUDA; }
     return CO3_OK;
 }
 

@@ -798,3 +798,29 @@ def test_negative_zeros_leave_fresh_moments_at_zero(binding, bits):
         opt.step([g])
     assert not opt.m.view(torch.int32 if bits == 32 else torch.uint8).any() and not opt.v.view(torch.int32 if bits == 32 else torch.uint8).any()
     assert torch.equal(p, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_on_a_side_stream_sees_steps_that_were_just_set(binding, bits):
+    """set_steps and status(clear=True), each followed at once by a step on a stream that does not wait for the null stream."""
+    gen = torch.Generator().manual_seed(12)
+    w, g = make([3000], torch.bfloat16, gen), make([3000], torch.bfloat16, gen)
+    side, out = torch.cuda.Stream(), []
+    for wait in (True, False):
+        p = [w[0].clone()]
+        opt = binding.AdamW(p, state_bits=bits, seed=6)
+        bound = opt.bind_grads(g)
+        torch.cuda.synchronize()
+        for t in (0, 10, 1000, 50_000):
+            opt.set_steps(t)
+            if wait:
+                torch.cuda.synchronize()
+            opt.step(bound, stream=side)
+            assert opt.status(clear=True) == (0, 0, 0)
+            if wait:
+                torch.cuda.synchronize()
+            opt.step(bound, stream=side)
+            assert opt.steps() == t + 2
+        out.append((p[0], opt.m, opt.v))
+    assert all(torch.equal(x, y) for x, y in zip(*out))
