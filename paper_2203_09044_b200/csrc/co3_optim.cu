@@ -1337,7 +1337,7 @@ extern "C" int co3_adamw_values(co3_adamw* h, const co3_adamw_state* state, void
 }
 
 extern "C" int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped_elements, uint64_t* skipped_steps, int32_t clear) {
-    if (!h) return CO3_EINVAL;
+    if (!h || !on_device(h)) return CO3_EINVAL;
     Scalars s;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, h->sc, sizeof(s), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     if (flags) *flags = s.flags;
@@ -1352,7 +1352,7 @@ extern "C" int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped
 }
 
 extern "C" int co3_adamw_steps_export(co3_adamw* h, int64_t* steps) {
-    if (!h || !steps) return CO3_EINVAL;
+    if (!h || !steps || !on_device(h)) return CO3_EINVAL;
     Scalars s;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, h->sc, sizeof(s), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     *steps = s.steps;
@@ -1360,7 +1360,7 @@ extern "C" int co3_adamw_steps_export(co3_adamw* h, int64_t* steps) {
 }
 
 extern "C" int co3_adamw_steps_import(co3_adamw* h, int64_t steps) {
-    if (!h || steps < 0) return CO3_EINVAL;
+    if (!h || steps < 0 || !on_device(h)) return CO3_EINVAL;
     Scalars s;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, h->sc, sizeof(s), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     s.steps = steps;

@@ -67,3 +67,16 @@ def test_nothing_is_left_to_be_copied_when_a_call_returns(fake, sizes):
         assert h.set_steps(7) == b.OK and fake.fake_waiting() == 0
         assert h.status(clear=1) == (b.OK, (0, 0, 0)) and fake.fake_waiting() == 0
         assert h.steps() == (b.OK, 7)
+
+
+def test_with_another_device_current_every_call_is_refused(fake):
+    """As the norm and the step refuse it; a wait would be for the wrong device."""
+    with Handle(fake) as h:
+        assert h.set_steps(3) == b.OK
+        fake.fake_set_device(1)
+        before = fake.fake_calls()
+        assert h.steps() == (b.EINVAL, -1) and h.set_steps(9) == b.EINVAL
+        assert h.status(clear=0)[0] == b.EINVAL and h.status(clear=1)[0] == b.EINVAL
+        assert fake.fake_calls() == before
+        fake.fake_set_device(0)
+        assert h.steps() == (b.OK, 3)
