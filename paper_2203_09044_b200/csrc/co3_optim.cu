@@ -8,6 +8,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 #include <new>
+#include <stddef.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -1343,10 +1344,12 @@ extern "C" int co3_adamw_status(co3_adamw* h, uint32_t* flags, uint64_t* skipped
     if (flags) *flags = s.flags;
     if (skipped_elements) *skipped_elements = s.skipped_elements;
     if (skipped_steps) *skipped_steps = s.skipped_steps;
-    if (clear) {
-        s.flags = 0;
-        s.skipped_elements = s.skipped_steps = 0;
-        if (!to_device(h->sc, &s, sizeof(s))) { (void)cudaGetLastError(); return CO3_ECUDA; }
+    if (clear) {                              // these three, side by side, and nothing that a step of another thread may be changing
+        constexpr size_t first = offsetof(Scalars, flags), past = offsetof(Scalars, skipped_steps) + sizeof(s.skipped_steps);
+        if (cudaMemset((char*)h->sc + first, 0, past - first) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return CO3_ECUDA;
+        }
     }
     return CO3_OK;
 }
@@ -1361,8 +1364,8 @@ extern "C" int co3_adamw_steps_export(co3_adamw* h, int64_t* steps) {
 
 extern "C" int co3_adamw_steps_import(co3_adamw* h, int64_t steps) {
     if (!h || steps < 0 || !on_device(h)) return CO3_EINVAL;
+    if (cudaDeviceSynchronize() != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     Scalars s;
-    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&s, h->sc, sizeof(s), cudaMemcpyDeviceToHost) != cudaSuccess) { (void)cudaGetLastError(); return CO3_ECUDA; }
     s.steps = steps;
     // the products that the steps themselves would have left, to the bit; after very many (0.1 s of them here) the powers
     s.pow1 = s.pow2 = 1.0;
@@ -1373,7 +1376,7 @@ extern "C" int co3_adamw_steps_import(co3_adamw* h, int64_t steps) {
         s.pow2 = pow(h->beta2, (double)steps);
     }
     next_scalars(s, h->beta1, h->beta2, h->seed);
-    if (!to_device(h->sc, &s, sizeof(s))) { (void)cudaGetLastError(); return CO3_ECUDA; }
+    if (!to_device(h->sc, &s, offsetof(Scalars, key) + sizeof(s.key))) { (void)cudaGetLastError(); return CO3_ECUDA; }
     return CO3_OK;
 }
 

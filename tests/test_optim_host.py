@@ -80,3 +80,20 @@ def test_with_another_device_current_every_call_is_refused(fake):
         assert fake.fake_calls() == before
         fake.fake_set_device(0)
         assert h.steps() == (b.OK, 3)
+
+
+def test_clearing_the_status_writes_nothing_else(fake):
+    """Not the step count, which another thread's step may have moved on since it was read."""
+    with Handle(fake) as h:
+        assert h.set_steps(3) == b.OK
+        fake.fake_advance()
+        assert h.status(clear=1) == (b.OK, (0, 0, 0))
+        assert h.steps() == (b.OK, 4)
+
+
+def test_setting_the_steps_leaves_the_status(fake):
+    """... and the tickets, which a step that another thread has begun may hold."""
+    with Handle(fake) as h:
+        fake.fake_written()
+        assert h.set_steps(3) == b.OK
+        assert fake.fake_written() <= 40                # count, two powers, two corrections, key
