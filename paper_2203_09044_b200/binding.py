@@ -663,6 +663,16 @@ class GradNorm:
                 t.record_stream(stream)
         return stream.cuda_stream
 
+    def _empty(self, shape, dtype, stream):
+        """Memory for an output that `stream` writes (None: the current one), from that stream's own: memory of the current stream may
+        still be in use by work that waits there.  The caller may in turn use it on the current stream when it is given back."""
+        if stream is None:
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+        with self.torch.cuda.stream(stream):
+            t = self.torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(self.torch.cuda.current_stream(self.device))
+        return t
+
     def bind_grads(self, grads):
         """Check the gradient tensors and keep their pointers, for programs whose gradients stay where they are.  (What another
         optimizer's bind_grads returned is checked again.)"""
@@ -675,7 +685,7 @@ class GradNorm:
         and in the last two the count of non-finite elements as one int64 (`info[2:].view(torch.int64)`)."""
         g = grads if type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype else self.bind_grads(grads)
         if info is None:
-            info = self.torch.empty(4, dtype=self.torch.float32, device=self.device)
+            info = self._empty(4, self.torch.float32, stream)
         _check(info, self.torch.float32, 4, self.device, "info")
         if tensor_norms is not None:
             _check(tensor_norms, self.torch.float32, len(self.sizes), self.device, "tensor_norms")
@@ -762,7 +772,7 @@ class AdamW(GradNorm):
     def state_values(self, m_out=None, v_out=None, stream=None):
         """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""
         if m_out is None or v_out is None:
-            m_out, v_out = (self.torch.empty((self.n_blocks, STATE_BLOCK), dtype=self.torch.bfloat16, device=self.device) for _ in range(2))
+            m_out, v_out = (self._empty((self.n_blocks, STATE_BLOCK), self.torch.bfloat16, stream) for _ in range(2))
         n, kind = self.n_blocks * STATE_BLOCK, m_out.dtype
         _check(m_out, kind, n, self.device, "m_out")
         _check(v_out, kind, n, self.device, "v_out")

@@ -824,3 +824,23 @@ def test_a_step_on_a_side_stream_sees_steps_that_were_just_set(binding, bits):
             assert opt.steps() == t + 2
         out.append((p[0], opt.m, opt.v))
     assert all(torch.equal(x, y) for x, y in zip(*out))
+
+
+@pytest.mark.gpu
+def test_outputs_for_another_stream_take_no_memory_that_is_still_in_use(binding):
+    """Tensors of the size of the outputs are given back while work that reads them still waits on the current stream."""
+    opt = binding.AdamW([torch.ones(1 << 20, device="cuda")], state_bits=8)
+    g = opt.bind_grads([torch.ones(1 << 20, device="cuda")])
+    opt.step(g)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    used = [torch.full((opt.n_blocks, 256), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)] + [torch.full((4,), 3.0, device="cuda")]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)                       # about 10 ms
+    copies = [x.clone() for x in used]
+    used.clear()
+    info = opt.grad_norm(g, stream=side)
+    m, v = opt.state_values(stream=side)
+    torch.cuda.synchronize()
+    assert all((x == 3.0).all() for x in copies)
+    assert info[1].item() == 1024.0 and (m > 0.09).all() and (v > 0).all()

@@ -1,11 +1,14 @@
 """The host side of the optimizer calls, without a GPU: csrc/co3_optim.cu linked with a runtime of host memory (fake_cudart.c), in
 which copies and fills are late as the real one may have them."""
+import contextlib
 import ctypes as C
 import os
 import subprocess
+import types
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2203_09044_b200 import binding as b, build
 
@@ -97,3 +100,76 @@ def test_setting_the_steps_leaves_the_status(fake):
         fake.fake_written()
         assert h.set_steps(3) == b.OK
         assert fake.fake_written() <= 40                # count, two powers, two corrections, key
+
+
+# ---- the Python binding, with tensors of the host in the place of the device's ----------------------------------------------
+STREAM = types.SimpleNamespace(cuda_stream=0)
+
+
+class Library:
+    """The library with the fake runtime; `steps` has the arguments of each co3_adamw_step."""
+
+    def __init__(self, L):
+        self.L, self.steps = L, []
+        for name in b.EXPORTS:
+            if "adamw" in name or name == "co3_grad_norm":
+                getattr(L, name).restype, getattr(L, name).argtypes = getattr(b.lib(), name).restype, getattr(b.lib(), name).argtypes
+
+    def __getattr__(self, name):
+        return getattr(self.L, name)
+
+    def co3_adamw_step(self, handle, weights, grads, copies, state, *rest):
+        self.steps.append((weights, grads, copies, state))
+        return self.L.co3_adamw_step(handle, weights, grads, copies, state, *rest)
+
+
+@pytest.fixture
+def host(fake, monkeypatch):
+    """A place to run the binding in: `library`, `inside` (whether torch.cuda.stream is in force), `events`."""
+    place = types.SimpleNamespace(library=Library(fake), inside=False, events=[])
+    create = b.GradNorm._create
+
+    def create_here(self, *a, **k):
+        create(self, *a, **k)
+        self.device, self._current_stream = torch.device("cpu"), lambda: 0
+
+    @contextlib.contextmanager
+    def in_stream(stream):
+        assert stream is STREAM
+        place.inside = True
+        yield
+        place.inside = False
+    monkeypatch.setattr(b, "_lib", place.library)
+    monkeypatch.setattr(b.GradNorm, "_create", create_here)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "stream", in_stream)
+    current = types.SimpleNamespace(cuda_stream=0, synchronize=lambda: place.events.append("synchronize"))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: place.events.append(("record", t.data_ptr(), s)))
+    place.current = current
+    return place
+
+
+def test_outputs_that_a_call_makes_for_a_stream_come_from_its_memory(host, monkeypatch):
+    """Memory of the current stream may still be in use by work that waits there; and what was made for the other stream may be in use
+    on the current one when it is given back."""
+    opt = b.AdamW([torch.ones(300)], state_bits=8)
+    made, empty_of = [], torch.empty
+
+    def empty(*a, **k):
+        made.append((empty_of(*a, **k), host.inside))
+        return made[-1][0]
+    monkeypatch.setattr(torch, "empty", empty)
+    g = [torch.ones(300)]
+    info = opt.grad_norm(g, stream=STREAM)
+    assert [i for _, i in made] == [True] and info is made[0][0]
+    assert ("record", info.data_ptr(), host.current) in host.events and ("record", info.data_ptr(), STREAM) in host.events
+    made.clear()
+    values = opt.state_values(stream=STREAM)
+    assert [i for _, i in made] == [True, True]
+    for v, (m, _) in zip(values, made):
+        assert v is m and ("record", v.data_ptr(), host.current) in host.events and ("record", v.data_ptr(), STREAM) in host.events
+    made.clear()
+    opt.grad_norm(g)
+    opt.state_values()
+    assert [i for _, i in made] == [False] * 3
