@@ -743,6 +743,8 @@ class AdamW(GradNorm):
             t = torch.zeros(shape, dtype=kind, device=self.device) if state is None else state[k]
             _check(t, kind, int(np.prod(shape)), self.device, k)
             setattr(self, k, t)
+        if state is None:
+            torch.cuda.current_stream(self.device).synchronize()      # zero for a first step on any stream
         self._state = AdamwState(*[getattr(self, k).data_ptr() if k in names else None for k in ("m", "v", "m_exp", "v_exp")])
         self._state_p = C.addressof(self._state)
         self._weights, self._copies = self.params.address, None if self.copies is None else self.copies.address

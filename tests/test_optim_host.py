@@ -173,3 +173,12 @@ def test_outputs_that_a_call_makes_for_a_stream_come_from_its_memory(host, monke
     opt.grad_norm(g)
     opt.state_values()
     assert [i for _, i in made] == [False] * 3
+
+
+def test_a_new_optimizer_s_moments_are_zero_for_every_stream(host):
+    """The fill is waited for, as what co3_adamw_create copies is: the first step may be on another stream."""
+    opt = b.AdamW([torch.ones(300)])
+    assert host.events == ["synchronize"]
+    host.events.clear()
+    b.AdamW([torch.ones(300)], state=dict(m=opt.m, v=opt.v))
+    assert host.events == []
