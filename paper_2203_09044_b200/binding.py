@@ -609,7 +609,7 @@ class TensorList:
             if order is not None and n and _order(t) != order[i]:
                 raise ValueError(f"{what} {i}: its elements lie in another order than those of its weights")
         self.pointers = (C.c_void_p * len(sizes))(*[t.data_ptr() if n else None for t, n in zip(self.tensors, sizes)])
-        self.address, self.sizes, self.dtype = C.addressof(self.pointers), sizes, dtype
+        self.address, self.sizes, self.dtype, self.order = C.addressof(self.pointers), sizes, dtype, order
 
 
 class GradNorm:
@@ -680,10 +680,14 @@ class GradNorm:
             grads = grads.tensors
         return TensorList(grads, self.sizes, self.grad_dtype, self.device, "gradients", self._order)
 
+    def _is_bound(self, grads):
+        """Whether bind_grads of this object returned `grads`."""
+        return type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype and grads.order is self._order
+
     def grad_norm(self, grads, info=None, max_norm=0.0, grad_scale=1.0, tensor_norms=None, stream=None):
         """grads: the tensors, or what bind_grads returned.  info: 4 float32 on the device, written and returned: factor, norm,
         and in the last two the count of non-finite elements as one int64 (`info[2:].view(torch.int64)`)."""
-        g = grads if type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype else self.bind_grads(grads)
+        g = grads if self._is_bound(grads) else self.bind_grads(grads)
         if info is None:
             info = self._empty(4, self.torch.float32, stream)
         _check(info, self.torch.float32, 4, self.device, "info")
@@ -713,12 +717,26 @@ def _check(t, dtype, n, device, what):
         raise ValueError(f"{what}: {n} contiguous {dtype} on {device} expected, got {t.numel()} {t.dtype} on {t.device}")
 
 
+def _moment(name):
+    def get(self):
+        if name not in self._moments:
+            raise AttributeError(name)
+        return self._moments[name]
+
+    def put(self, tensor):
+        self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, {**self._moments, name: tensor})
+    return property(get, put)
+
+
 class AdamW(GradNorm):
     """AdamW over the tensors `params` (float32 or bfloat16, on the current CUDA device, updated in place; any dense order of
     dimensions, gradients and copies in the same).  copies: tensors of bfloat16 or float16 that receive the new float32 weights.
     weight_decay: one number, or one per tensor.  state_bits: 32, or 8 for moments of one byte each (include/co3.h).
     The moments are the attributes m, v (and m_exp, v_exp): [n_blocks][256]; `state` gives existing ones (set_steps then sets the
-    steps that they come from)."""
+    steps that they come from).  Weights, copies and moments may be given other storage between two steps (`p.data = x`, `opt.m = x`);
+    a captured step keeps the one that it was captured with."""
+
+    m, v, m_exp, v_exp = (_moment(k) for k in ("m", "v", "m_exp", "v_exp"))
 
     def __init__(self, params, grad_dtype=None, copies=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32,
                  seed=0, state=None):
@@ -733,26 +751,48 @@ class AdamW(GradNorm):
             raise ValueError("no copies")
         self._create(sizes, dtype, grad_dtype or dtype, copies[0].dtype if copies else None, state_bits, betas, eps, weight_decay, seed)
         self.lr, self.state_bits = float(lr), int(state_bits)
-        self.params = TensorList(params, sizes, dtype, self.device, "weights")
-        self._order = [_order(p) for p in params]
-        self.copies = None if copies is None else TensorList(copies, sizes, copies[0].dtype, self.device, "copies", self._order)
-        kind = torch.float32 if self.state_bits == 32 else torch.uint8
-        names = ("m", "v") if self.state_bits == 32 else ("m", "v", "m_exp", "v_exp")
-        for k in names:
-            shape = (self.n_blocks, STATE_BLOCK) if k in ("m", "v") else (self.n_blocks,)
-            t = torch.zeros(shape, dtype=kind, device=self.device) if state is None else state[k]
-            _check(t, kind, int(np.prod(shape)), self.device, k)
-            setattr(self, k, t)
+        self._dtype, self._copy_dtype = dtype, copies[0].dtype if copies else None
+        self._kind = torch.float32 if self.state_bits == 32 else torch.uint8
+        self._shapes = dict(m=(self.n_blocks, STATE_BLOCK), v=(self.n_blocks, STATE_BLOCK))
+        if self.state_bits == 8:
+            self._shapes.update(m_exp=(self.n_blocks,), v_exp=(self.n_blocks,))
         if state is None:
+            state = {k: torch.zeros(shape, dtype=self._kind, device=self.device) for k, shape in self._shapes.items()}
             torch.cuda.current_stream(self.device).synchronize()      # zero for a first step on any stream
-        self._state = AdamwState(*[getattr(self, k).data_ptr() if k in names else None for k in ("m", "v", "m_exp", "v_exp")])
+        self._bind_own(params, copies, {k: state[k] for k in self._shapes})
+
+    def _bind_own(self, params, copies, moments):
+        """Look at weights, copies and moments and keep where they are; nothing changes if one does not fit."""
+        weights = TensorList(params, self.sizes, self._dtype, self.device, "weights")
+        order = [_order(p) for p in weights.tensors]
+        if order == self._order:
+            order = self._order                           # gradients bound by it stay bound
+        if copies is not None:
+            copies = TensorList(copies, self.sizes, self._copy_dtype, self.device, "copies", order)
+        for k, shape in self._shapes.items():
+            _check(moments[k], self._kind, int(np.prod(shape)), self.device, k)
+        self.params, self.copies, self._moments, self._order = weights, copies, moments, order
+        self._state = AdamwState(*[moments[k].data_ptr() if k in moments else None for k in ("m", "v", "m_exp", "v_exp")])
         self._state_p = C.addressof(self._state)
-        self._weights, self._copies = self.params.address, None if self.copies is None else self.copies.address
+        self._weights, self._copies = weights.address, None if copies is None else copies.address
+        self._own = weights.tensors + (copies.tensors if copies else []) + list(moments.values())
+        self._at = [t.data_ptr() for t in self._own]
+        self._data_ptr = self.torch.Tensor.data_ptr
+
+    def _look(self):
+        """A program may have given one of them other storage since, and what they had may be somebody else's by now."""
+        if [*map(self._data_ptr, self._own)] != self._at:
+            self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, self._moments)
+
+    def bind_grads(self, grads):
+        self._look()                                      # the order of the weights is the gradients'
+        return super().bind_grads(grads)
 
     def step(self, grads, info=None, lr=None, stream=None):
         """One step.  info: what grad_norm returned (its factor multiplies the gradients, and nothing is changed if it counted
         non-finite elements).  lr: a number, or one float32 on the device, in place of the optimizer's."""
-        g = grads if type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype else self.bind_grads(grads)
+        self._look()
+        g = grads if self._is_bound(grads) else GradNorm.bind_grads(self, grads)
         d_lr = None
         if lr is None:
             lr = self.lr
@@ -761,27 +801,24 @@ class AdamW(GradNorm):
             d_lr, lr = lr, 0.0
         if info is not None:
             _check(info, self.torch.float32, 4, self.device, "info")
-        s = self._current_stream() if stream is None else self._record(stream, [info, d_lr, *self._all(g)])
+        s = self._current_stream() if stream is None else self._record(stream, [info, d_lr, *g.tensors, *self._own])
         rc = self._lib.co3_adamw_step(self.handle, self._weights, g.address, self._copies, self._state_p, lr,
                                       None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_step")
 
-    def _all(self, g):
-        state = [self.m, self.v] if self.state_bits == 32 else [self.m, self.v, self.m_exp, self.v_exp]
-        return g.tensors + self.params.tensors + (self.copies.tensors if self.copies else []) + state
-
     def state_values(self, m_out=None, v_out=None, stream=None):
         """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""
         if m_out is None or v_out is None:
             m_out, v_out = (self._empty((self.n_blocks, STATE_BLOCK), self.torch.bfloat16, stream) for _ in range(2))
+        self._look()
         n, kind = self.n_blocks * STATE_BLOCK, m_out.dtype
         _check(m_out, kind, n, self.device, "m_out")
         _check(v_out, kind, n, self.device, "v_out")
         if stream is None:
             s = self._current_stream()
         else:
-            s = self._record(stream, [m_out, v_out, *([self.m, self.v, self.m_exp, self.v_exp] if self.state_bits == 8 else [])])
+            s = self._record(stream, [m_out, v_out, *self._moments.values()])
         rc = self._lib.co3_adamw_values(self.handle, self._state_p, m_out.data_ptr(), v_out.data_ptr(), _type_code(kind), s)
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_values")

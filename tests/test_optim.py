@@ -844,3 +844,23 @@ def test_outputs_for_another_stream_take_no_memory_that_is_still_in_use(binding)
     torch.cuda.synchronize()
     assert all((x == 3.0).all() for x in copies)
     assert info[1].item() == 1024.0 and (m > 0.09).all() and (v > 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_weights_that_are_given_other_storage(binding, bits):
+    """`p.data = x` between two steps: the second one updates x, and the old storage is left alone."""
+    p = [torch.nn.Parameter(torch.ones(700, device="cuda")), torch.nn.Parameter(torch.ones(9, device="cuda"))]
+    g = [torch.full((700,), 0.5, device="cuda"), torch.full((9,), -0.5, device="cuda")]
+    opt = binding.AdamW(p, lr=0.1, weight_decay=0.0, state_bits=bits)
+    bound = opt.bind_grads(g)
+    opt.step(bound)
+    old, kept, m = p[0].detach(), p[0].detach().clone(), opt.m
+    p[0].data = torch.full((700,), 5.0, device="cuda")
+    opt.m = m.clone()
+    before = m.clone()
+    opt.step(bound)
+    assert torch.equal(old, kept) and torch.equal(m, before) and not torch.equal(opt.m, before)
+    # gradients that do not change: an update of lr, but for the rounding of 8-bit moments (a first moment's by an eighth, a root's by 15 %)
+    for x, want in ((p[0], 4.9), (p[1], 1.2)):
+        assert ((x.detach() - want).abs() < (0.05 if bits == 8 else 1e-5)).all()

@@ -182,3 +182,73 @@ def test_a_new_optimizer_s_moments_are_zero_for_every_stream(host):
     host.events.clear()
     b.AdamW([torch.ones(300)], state=dict(m=opt.m, v=opt.v))
     assert host.events == []
+
+
+def pointers(address, n):
+    return list((C.c_void_p * n).from_address(address))
+
+
+def test_weights_copies_and_moments_that_are_given_other_storage(host):
+    """Each step takes them where they are then, not where they were when the optimizer was made."""
+    p, q = torch.nn.Parameter(torch.ones(300)), torch.nn.Parameter(torch.ones(5))
+    copies = [torch.zeros(300, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.bfloat16)]
+    opt = b.AdamW([p, q], copies=copies)
+    grads = opt.bind_grads([torch.ones(300), torch.ones(5)])
+    seen = host.library.steps
+    kept = []                                            # so that no storage can come back at its old place
+
+    def step():
+        opt.step(grads)
+        weights, _, c, state = seen[-1]
+        m, v = (C.c_void_p * 2).from_address(state)
+        assert pointers(weights, 2) == [p.data_ptr(), q.data_ptr()] and pointers(c, 2) == [c.data_ptr() for c in copies]
+        assert (m, v) == (opt.m.data_ptr(), opt.v.data_ptr())
+    step()
+    for change in (lambda: setattr(p, "data", torch.zeros(300)), lambda: setattr(copies[1], "data", torch.ones(5, dtype=torch.bfloat16)),
+                   lambda: setattr(opt, "m", torch.ones(3, 256)), lambda: opt.v.set_(torch.ones(3, 256))):
+        before = [t.data_ptr() for t in (p, q, *copies, opt.m, opt.v)]
+        kept.append([t.detach() for t in (p, q, *copies, opt.m, opt.v)])
+        change()
+        assert before != [t.data_ptr() for t in (p, q, *copies, opt.m, opt.v)]
+        step()
+    n = len(seen)
+    for word, change, back in (("300 elements", lambda: setattr(p, "data", torch.zeros(299)), lambda: setattr(p, "data", torch.zeros(300))),
+                               ("one piece", lambda: setattr(q, "data", torch.zeros(10)[::2]), lambda: setattr(q, "data", torch.zeros(5)))):
+        change()
+        with pytest.raises(ValueError, match=word):
+            opt.step(grads)
+        assert len(seen) == n
+        back()
+    step()
+    with pytest.raises(ValueError, match="v: 768"):
+        opt.v = torch.zeros(2, 256)
+    step()
+    with pytest.raises(AttributeError):
+        opt.m_exp
+
+
+def test_gradients_bound_before_weights_took_another_order_are_looked_at_again(host):
+    p = torch.nn.Parameter(torch.ones(4, 3, 2, 2))
+    opt = b.AdamW([p])
+    g = torch.ones(4, 3, 2, 2)
+    bound = opt.bind_grads([g])
+    opt.step(bound)
+    p.data = torch.ones(4, 3, 2, 2).contiguous(memory_format=torch.channels_last)
+    with pytest.raises(ValueError, match="another order"):
+        opt.step(bound)
+    bound = opt.bind_grads([g.contiguous(memory_format=torch.channels_last)])
+    opt.step(bound)
+    assert len(host.library.steps) == 2
+
+
+def test_values_of_moments_that_are_given_other_storage(host, monkeypatch):
+    opt = b.AdamW([torch.ones(300)], state_bits=8)
+    seen = []
+    monkeypatch.setattr(Library, "co3_adamw_values", lambda self, h, state, *rest: seen.append(pointers(state, 4)) or b.OK, raising=False)
+    for name in ("m", "v", "m_exp", "v_exp"):
+        setattr(opt, name, getattr(opt, name).clone())
+        opt.state_values()
+        assert seen[-1] == [getattr(opt, k).data_ptr() for k in ("m", "v", "m_exp", "v_exp")]
+    opt.m.set_(opt.m.clone())
+    opt.state_values()
+    assert seen[-1][0] == opt.m.data_ptr()
