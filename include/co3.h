@@ -391,9 +391,11 @@ int co3_moments_static(const float* grad, const float* residual, int64_t n, floa
  *
  * Tensors.  Weights, gradients and copies are given by one device pointer per tensor in host arrays, which are read
  * before the call returns; the pointers may change from call to call and need only the alignment of their type, so
- * the segments of a gradient row serve as they are.  Tensors may be empty.  The moments are one array each: tensor l
- * starts at a multiple of 256 elements (the sum over the tensors before it of their sizes rounded up to 256), and
- * places that belong to no element are neither read nor written, except that the 8-bit forms read them.
+ * the segments of a gradient row serve as they are.  Tensors may be empty.  What a step writes (weights, copies and
+ * moments) must not share memory with anything else of the call; the library does not look for that, the Python
+ * binding does among these three.  The moments are one array each: tensor l starts at a multiple of 256 elements (the
+ * sum over the tensors before it of their sizes rounded up to 256), and places that belong to no element are neither
+ * read nor written, except that the 8-bit forms read them.
  *
  * 8-bit moments (state_bits = 8).  Codes of one byte, and per block of 256 elements of a tensor the exponent `top` of
  * its largest magnitude, stored as a 32-bit float stores its own (at least 17 for m, 33 for v).

@@ -591,6 +591,14 @@ def _order(t):
     return None if t.is_contiguous() else tuple((n, st) for n, st in zip(t.shape, t.stride()) if n != 1)
 
 
+def _refuse_shared(arrays):
+    """arrays: (name, tensor) of all that a step writes, each in one piece of memory; raises if two of them share some."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name) for name, t in arrays if t.numel())
+    for (_, end, a), (begin, _, b) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError(f"{a} and {b} share memory")
+
+
 class TensorList:
     """Tensors of one dtype whose pointers have been looked at and put into a host array once (GradNorm.bind_grads).  It keeps
     the tensors; bind again after giving one of them other storage."""
@@ -730,7 +738,8 @@ def _moment(name):
 
 class AdamW(GradNorm):
     """AdamW over the tensors `params` (float32 or bfloat16, on the current CUDA device, updated in place; any dense order of
-    dimensions, gradients and copies in the same).  copies: tensors of bfloat16 or float16 that receive the new float32 weights.
+    dimensions, gradients and copies in the same).  copies: tensors of bfloat16 or float16 that receive the new float32 weights.  No
+    two of these share memory: a tensor that a model uses in two places is given once.
     weight_decay: one number, or one per tensor.  state_bits: 32, or 8 for moments of one byte each (include/co3.h).
     The moments are the attributes m, v (and m_exp, v_exp): [n_blocks][256]; `state` gives existing ones (set_steps then sets the
     steps that they come from).  Weights, copies and moments may be given other storage between two steps (`p.data = x`, `opt.m = x`);
@@ -771,6 +780,8 @@ class AdamW(GradNorm):
             copies = TensorList(copies, self.sizes, self._copy_dtype, self.device, "copies", order)
         for k, shape in self._shapes.items():
             _check(moments[k], self._kind, int(np.prod(shape)), self.device, k)
+        _refuse_shared([*((f"weights {i}", t) for i, t in enumerate(weights.tensors)),
+                        *((f"copies {i}", t) for i, t in enumerate(copies.tensors if copies else [])), *moments.items()])
         self.params, self.copies, self._moments, self._order = weights, copies, moments, order
         self._state = AdamwState(*[moments[k].data_ptr() if k in moments else None for k in ("m", "v", "m_exp", "v_exp")])
         self._state_p = C.addressof(self._state)

@@ -252,3 +252,30 @@ def test_values_of_moments_that_are_given_other_storage(host, monkeypatch):
     opt.m.set_(opt.m.clone())
     opt.state_values()
     assert seen[-1][0] == opt.m.data_ptr()
+
+
+def test_tensors_that_share_memory_are_refused(host):
+    """Two warps would write the same elements."""
+    row = torch.ones(1000)
+    half = torch.zeros(1000, dtype=torch.bfloat16)
+    for params, copies, word in (([row, row], None, "weights 0 and weights 1"), ([row[:600], row[500:]], None, "weights 0 and weights 1"),
+                                 ([row[500:], torch.ones(3), row[:501]], None, "weights 2 and weights 0"),
+                                 ([row[:500], row[500:]], [half[:500], half[499:999]], "copies 0 and copies 1"),
+                                 ([row[:500]], [row[250:500].view(torch.bfloat16)], "weights 0 and copies 0")):
+        with pytest.raises(ValueError, match=word):
+            b.AdamW(params, copies=copies)
+    m, e = torch.zeros(4, 256, dtype=torch.uint8), torch.zeros(4, dtype=torch.uint8)
+    for state, word in ((dict(m=m, v=m, m_exp=e, v_exp=e.clone()), "m and v"), (dict(m=m, v=m.clone(), m_exp=e, v_exp=e), "m_exp and v_exp")):
+        with pytest.raises(ValueError, match=word):
+            b.AdamW([row], state_bits=8, state=state)
+    with pytest.raises(ValueError, match="weights 0 and m"):
+        big = torch.zeros(4, 256)
+        b.AdamW([big.view(-1)[:1000]], state=dict(m=big, v=torch.zeros(4, 256)))
+    # neighbours, empty tensors anywhere, and gradients that share memory with one another are fine
+    opt = b.AdamW([row[:500], row[500:], row[200:200], row[0:0]])
+    opt.step([row.clone()[:500]] * 2 + [row[0:0]] * 2)
+    with pytest.raises(ValueError, match="m and v"):
+        opt.v = opt.m
+    opt.params.tensors[1].data = row[:500]
+    with pytest.raises(ValueError, match="weights 0 and weights 1"):
+        opt.step([row.clone()[:500]] * 2 + [row[0:0]] * 2)
