@@ -631,6 +631,7 @@ class GradNorm:
     def _create(self, sizes, weight_dtype, grad_dtype, copy_dtype, state_bits, betas, eps, weight_decay, seed, device=None):
         import torch
         self.torch, self.sizes, self.grad_dtype = torch, sizes, grad_dtype
+        self._increment_version = torch.autograd.graph.increment_version
         self._order = None
         n = np.ascontiguousarray(sizes, np.int64)
         per_tensor = None if np.ndim(weight_decay) == 0 else np.ascontiguousarray(weight_decay, np.float32)
@@ -789,6 +790,9 @@ class AdamW(GradNorm):
         self._own = weights.tensors + (copies.tensors if copies else []) + list(moments.values())
         self._at = [t.data_ptr() for t in self._own]
         self._data_ptr = self.torch.Tensor.data_ptr
+        # what autograd is told of after a step: weights and copies, and of the views of one tensor, which share its counter, only one
+        bases = [t._base if t._is_view() else t for t in weights.tensors + (copies.tensors if copies else [])]
+        self._written = list({id(t): t for t in bases}.values())
 
     def _look(self):
         """A program may have given one of them other storage since, and what they had may be somebody else's by now."""
@@ -817,6 +821,7 @@ class AdamW(GradNorm):
                                       None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_step")
+        self._increment_version(self._written)
 
     def state_values(self, m_out=None, v_out=None, stream=None):
         """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""

@@ -110,7 +110,7 @@ class Library:
     """The library with the fake runtime; `steps` has the arguments of each co3_adamw_step."""
 
     def __init__(self, L):
-        self.L, self.steps = L, []
+        self.L, self.steps, self.co3_strerror = L, [], b.lib().co3_strerror
         for name in b.EXPORTS:
             if "adamw" in name or name == "co3_grad_norm":
                 getattr(L, name).restype, getattr(L, name).argtypes = getattr(b.lib(), name).restype, getattr(b.lib(), name).argtypes
@@ -279,3 +279,31 @@ def test_tensors_that_share_memory_are_refused(host):
     opt.params.tensors[1].data = row[:500]
     with pytest.raises(ValueError, match="weights 0 and weights 1"):
         opt.step([row.clone()[:500]] * 2 + [row[0:0]] * 2)
+
+
+def test_autograd_sees_that_a_step_changed_weights_and_copies(host):
+    p, row = torch.nn.Parameter(torch.ones(300)), torch.ones(600)
+    copies = [torch.ones(300, dtype=torch.bfloat16), torch.ones(300, dtype=torch.bfloat16), torch.ones(300, dtype=torch.bfloat16)]
+    opt = b.AdamW([p, row[:300], row[300:]], copies=copies)
+    bound = opt.bind_grads([torch.ones(300)] * 3)
+    x = torch.ones(300, requires_grad=True)
+    losses = [(x * p).sum(), (x * row[:300]).sum(), (x * copies[2].float()).sum(), (x.bfloat16() * copies[2]).sum()]
+    before = [p._version, row._version, copies[0]._version]
+    opt.step(bound)
+    assert all(now > then for now, then in zip([p._version, row._version, copies[0]._version], before))
+    for loss, stale in zip(losses, (True, True, False, True)):
+        if stale:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+        else:
+            loss.backward()
+    p.data = torch.ones(300)
+    before = p._version
+    opt.step(bound)
+    assert p._version > before
+    with pytest.raises(b.Co3Error):
+        opt.step(bound, lr=float("nan"))
+    assert p._version == before + 1
+    with torch.inference_mode():                         # has no counter
+        w = torch.ones(5)
+    b.AdamW([w]).step([torch.ones(5)])
