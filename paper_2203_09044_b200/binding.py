@@ -824,11 +824,12 @@ class AdamW(GradNorm):
         self._increment_version(self._written)
 
     def state_values(self, m_out=None, v_out=None, stream=None):
-        """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if not given)."""
-        if m_out is None or v_out is None:
-            m_out, v_out = (self._empty((self.n_blocks, STATE_BLOCK), self.torch.bfloat16, stream) for _ in range(2))
+        """What the 8-bit moments stand for, [n_blocks][256] each, in float32 or bfloat16 (exact in both; bfloat16 if neither is
+        given)."""
+        given = m_out if m_out is not None else v_out
+        n, kind = self.n_blocks * STATE_BLOCK, self.torch.bfloat16 if given is None else given.dtype
+        m_out, v_out = (self._empty((self.n_blocks, STATE_BLOCK), kind, stream) if t is None else t for t in (m_out, v_out))
         self._look()
-        n, kind = self.n_blocks * STATE_BLOCK, m_out.dtype
         _check(m_out, kind, n, self.device, "m_out")
         _check(v_out, kind, n, self.device, "v_out")
         if stream is None:

@@ -307,3 +307,19 @@ def test_autograd_sees_that_a_step_changed_weights_and_copies(host):
     with torch.inference_mode():                         # has no counter
         w = torch.ones(5)
     b.AdamW([w]).step([torch.ones(5)])
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_values_go_to_the_one_output_that_is_given(host, monkeypatch, kind):
+    """... and the other is made to match it."""
+    opt = b.AdamW([torch.ones(300)], state_bits=8)
+    seen = []
+    monkeypatch.setattr(Library, "co3_adamw_values", lambda self, h, state, m, v, code, s: seen.append((m, v, code)) or b.OK, raising=False)
+    mine = torch.zeros(opt.n_blocks, 256, dtype=kind)
+    for which in (0, 1):
+        out = opt.state_values(**{("m_out", "v_out")[which]: mine})
+        assert out[which] is mine and out[1 - which] is not mine and out[1 - which].dtype == kind and out[1 - which].shape == mine.shape
+        assert seen[-1] == (out[0].data_ptr(), out[1].data_ptr(), b._type_code(kind))
+    assert [t.dtype for t in opt.state_values()] == [torch.bfloat16] * 2
+    with pytest.raises(ValueError, match="v_out"):
+        opt.state_values(mine, mine.view(torch.int16 if kind == torch.bfloat16 else torch.int32))
