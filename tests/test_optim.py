@@ -864,3 +864,120 @@ def test_weights_that_are_given_other_storage(binding, bits):
     # gradients that do not change: an update of lr, but for the rounding of 8-bit moments (a first moment's by an eighth, a root's by 15 %)
     for x, want in ((p[0], 4.9), (p[1], 1.2)):
         assert ((x.detach() - want).abs() < (0.05 if bits == 8 else 1e-5)).all()
+
+
+# ---- sets large enough that each warp takes several blocks ----------------------------------------------------------------------
+# A thread block has 8 warps and one block of 256 for each at least; what comes after it (the loads one block ahead, the two stages in
+# turn, a tensor's border inside a thread block's blocks, their exponents) needs more: 2 to 16 blocks a warp here, fewer in the least.
+LARGE = {
+    "1.6M": [700_000, 255, 700, 130_007, 2048, 1, 513, 377_781, 4096, 65_537, 0, 300_000, 7, 3000, 20_003],
+    "7.6M": [2_700_000, 255, 700, 430_007, 2048, 1, 513, 1_377_781, 4096, 65_537, 0, 1_900_000, 7, 3000, 1_120_003],
+    "19.2M": [6_000_000, 255, 700, 1_300_007, 2048, 1, 513, 3_777_781, 4096, 65_537, 0, 4_500_000, 7, 3000, 3_500_003],
+}
+
+
+class LargeReference:
+    """The formula on the device, elementary operations only: the moments' products and sums one by one in 32 bits, all else in 64."""
+
+    def __init__(self, sizes, bits, betas, eps, seed):
+        self.sizes, self.bits, self.betas, self.eps, self.seed, self.t = sizes, bits, betas, eps, seed, 0
+        nb = [(n + 255) // 256 for n in sizes]
+        self.owner = torch.repeat_interleave(torch.arange(len(sizes), device="cuda"), torch.tensor(nb, device="cuda"))
+        begin = np.concatenate([[0], np.cumsum(nb)])[:-1] * 256
+        self.at = [slice(int(b), int(b) + n) for b, n in zip(begin, sizes)]
+        self.m, self.v = (torch.zeros(sum(nb), 256, device="cuda") for _ in range(2))
+        self.codes = None
+
+    def blocks(self, tensors):
+        out = torch.zeros(self.m.numel(), device="cuda")
+        for at, x in zip(self.at, tensors):
+            out[at] = x.float()
+        return out.view(-1, 256)
+
+    @staticmethod
+    def value(code, top, field, signed):
+        c = code.long()
+        mag = c & 127 if signed else c
+        e = mag >> 3
+        n = torch.where(e > 0, 8 + (mag & 7), mag & 7).double()
+        x = n * torch.exp2((e.clamp(min=1) - 1 + top.long()[:, None] - 127 - field - 2).double())
+        return torch.where(c > 127, -x, x) if signed else x
+
+    @staticmethod
+    def code(x, rand, field, signed):
+        a = x.abs().double()
+        top = (x.abs().amax(1).view(torch.int32) >> 23).clamp(min=field + 3).long()
+        least = (top - 127 - field + 1)[:, None]
+        octave = torch.maximum(torch.frexp(torch.where(a > 0, a, 1e-300))[1].long() - 1, least)
+        steps = (a * torch.exp2((23 - octave).double())).round().long()
+        code = (octave - least) * 8 + ((steps + rand) >> 20)
+        code = torch.where(x < 0, code + 128, code) if signed else torch.maximum(code, (x > 0).long())
+        return code.to(torch.uint8), top.to(torch.uint8)
+
+    def step(self, weights, grads, factor, lr, decay):
+        """New weights in 64 bits, their tolerance, the random bits; blocks each."""
+        self.t += 1
+        b1, b2 = self.betas
+        if self.bits == 8 and self.codes is not None:
+            self.m, self.v = (self.value(c, t, f, s).float() for c, t, f, s in ((*self.codes[:2], M_FIELD, True), (*self.codes[2:], V_FIELD, False)))
+        g = self.blocks(grads) * torch.tensor(factor, device="cuda")
+        self.m = self.m * float(f32(b1)) + g * float(f32(1.0 - b1))
+        self.v = self.v * float(f32(b2)) + (g * g) * float(f32(1.0 - b2))
+        w, d = self.blocks(weights).double(), lr * torch.tensor(decay, device="cuda", dtype=torch.float64)[self.owner][:, None]
+        upd = lr * (self.m.double() / (1 - b1 ** self.t)) / (torch.sqrt(self.v.double() / (1 - b2 ** self.t)) + self.eps)
+        new = w - (d * w + upd)
+        tol = 2.0 ** -23 * new.abs() + 2.0 ** -20 * (upd.abs() + (d * w).abs()) + 1e-44
+        p = torch.arange(self.m.numel(), device="cuda").view(-1, 256)
+        s = (mix32((mix32(self.seed) + self.t) & 0xFFFFFFFF) + p * 0x9E3779B9) & 0xFFFFFFFF
+        rand = ((s ^ (s >> 15)) * 0x2C1B3C6D) & 0xFFFFFFFF
+        if self.bits == 8:
+            self.codes = (*self.code(self.m, rand & 0xFFFFF, M_FIELD, True), *self.code(self.v, rand >> 12, V_FIELD, False))
+        return new, tol, rand
+
+
+def spread(sizes, dtype, gen, apart, scale):
+    """Tensors each at a multiple of 256 elements, or back to back from an odd one."""
+    at, out = 0 if apart else 1, []
+    buf = torch.randn(sum(n + 255 for n in sizes) + 64, generator=gen, device="cuda").mul_(scale).to(dtype)
+    for n in sizes:
+        out.append(buf[at:at + n])
+        at += (n + 255) // 256 * 256 if apart else n
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("apart", [True, False])
+@pytest.mark.parametrize("weight,grad,copy", [("f32", "f32", None), ("bf16", "bf16", None), ("f32", "bf16", "bf16"), ("f32", "f16", "f16"), ("bf16", "f32", None)])
+@pytest.mark.parametrize("name", list(LARGE))
+def test_step_over_large_sets(binding, name, weight, grad, copy, apart, bits):
+    sizes, lr, seed = LARGE[name], 1e-2, 21
+    gen = torch.Generator(device="cuda").manual_seed(len(name) + bits)
+    params = spread(sizes, DT[weight], gen, apart, 0.05)
+    copies = None if copy is None else spread(sizes, DT[copy], gen, apart, 1.0)
+    decay = [0.1 * (i % 3) for i in range(len(sizes))]
+    opt = binding.AdamW(params, grad_dtype=DT[grad], copies=copies, lr=lr, weight_decay=decay, state_bits=bits, seed=seed)
+    ref = LargeReference(sizes, bits, (0.9, 0.999), 1e-8, seed)
+    inside = ref.blocks([torch.ones(n, device="cuda") for n in sizes]) > 0
+    info = torch.tensor([0.5, 0, 0, 0], device="cuda")
+    for t in range(3):
+        grads = spread(sizes, DT[grad], gen, apart, 10.0 ** -t)
+        before = [p.clone() for p in params]
+        opt.step(grads, info)
+        new, tol, rand = ref.step(before, grads, 0.5, lr, np.array(decay, f32).astype(np.float64))
+        if bits == 8:
+            for got, want, what in zip((opt.m, opt.m_exp, opt.v, opt.v_exp), ref.codes, ("m", "m_exp", "v", "v_exp")):
+                assert torch.equal(got, want), f"t={t} {what}"
+        else:
+            assert torch.equal(opt.m.view(torch.int32), ref.m.view(torch.int32)) and torch.equal(opt.v.view(torch.int32), ref.v.view(torch.int32)), f"t={t}"
+        got = ref.blocks(params)
+        if weight == "bf16":                              # as in run_steps
+            r = (rand >> 10 & 0xFFFF).int()
+            a, b = (((x.float().view(torch.int32) + r) & -65536).view(torch.float32) for x in (new - tol, new + tol))
+            ok = (got >= torch.minimum(a, b)) & (got <= torch.maximum(a, b))
+        else:
+            ok = (got.double() - new).abs() <= tol
+        assert (ok | ~inside).all(), f"t={t} weights"
+        if copies is not None:
+            assert all(torch.equal(c, p.to(DT[copy])) for c, p in zip(copies, params)), f"t={t} copies"
+    assert opt.status() == (0, 0, 0) and opt.steps() == 3
