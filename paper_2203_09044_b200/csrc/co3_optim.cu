@@ -584,6 +584,8 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
     } else if (__any_sync(0xffffffffu, other || v_max >= __float_as_uint(V_LIMIT))) {
         return false;
     }
+    // The lanes have read the stage and the block's exponents, which are overwritten below: the votes above order no memory.
+    if (STAGED<BITS, ANY>) __syncwarp();
     uint32_t r[PER_LANE];
     if (BITS == 8 || W16) {
 #pragma unroll
