@@ -398,7 +398,7 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
                 else reinterpret_cast<float*>(pw)[i] = w[k];
             }
         } else {
-            ++kept;                                       // never one of the places past n: their moments are 0
+            kept += i < n;                                // (with a factor that is not finite the places past n are no numbers either)
         }
         if (i < n) {
             if (a.copy_type == CO3_BF16) reinterpret_cast<__nv_bfloat16*>(p.copy)[place + i] = __float2bfloat16_rn(w[k]);

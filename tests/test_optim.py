@@ -981,3 +981,16 @@ def test_step_over_large_sets(binding, name, weight, grad, copy, apart, bits):
         if copies is not None:
             assert all(torch.equal(c, p.to(DT[copy])) for c, p in zip(copies, params)), f"t={t} copies"
     assert opt.status() == (0, 0, 0) and opt.steps() == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("n", [5, 256, 261])
+@pytest.mark.parametrize("factor", [float("inf"), float("nan")])
+def test_elements_left_out_are_counted_within_the_tensors(binding, bits, n, factor):
+    """A factor that is not finite leaves every element out, and no place past a tensor's end counts (0 times infinity is no number)."""
+    p, g = torch.ones(n, device="cuda"), torch.full((n,), 0.5, device="cuda")
+    opt = binding.AdamW([p], state_bits=bits)
+    opt.step([g], torch.tensor([factor, 0, 0, 0], device="cuda"))
+    assert opt.status() == (binding.FLAG_NONFINITE, n, 0)
+    assert (p == 1).all() and not opt.m.any() and not opt.v.any()
