@@ -386,7 +386,8 @@ int co3_moments_static(const float* grad, const float* residual, int64_t n, floa
  *   w <- w - lr (decay_l w + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
  * where t counts the steps from 1.  Each product and sum of the two moments is rounded to 32 bits by itself, so the
  * moments are the same bits wherever an element lies.  An element whose new v would not be below 2^126 (a gradient
- * that is not finite, or beyond 1e19) keeps w, m and v, is counted, and raises CO3_FLAG_NONFINITE in
+ * that is not finite, or beyond 1e19) keeps w, m and v (8-bit ones are rounded again, like any other value, if the
+ * largest of their block has grown and the grid with it), is counted, and raises CO3_FLAG_NONFINITE in
  * co3_adamw_status.  If info->nonfinite is not 0 the whole step is left out and not counted as one: nothing changes.
  *
  * Tensors.  Weights, gradients and copies are given by one device pointer per tensor in host arrays, which are read

@@ -994,3 +994,33 @@ def test_elements_left_out_are_counted_within_the_tensors(binding, bits, n, fact
     opt.step([g], torch.tensor([factor, 0, 0, 0], device="cuda"))
     assert opt.status() == (binding.FLAG_NONFINITE, n, 0)
     assert (p == 1).all() and not opt.m.any() and not opt.v.any()
+
+
+@pytest.mark.gpu
+def test_elements_left_out_of_a_step_share_their_block_s_exponents(binding):
+    """8-bit moments of an element that a step leaves out: the same values where its block's largest did not grow, and where it did, one
+    of the two neighbours on the coarser grid."""
+    n, bad = 512, [3, 300]
+    p, g = torch.ones(n, device="cuda"), torch.linspace(0.5, 1.0, n, device="cuda")
+    opt = binding.AdamW([p], state_bits=8, lr=0.1)
+    opt.step([g])
+    w, (m, v) = p.clone(), opt.state_values()
+    quiet = torch.zeros(n, device="cuda")
+    quiet[bad] = float("inf")
+    opt.step([quiet])
+    m1, v1 = opt.state_values()
+    for x, y in ((w, p), (m.view(-1), m1.view(-1)), (v.view(-1), v1.view(-1))):
+        assert torch.equal(x[bad], y[bad])
+    assert not torch.equal(m, m1)
+    loud = quiet.clone()
+    loud[[100, 400]] = 3e4
+    opt.step([loud])
+    m2, v2 = opt.state_values()
+    assert torch.equal(w[bad], p[bad])
+    # first moments of 0.05 to 0.1 beside one of 3000: the top is 2^11, the smallest steps 2^(11-16); second ones of 3e-4 to 1e-3 beside
+    # 9e5: the top is 2^19, the smallest steps 2^(19-32), and none goes to zero
+    for x, y, step in ((m1, m2, 2.0 ** -5), (v1, v2, 2.0 ** -13)):
+        x, y = x.view(-1)[bad].double(), y.view(-1)[bad].double()
+        assert ((x - y).abs() <= step).all() and (y % step == 0).all()
+    assert m1.view(-1)[3] != m2.view(-1)[3] and (v2.view(-1)[bad] > 0).all()
+    assert opt.status()[1] == 4
