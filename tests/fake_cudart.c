@@ -35,6 +35,8 @@ static int carry_out(void) {
 
 /* ---- for the tests ---- */
 int fake_waiting(void) { return n_waiting; }
+static void* allocated;
+void* fake_allocated(void) { return allocated; }           /* the last allocation of device memory */
 int fake_launches(void) { return launches; }
 int fake_calls(void) { return calls; }                     /* that wait or touch device memory */
 long fake_written(void) { long n = (long)written; written = 0; return n; }
@@ -47,7 +49,7 @@ void fake_advance(void) { advance_next = 1; }
 int cudaGetDevice(int* d) { *d = device; return SUCCESS; }
 int cudaDeviceGetAttribute(int* v, int what, int d) { (void)d; *v = what == MULTIPROCESSORS ? 148 : 0; return SUCCESS; }
 int cudaGetLastError(void) { return SUCCESS; }
-int cudaMalloc(void** p, size_t n) { *p = NULL; if (posix_memalign(p, 256, n ? n : 256)) return 2; memset(*p, 0xA5, n); return SUCCESS; }
+int cudaMalloc(void** p, size_t n) { *p = NULL; if (posix_memalign(p, 256, n ? n : 256)) return 2; allocated = memset(*p, 0xA5, n); return SUCCESS; }
 int cudaFree(void* p) { carry_out(); free(p); return SUCCESS; }
 int cudaMemset(void* p, int value, size_t n) { ++calls; return add(p, NULL, value, n); }
 int cudaMemcpy(void* to, const void* from, size_t n, int kind) {

@@ -4,6 +4,7 @@ import contextlib
 import ctypes as C
 import os
 import subprocess
+import time
 import types
 
 import numpy as np
@@ -31,6 +32,7 @@ def fake(tmp_path_factory):
     L.co3_adamw_steps_export.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
     L.co3_adamw_steps_import.argtypes = [C.c_void_p, C.c_int64]
     L.fake_written.restype = C.c_long
+    L.fake_allocated.restype = C.c_void_p
     return L
 
 
@@ -100,6 +102,30 @@ def test_setting_the_steps_leaves_the_status(fake):
         fake.fake_written()
         assert h.set_steps(3) == b.OK
         assert fake.fake_written() <= 40                # count, two powers, two corrections, key
+
+
+@pytest.mark.parametrize("betas", [(0.9, 0.999), (0.5, 0.75), (0.0, 0.3), (0.99, 0.0), (1.0 - 2.0 ** -53, 0.9999)])
+def test_set_steps_leaves_the_powers_that_the_steps_would_have(fake, betas):
+    """Products of 64 bits one after the other, to the last subnormal one and beyond."""
+    with Handle(fake, betas=betas) as h:
+        at = fake.fake_allocated()                        # count, then the two powers
+        powers, t = [1.0, 1.0], 0
+        for stop in (0, 1, 7, 60, 1074, 1080, 7200, 760_000, 1_000_001):
+            while t < stop:
+                powers = [powers[0] * betas[0], powers[1] * betas[1]]
+                t += 1
+            assert h.set_steps(stop) == b.OK
+            assert C.c_int64.from_address(at).value == stop
+            assert [x.hex() for x in (C.c_double * 2).from_address(at + 8)] == [x.hex() for x in powers], stop
+
+
+def test_set_steps_far_into_a_run_is_quick(fake):
+    """The powers of usual betas stop at a subnormal number that a product no longer changes: 6 s of products of such for 2^26 steps if
+    one goes on, 2 ms until then."""
+    with Handle(fake) as h:
+        begin = time.process_time()
+        assert h.set_steps(1 << 26) == b.OK
+        assert time.process_time() - begin < 1.0
 
 
 # ---- the Python binding, with tensors of the host in the place of the device's ----------------------------------------------
