@@ -428,7 +428,8 @@ typedef struct {
     int32_t copy_type;    /* CO3_BF16 / CO3_F16: f32 weights are also written in that type; else CO3_NONE    */
     int32_t state_bits;   /* 32 or 8                                                                         */
     double beta1, beta2;  /* in [0, 1)                                                                       */
-    double eps, weight_decay;
+    double eps;           /* 0, or 1.2e-38 / sqrt(1 - beta2) to 2^126: what 32 bits can work with               */
+    double weight_decay;  /* >= 0                                                                            */
     uint32_t seed;        /* of the stochastic rounding                                                      */
     int32_t reserved;     /* 0                                                                               */
 } co3_adamw_config;

@@ -1160,7 +1160,10 @@ extern "C" int co3_adamw_create(co3_adamw** out, const co3_adamw_config* cfg) {
     if (cfg->copy_type != CO3_NONE && cfg->weight_type != CO3_F32) return CO3_EINVAL;
     if (cfg->state_bits != 32 && cfg->state_bits != 8) return CO3_EINVAL;
     if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return CO3_EINVAL;
-    if (!(cfg->eps >= 0.0 && cfg->eps < INFINITY) || !(cfg->weight_decay >= 0.0 && cfg->weight_decay < INFINITY)) return CO3_EINVAL;
+    // eps times a bias correction, which is sqrt(1 - beta2) at least, has to be a normal number of 32 bits where it is not 0, and no
+    // denominator may pass 2^126, where the kernels' quotients end.
+    if (!(cfg->eps == 0.0 || (cfg->eps * sqrt(1.0 - cfg->beta2) >= 0x1p-126 && cfg->eps <= 0x1p126))) return CO3_EINVAL;
+    if (!(cfg->weight_decay >= 0.0 && (float)cfg->weight_decay < INFINITY)) return CO3_EINVAL;
     int64_t blocks = 0, elements = 0;
     for (int t = 0; t < n; ++t) {
         if (cfg->sizes[t] < 0 || cfg->sizes[t] > ((int64_t)1 << 40)) return CO3_EINVAL;
@@ -1265,7 +1268,7 @@ extern "C" int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_
 
 extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* const* grads, void* const* copies, const co3_adamw_state* state,
                               double lr, const float* d_lr, const co3_grad_info* info, void* cuda_stream) {
-    if (!h || !weights || !grads || !state || !(fabs(lr) < INFINITY)) return CO3_EINVAL;
+    if (!h || !weights || !grads || !state || !(fabsf((float)lr) < INFINITY)) return CO3_EINVAL;
     if ((copies != nullptr) != (h->copy_type != CO3_NONE)) return CO3_EINVAL;
     if (((uintptr_t)info & 15) || ((uintptr_t)d_lr & 3)) return CO3_EINVAL;
     if (h->n_blocks) {

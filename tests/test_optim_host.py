@@ -39,11 +39,11 @@ def fake(tmp_path_factory):
 class Handle:
     """A handle of the library with the fake runtime."""
 
-    def __init__(self, L, sizes=(1000, 5), betas=(0.9, 0.999), eps=1e-8):
+    def __init__(self, L, sizes=(1000, 5), betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, expect=b.OK):
         n = np.array(sizes, np.int64)
-        cfg = b.AdamwConfig(len(n), n.ctypes.data_as(C.POINTER(C.c_int64)), None, b.F32, b.F32, b.NONE, 32, betas[0], betas[1], eps, 0.0, 0, 0)
+        cfg = b.AdamwConfig(len(n), n.ctypes.data_as(C.POINTER(C.c_int64)), None, b.F32, b.F32, b.NONE, 32, betas[0], betas[1], eps, weight_decay, 0, 0)
         self.L, self.h = L, C.c_void_p()
-        assert L.co3_adamw_create(C.byref(self.h), C.byref(cfg)) == b.OK
+        assert L.co3_adamw_create(C.byref(self.h), C.byref(cfg)) == expect
 
     def __enter__(self):
         return self
@@ -126,6 +126,18 @@ def test_set_steps_far_into_a_run_is_quick(fake):
         begin = time.process_time()
         assert h.set_steps(1 << 26) == b.OK
         assert time.process_time() - begin < 1.0
+
+
+def test_numbers_that_32_bits_cannot_hold_are_refused(fake):
+    """An eps that would be zero there makes 0 / 0 of an element without a gradient, a learning rate or decay that would be infinite no
+    numbers of all weights."""
+    least = 2.0 ** -126
+    for kw in (dict(eps=1e-50), dict(eps=1e39), dict(eps=2.0 ** 126 * 1.001), dict(eps=least / 1.001, betas=(0.9, 0.0)), dict(eps=least * 9.9, betas=(0.9, 0.99)),
+               dict(weight_decay=1e39)):
+        Handle(fake, expect=b.EINVAL, **kw)
+    for kw in (dict(eps=0.0), dict(eps=least, betas=(0.9, 0.0)), dict(eps=least * 10.1, betas=(0.9, 0.99)), dict(eps=1e-30), dict(eps=2.0 ** 126), dict(weight_decay=1e38)):
+        with Handle(fake, **kw):
+            pass
 
 
 # ---- the Python binding, with tensors of the host in the place of the device's ----------------------------------------------
@@ -349,3 +361,13 @@ def test_values_go_to_the_one_output_that_is_given(host, monkeypatch, kind):
     assert [t.dtype for t in opt.state_values()] == [torch.bfloat16] * 2
     with pytest.raises(ValueError, match="v_out"):
         opt.state_values(mine, mine.view(torch.int16 if kind == torch.bfloat16 else torch.int32))
+
+
+def test_a_learning_rate_that_32_bits_cannot_hold_is_refused(host):
+    opt = b.AdamW([torch.ones(300)])
+    for lr in (1e39, -1e39, float("inf"), float("nan")):
+        with pytest.raises(b.Co3Error) as e:
+            opt.step([torch.ones(300)], lr=lr)
+        assert e.value.code == b.EINVAL
+    for lr in (1e38, -1e38, 0.0):
+        opt.step([torch.ones(300)], lr=lr)
