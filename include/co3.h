@@ -451,7 +451,7 @@ void co3_adamw_destroy(co3_adamw* h);
 int co3_adamw_sizes(const co3_adamw* h, int64_t* n_blocks, int64_t* n_elements);
 
 /* L2 norm of all gradients together, of the finite elements: norm = |grad_scale| sqrt(sum g^2), and what the step is to
- * multiply them by: factor = grad_scale min(1, max_norm / norm), or grad_scale if max_norm <= 0.  nonfinite counts the
+ * multiply them by: factor = grad_scale min(1, max_norm / norm), or grad_scale if max_norm <= 0 or infinite.  nonfinite counts the
  * elements that are infinite or NaN.  tensor_norms: device [n_tensors] f32 or NULL, the same norm per tensor.
  * Squares are formed without overflow or underflow for every finite gradient and summed in 64 bits in a fixed order:
  * the same gradients give the same bits. */

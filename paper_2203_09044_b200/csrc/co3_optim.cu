@@ -1244,7 +1244,7 @@ extern "C" int co3_adamw_sizes(const co3_adamw* h, int64_t* n_blocks, int64_t* n
 extern "C" int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_scale, float max_norm, float* tensor_norms, co3_grad_info* info,
                              void* cuda_stream) {
     if (!h || !grads || !info || ((uintptr_t)info & 15) || ((uintptr_t)tensor_norms & 3)) return CO3_EINVAL;
-    if (!(fabsf(grad_scale) < INFINITY) || !(max_norm < INFINITY)) return CO3_EINVAL;
+    if (!(fabsf(grad_scale) < INFINITY) || isnan(max_norm)) return CO3_EINVAL;
     if (!on_device(h)) return CO3_EINVAL;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (!pointers_fine(h, grads, nullptr, nullptr)) return CO3_EINVAL;

@@ -1024,3 +1024,13 @@ def test_elements_left_out_of_a_step_share_their_block_s_exponents(binding):
         assert ((x - y).abs() <= step).all() and (y % step == 0).all()
     assert m1.view(-1)[3] != m2.view(-1)[3] and (v2.view(-1)[bad] > 0).all()
     assert opt.status()[1] == 4
+
+
+@pytest.mark.gpu
+def test_an_infinite_bound_clips_nothing(binding):
+    g = [torch.full((100,), 3.0, device="cuda")]
+    info = binding.GradNorm([100]).grad_norm(g, max_norm=float("inf"), grad_scale=0.5)
+    assert info[:2].tolist() == [0.5, 15.0]
+    for bad in (float("nan"), -float("nan")):
+        with pytest.raises(binding.Co3Error):
+            binding.GradNorm([100]).grad_norm(g, max_norm=bad)
