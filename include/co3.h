@@ -451,10 +451,13 @@ void co3_adamw_destroy(co3_adamw* h);
 int co3_adamw_sizes(const co3_adamw* h, int64_t* n_blocks, int64_t* n_elements);
 
 /* L2 norm of all gradients together, of the finite elements: norm = |grad_scale| sqrt(sum g^2), and what the step is to
- * multiply them by: factor = grad_scale min(1, max_norm / norm), or grad_scale if max_norm <= 0 or infinite.  nonfinite counts the
- * elements that are infinite or NaN.  tensor_norms: device [n_tensors] f32 or NULL, the same norm per tensor.
- * Squares are formed without overflow or underflow for every finite gradient and summed in 64 bits in a fixed order:
- * the same gradients give the same bits. */
+ * multiply them by: factor = grad_scale min(1, max_norm / norm), or grad_scale if max_norm <= 0 or infinite.  nonfinite
+ * counts the elements that are infinite or NaN.  tensor_norms: device [n_tensors] f32 or NULL, the same norm per tensor.
+ * No square overflows for any finite gradient, and none underflows that would count.  Squares are summed in 64 bits, of
+ * 16-bit elements two neighbours in 32 bits before.  The order depends on the sizes, the type and on which gradients
+ * begin on a multiple of 32 bytes (f32) or 16 (the others), on nothing else: alike in these, the same gradients give the
+ * same bits; at other addresses the norms agree to 2^-22 and the factors, and moments with them, may differ in their last
+ * bits. */
 int co3_grad_norm(co3_adamw* h, const void* const* grads, float grad_scale, float max_norm, float* tensor_norms,
                   co3_grad_info* info, void* cuda_stream);
 

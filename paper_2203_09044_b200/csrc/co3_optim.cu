@@ -793,7 +793,8 @@ __device__ __forceinline__ T block_sum(T x, T* sh) {      // same value in every
 
 // The square of a 32-bit float is exact in 64 bits: no range is lost, and the sum rounds at 2^-53.  The conversions (16 a clock on an
 // SM) would bind with 16-bit elements: the squares of those are exact in 32 bits too, so that two of them are added there, with
-// one rounding, where all of a lane's eight are of a size that leaves their squares in range.
+// one rounding, where the largest of a lane's eight has a square well within the range (one that underflows beside it, below 2^-149
+// against 2^-100, would not change the sum in 32 bits).  Which two are neighbours in a lane depends on how the gradient is loaded.
 template <class G>
 __device__ __forceinline__ void add_squares(const float* x, double& s0, double& s1, uint32_t& bad) {
     uint32_t top = 0;

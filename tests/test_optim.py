@@ -1034,3 +1034,29 @@ def test_an_infinite_bound_clips_nothing(binding):
     for bad in (float("nan"), -float("nan")):
         with pytest.raises(binding.Co3Error):
             binding.GradNorm([100]).grad_norm(g, max_norm=bad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,whole", [("bf16", 8), ("f16", 8), ("f32", 8)])
+def test_norm_at_other_addresses(binding, dtype, whole):
+    """The same bits at addresses alike to the header's rule.  At others: pairs of squares with one rounding of 2^-24 each, which the
+    root halves, and the norm's own rounding of 2^-24, on either side: 3 * 2^-24 between them."""
+    sizes = [256, 700, 2048, 5000] * 80
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    data = [torch.randn(n, generator=gen, device="cuda").to(DT[dtype]) for n in sizes]
+    opt = binding.GradNorm(sizes, DT[dtype])
+
+    def norms(places):                                    # of each tensor in turn, in elements past a multiple of `whole`
+        buf = torch.zeros(sum(n + 4 * whole for n in sizes), dtype=DT[dtype], device="cuda")
+        at, grads = 0, []
+        for i, x in enumerate(data):
+            at = -(-at // whole) * whole + places[i % len(places)]
+            grads.append(buf[at:at + x.numel()])
+            grads[-1].copy_(x)
+            at += x.numel()
+        out = torch.empty(len(sizes), device="cuda")
+        info = opt.grad_norm(grads, max_norm=1.0, tensor_norms=out)
+        return torch.cat([out, info[:2]])
+    on, off = norms([0]), norms([1])
+    assert torch.equal(norms([whole, 0, 2 * whole]), on) and torch.equal(norms([3, 5, whole + 1, 2]), off)
+    assert ((on.double() - off.double()).abs() <= 3 * 2.0 ** -24 * on.double()).all()
