@@ -265,6 +265,23 @@ def test_weights_copies_and_moments_that_are_given_other_storage(host):
         opt.m_exp
 
 
+def test_views_of_a_row_that_is_given_other_memory(host):
+    """One of them is looked at, for all have the row's storage."""
+    row, other = torch.ones(1000), torch.nn.Parameter(torch.ones(4))
+    opt = b.AdamW([row[:300], other, row[300:900], row[900:]])
+    grads = opt.bind_grads([torch.ones(n) for n in (300, 4, 600, 100)])
+    seen, kept = host.library.steps, []
+    assert len(opt._watched) == 4 and len(opt._written) == 2          # the row, the other one, two moments
+    for change in (lambda: None, lambda: row.untyped_storage().resize_(1 << 20), lambda: setattr(other, "data", torch.zeros(4))):
+        kept.append((row.clone(), other.detach()))
+        change()
+        opt.step(grads)
+        assert pointers(seen[-1][0], 4) == [row.data_ptr(), other.data_ptr(), row[300:].data_ptr(), row[900:].data_ptr()]
+    version = row._version
+    opt.step(grads)
+    assert row._version == version + 1
+
+
 def test_gradients_bound_before_weights_took_another_order_are_looked_at_again(host):
     p = torch.nn.Parameter(torch.ones(4, 3, 2, 2))
     opt = b.AdamW([p])
@@ -314,9 +331,11 @@ def test_tensors_that_share_memory_are_refused(host):
     opt.step([row.clone()[:500]] * 2 + [row[0:0]] * 2)
     with pytest.raises(ValueError, match="m and v"):
         opt.v = opt.m
-    opt.params.tensors[1].data = row[:500]
+    p = [torch.nn.Parameter(torch.ones(500)) for _ in range(2)]
+    opt = b.AdamW(p)
+    p[1].data = p[0].data
     with pytest.raises(ValueError, match="weights 0 and weights 1"):
-        opt.step([row.clone()[:500]] * 2 + [row[0:0]] * 2)
+        opt.step([row[:500]] * 2)
 
 
 def test_autograd_sees_that_a_step_changed_weights_and_copies(host):
