@@ -1060,3 +1060,10 @@ def test_norm_at_other_addresses(binding, dtype, whole):
     on, off = norms([0]), norms([1])
     assert torch.equal(norms([whole, 0, 2 * whole]), on) and torch.equal(norms([3, 5, whole + 1, 2]), off)
     assert ((on.double() - off.double()).abs() <= 3 * 2.0 ** -24 * on.double()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("n", [63, 64, 65, 159, 160, 161])
+def test_pointers_with_the_launch_and_by_way_of_the_table(binding, bits, n):
+    run_steps(binding, [1 + 37 * i % 300 for i in range(n)], bits, factor=0.5, steps=2)
