@@ -603,7 +603,7 @@ class TensorList:
     """Tensors of one dtype whose pointers have been looked at and put into a host array once (GradNorm.bind_grads).  It keeps
     the tensors; bind again after giving one of them other storage."""
 
-    def __init__(self, tensors, sizes, dtype, device, what, order=None):
+    def __init__(self, tensors, sizes, dtype, device, what, order=None, fits=None):
         self.tensors = list(tensors)
         if len(self.tensors) != len(sizes):
             raise ValueError(f"{len(sizes)} {what} expected, got {len(self.tensors)}")
@@ -617,7 +617,7 @@ class TensorList:
             if order is not None and n and _order(t) != order[i]:
                 raise ValueError(f"{what} {i}: its elements lie in another order than those of its weights")
         self.pointers = (C.c_void_p * len(sizes))(*[t.data_ptr() if n else None for t, n in zip(self.tensors, sizes)])
-        self.address, self.sizes, self.dtype, self.order = C.addressof(self.pointers), sizes, dtype, order
+        self.address, self.fits = C.addressof(self.pointers), fits
 
 
 class GradNorm:
@@ -631,8 +631,9 @@ class GradNorm:
     def _create(self, sizes, weight_dtype, grad_dtype, copy_dtype, state_bits, betas, eps, weight_decay, seed, device=None):
         import torch
         self.torch, self.sizes, self.grad_dtype = torch, sizes, grad_dtype
-        self._increment_version = torch.autograd.graph.increment_version
-        self._order = None
+        self._increment_version = torch._C._increment_version          # torch.autograd.graph.increment_version of a list
+        self._data_ptr, self._float32 = torch.Tensor.data_ptr, torch.float32
+        self._order, self._fits = None, object()          # the second goes into every list that was looked at by this object, in this order
         n = np.ascontiguousarray(sizes, np.int64)
         per_tensor = None if np.ndim(weight_decay) == 0 else np.ascontiguousarray(weight_decay, np.float32)
         if per_tensor is not None and per_tensor.shape != n.shape:
@@ -687,16 +688,12 @@ class GradNorm:
         optimizer's bind_grads returned is checked again.)"""
         if type(grads) is TensorList:
             grads = grads.tensors
-        return TensorList(grads, self.sizes, self.grad_dtype, self.device, "gradients", self._order)
-
-    def _is_bound(self, grads):
-        """Whether bind_grads of this object returned `grads`."""
-        return type(grads) is TensorList and grads.sizes is self.sizes and grads.dtype is self.grad_dtype and grads.order is self._order
+        return TensorList(grads, self.sizes, self.grad_dtype, self.device, "gradients", self._order, self._fits)
 
     def grad_norm(self, grads, info=None, max_norm=0.0, grad_scale=1.0, tensor_norms=None, stream=None):
         """grads: the tensors, or what bind_grads returned.  info: 4 float32 on the device, written and returned: factor, norm,
         and in the last two the count of non-finite elements as one int64 (`info[2:].view(torch.int64)`)."""
-        g = grads if self._is_bound(grads) else self.bind_grads(grads)
+        g = grads if type(grads) is TensorList and grads.fits is self._fits else self.bind_grads(grads)
         if info is None:
             info = self._empty(4, self.torch.float32, stream)
         _check(info, self.torch.float32, 4, self.device, "info")
@@ -722,7 +719,7 @@ class GradNorm:
 
 
 def _check(t, dtype, n, device, what):
-    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous {dtype} on {device} expected, got {t.numel()} {t.dtype} on {t.device}")
 
 
@@ -776,14 +773,14 @@ class AdamW(GradNorm):
         """Look at weights, copies and moments and keep where they are; nothing changes if one does not fit."""
         weights = TensorList(params, self.sizes, self._dtype, self.device, "weights")
         order = [_order(p) for p in weights.tensors]
-        if order == self._order:
-            order = self._order                           # gradients bound by it stay bound
         if copies is not None:
             copies = TensorList(copies, self.sizes, self._copy_dtype, self.device, "copies", order)
         for k, shape in self._shapes.items():
             _check(moments[k], self._kind, int(np.prod(shape)), self.device, k)
         _refuse_shared([*((f"weights {i}", t) for i, t in enumerate(weights.tensors)),
                         *((f"copies {i}", t) for i, t in enumerate(copies.tensors if copies else [])), *moments.items()])
+        if order != self._order:
+            self._fits = object()                         # gradients bound so far are looked at again
         self.params, self.copies, self._moments, self._order = weights, copies, moments, order
         self._state = AdamwState(*[moments[k].data_ptr() if k in moments else None for k in ("m", "v", "m_exp", "v_exp")])
         self._state_p = C.addressof(self._state)
@@ -796,30 +793,32 @@ class AdamW(GradNorm):
         self._watched = list({id(base): t for base, t in zip(bases, self._own)}.values())
         self._written = list({id(base): t for base, t in zip(bases, written)}.values())
         self._at = [t.data_ptr() for t in self._watched]
-        self._data_ptr = self.torch.Tensor.data_ptr
+        self._moments_list = list(moments.values())
+        self._moments_at = [t.data_ptr() for t in self._moments_list]
 
-    def _look(self):
-        """A program may have given one of them other storage since, and what they had may be somebody else's by now."""
-        if [*map(self._data_ptr, self._watched)] != self._at:
-            self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, self._moments)
+    def _rebind(self):
+        """A program has given one of them other storage since, and what it had may be somebody else's by now."""
+        self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, self._moments)
 
     def bind_grads(self, grads):
-        self._look()                                      # the order of the weights is the gradients'
+        if [*map(self._data_ptr, self._watched)] != self._at:
+            self._rebind()                                # the order of the weights is the gradients'
         return super().bind_grads(grads)
 
     def step(self, grads, info=None, lr=None, stream=None):
         """One step.  info: what grad_norm returned (its factor multiplies the gradients, and nothing is changed if it counted
         non-finite elements).  lr: a number, or one float32 on the device, in place of the optimizer's."""
-        self._look()
-        g = grads if self._is_bound(grads) else GradNorm.bind_grads(self, grads)
+        if [*map(self._data_ptr, self._watched)] != self._at:
+            self._rebind()
+        g = grads if type(grads) is TensorList and grads.fits is self._fits else GradNorm.bind_grads(self, grads)
         d_lr = None
         if lr is None:
             lr = self.lr
         elif isinstance(lr, self.torch.Tensor):
-            _check(lr, self.torch.float32, 1, self.device, "lr")
+            _check(lr, self._float32, 1, self.device, "lr")
             d_lr, lr = lr, 0.0
         if info is not None:
-            _check(info, self.torch.float32, 4, self.device, "info")
+            _check(info, self._float32, 4, self.device, "info")
         s = self._current_stream() if stream is None else self._record(stream, [info, d_lr, *g.tensors, *self._own])
         rc = self._lib.co3_adamw_step(self.handle, self._weights, g.address, self._copies, self._state_p, lr,
                                       None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
@@ -832,8 +831,12 @@ class AdamW(GradNorm):
         given)."""
         given = m_out if m_out is not None else v_out
         n, kind = self.n_blocks * STATE_BLOCK, self.torch.bfloat16 if given is None else given.dtype
-        m_out, v_out = (self._empty((self.n_blocks, STATE_BLOCK), kind, stream) if t is None else t for t in (m_out, v_out))
-        self._look()
+        if m_out is None:
+            m_out = self._empty((self.n_blocks, STATE_BLOCK), kind, stream)
+        if v_out is None:
+            v_out = self._empty((self.n_blocks, STATE_BLOCK), kind, stream)
+        if [*map(self._data_ptr, self._moments_list)] != self._moments_at:
+            self._rebind()
         _check(m_out, kind, n, self.device, "m_out")
         _check(v_out, kind, n, self.device, "v_out")
         if stream is None:
