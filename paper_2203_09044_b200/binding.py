@@ -720,14 +720,18 @@ class GradNorm:
 
 def _check(t, dtype, n, device, what):
     if t.dtype is not dtype or t.numel() != n or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: {n} contiguous {dtype} on {device} expected, got {t.numel()} {t.dtype} on {t.device}")
+        _refuse(t, dtype, n, device, what)
+
+
+def _refuse(t, dtype, n, device, what):
+    raise ValueError(f"{what}: {n} contiguous {dtype} on {device} expected, got {t.numel()} {t.dtype} on {t.device}")
 
 
 def _moment(name):
     def get(self):
         if name not in self._moments:
             raise AttributeError(name)
-        return self._moments[name]
+        return self._moments[name].detach()               # the optimizer's own is nobody else's, to be given other storage
 
     def put(self, tensor):
         self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, {**self._moments, name: tensor})
@@ -777,6 +781,7 @@ class AdamW(GradNorm):
             copies = TensorList(copies, self.sizes, self._copy_dtype, self.device, "copies", order)
         for k, shape in self._shapes.items():
             _check(moments[k], self._kind, int(np.prod(shape)), self.device, k)
+        moments = {k: moments[k].detach() for k in self._shapes}
         _refuse_shared([*((f"weights {i}", t) for i, t in enumerate(weights.tensors)),
                         *((f"copies {i}", t) for i, t in enumerate(copies.tensors if copies else [])), *moments.items()])
         if order != self._order:
@@ -789,26 +794,23 @@ class AdamW(GradNorm):
         self._own = written + list(moments.values())
         # Of the views of one tensor only one is looked at before a step, and one version counter moved after it: they share both memory and
         # counter, and a row in hundreds of pieces costs no more than one tensor (290 pieces 0.3 us, 290 tensors of their own 26).
-        bases = [t._base if t._is_view() else t for t in self._own]
-        self._watched = list({id(base): t for base, t in zip(bases, self._own)}.values())
+        bases = [t._base if t._is_view() else t for t in written]
         self._written = list({id(base): t for base, t in zip(bases, written)}.values())
-        self._at = [t.data_ptr() for t in self._watched]
-        self._moments_list = list(moments.values())
-        self._moments_at = [t.data_ptr() for t in self._moments_list]
+        self._at = [t.data_ptr() for t in self._written]
 
     def _rebind(self):
-        """A program has given one of them other storage since, and what it had may be somebody else's by now."""
+        """A program has given a weight or copy other storage since, and what it had may be somebody else's by now."""
         self._bind_own(self.params.tensors, self.copies.tensors if self.copies else None, self._moments)
 
     def bind_grads(self, grads):
-        if [*map(self._data_ptr, self._watched)] != self._at:
+        if [*map(self._data_ptr, self._written)] != self._at:
             self._rebind()                                # the order of the weights is the gradients'
         return super().bind_grads(grads)
 
     def step(self, grads, info=None, lr=None, stream=None):
         """One step.  info: what grad_norm returned (its factor multiplies the gradients, and nothing is changed if it counted
         non-finite elements).  lr: a number, or one float32 on the device, in place of the optimizer's."""
-        if [*map(self._data_ptr, self._watched)] != self._at:
+        if [*map(self._data_ptr, self._written)] != self._at:
             self._rebind()
         g = grads if type(grads) is TensorList and grads.fits is self._fits else GradNorm.bind_grads(self, grads)
         d_lr = None
@@ -817,8 +819,8 @@ class AdamW(GradNorm):
         elif isinstance(lr, self.torch.Tensor):
             _check(lr, self._float32, 1, self.device, "lr")
             d_lr, lr = lr, 0.0
-        if info is not None:
-            _check(info, self._float32, 4, self.device, "info")
+        if info is not None and (info.dtype is not self._float32 or info.numel() != 4 or info.device != self.device or not info.is_contiguous()):
+            _refuse(info, self._float32, 4, self.device, "info")
         s = self._current_stream() if stream is None else self._record(stream, [info, d_lr, *g.tensors, *self._own])
         rc = self._lib.co3_adamw_step(self.handle, self._weights, g.address, self._copies, self._state_p, lr,
                                       None if d_lr is None else d_lr.data_ptr(), None if info is None else info.data_ptr(), s)
@@ -835,8 +837,6 @@ class AdamW(GradNorm):
             m_out = self._empty((self.n_blocks, STATE_BLOCK), kind, stream)
         if v_out is None:
             v_out = self._empty((self.n_blocks, STATE_BLOCK), kind, stream)
-        if [*map(self._data_ptr, self._moments_list)] != self._moments_at:
-            self._rebind()
         _check(m_out, kind, n, self.device, "m_out")
         _check(v_out, kind, n, self.device, "v_out")
         if stream is None:

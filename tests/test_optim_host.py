@@ -243,7 +243,7 @@ def test_weights_copies_and_moments_that_are_given_other_storage(host):
         assert (m, v) == (opt.m.data_ptr(), opt.v.data_ptr())
     step()
     for change in (lambda: setattr(p, "data", torch.zeros(300)), lambda: setattr(copies[1], "data", torch.ones(5, dtype=torch.bfloat16)),
-                   lambda: setattr(opt, "m", torch.ones(3, 256)), lambda: opt.v.set_(torch.ones(3, 256))):
+                   lambda: setattr(opt, "m", torch.ones(3, 256)), lambda: setattr(opt, "v", torch.ones(3, 256))):
         before = [t.data_ptr() for t in (p, q, *copies, opt.m, opt.v)]
         kept.append([t.detach() for t in (p, q, *copies, opt.m, opt.v)])
         change()
@@ -263,6 +263,18 @@ def test_weights_copies_and_moments_that_are_given_other_storage(host):
     step()
     with pytest.raises(AttributeError):
         opt.m_exp
+    before = opt.m.data_ptr(), opt.v.data_ptr()          # what one reads is not the optimizer's own object
+    opt.m.set_(torch.ones(3, 256))
+    opt.v.data = torch.ones(3, 256)
+    assert (opt.m.data_ptr(), opt.v.data_ptr()) == before
+    step()
+    given = dict(m=torch.ones(3, 256), v=torch.ones(3, 256))
+    kept.append([t.detach() for t in given.values()])
+    opt = b.AdamW([p, q], copies=copies, state=given)
+    grads = opt.bind_grads([torch.ones(300), torch.ones(5)])
+    given["m"].set_(torch.ones(3, 256))
+    assert opt.m.data_ptr() == kept[-1][0].data_ptr() and opt.v.data_ptr() == given["v"].data_ptr()
+    step()
 
 
 def test_views_of_a_row_that_is_given_other_memory(host):
@@ -271,7 +283,7 @@ def test_views_of_a_row_that_is_given_other_memory(host):
     opt = b.AdamW([row[:300], other, row[300:900], row[900:]])
     grads = opt.bind_grads([torch.ones(n) for n in (300, 4, 600, 100)])
     seen, kept = host.library.steps, []
-    assert len(opt._watched) == 4 and len(opt._written) == 2          # the row, the other one, two moments
+    assert len(opt._written) == 2                        # the row and the other one
     for change in (lambda: None, lambda: row.untyped_storage().resize_(1 << 20), lambda: setattr(other, "data", torch.zeros(4))):
         kept.append((row.clone(), other.detach()))
         change()
@@ -306,7 +318,7 @@ def test_values_of_moments_that_are_given_other_storage(host, monkeypatch):
         assert seen[-1] == [getattr(opt, k).data_ptr() for k in ("m", "v", "m_exp", "v_exp")]
     opt.m.set_(opt.m.clone())
     opt.state_values()
-    assert seen[-1][0] == opt.m.data_ptr()
+    assert seen[-1][0] == opt.m.data_ptr() == seen[-2][0]
 
 
 def test_tensors_that_share_memory_are_refused(host):
