@@ -742,7 +742,8 @@ class AdamW(GradNorm):
     """AdamW over the tensors `params` (float32 or bfloat16, on the current CUDA device, updated in place; any dense order of
     dimensions, gradients and copies in the same).  copies: tensors of bfloat16 or float16 that receive the new float32 weights.  No
     two of these share memory: a tensor that a model uses in two places is given once.
-    weight_decay: one number, or one per tensor.  state_bits: 32, or 8 for moments of one byte each (include/co3.h).
+    weight_decay: one number, or one per tensor.  state_bits: 32, or 8 for moments of one byte each (include/co3.h).  An eps below
+    about 6e-11 makes steps slower (ditto).
     The moments are the attributes m, v (and m_exp, v_exp): [n_blocks][256]; `state` gives existing ones (set_steps then sets the
     steps that they come from).  Weights, copies and moments may be given other storage between two steps (`p.data = x`, `opt.m = x`;
     a view stands for its part of the tensor that it is a view of, whatever becomes of the view); a captured step keeps what it was
