@@ -432,7 +432,7 @@ typedef struct {
     double beta1, beta2;  /* in [0, 1)                                                                       */
     double eps;           /* 0, or 1.2e-38 / sqrt(1 - beta2) to 2^126: what 32 bits can work with.  Below 1.8e-12 /
                              sqrt(1 - beta2) (6e-11 for 0.999), and with 8-bit moments for a beta1 in (0, 2^-9), a step
-                             takes its general way: up to 1.3 times as long with 32-bit moments, 1.6 (f32) to 2.9 (bf16)
+                             takes its general way: up to 1.3 times as long with 32-bit moments, 1.5 (f32) to 2.8 (bf16)
                              times with 8-bit ones */
     double weight_decay;  /* >= 0                                                                            */
     uint32_t seed;        /* of the stochastic rounding                                                      */

@@ -405,7 +405,7 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
                 else reinterpret_cast<float*>(pw)[i] = w[k];
             }
         } else {
-            kept += i < n;                                // (with a factor that is not finite the places past n are no numbers either)
+            ++kept;
         }
         if (i < n) {
             if (a.copy_type == CO3_BF16) reinterpret_cast<__nv_bfloat16*>(p.copy)[place + i] = __float2bfloat16_rn(w[k]);
@@ -434,7 +434,8 @@ __device__ __forceinline__ uint32_t block_any(const StepArgs& a, const Step& s, 
             if (i < n) static_cast<uint8_t*>(a.v)[place + i] = (uint8_t)c;
         }
     }
-    return kept;
+    // with a factor that is not finite every element is left out, but the places past n, 0 times it, are no numbers either
+    return fabsf(s.factor) < INFINITY ? kept : (uint32_t)(n + 31 - lane) >> 5;
 }
 
 __device__ __forceinline__ float root_fast(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -1306,8 +1307,8 @@ extern "C" int co3_adamw_step(co3_adamw* h, void* const* weights, const void* co
     // block_whole takes roots of numbers below 2^-126 as 0.  Beside eps that is less than 2^-24 of the denominator if eps is above
     // 2^24 * 2^-63 / sqrt(1 - beta2) (6e-11 for beta2 = 0.999); a smaller eps takes the general way.
     // The scale of 8-bit moments (2^-117 at least) times beta1 has to stay a normal number.
-    // What the general way costs where every block takes it (67M elements, eps = 1e-15 against 1e-8): 8-bit moments, bf16 327 us against
-    // 111, f32 259 against 166; 32-bit ones, bf16 286 against 225, f32 293 against 277.
+    // What the general way costs where every block takes it (67M elements, eps = 1e-15 against 1e-8): 8-bit moments, bf16 309 us against
+    // 111, f32 247 against 166; 32-bit ones, bf16 286 against 225, f32 293 against 277.
     a.fast = h->eps * sqrt(1.0 - h->beta2) >= 0x1p-39 && (h->state_bits == 32 || h->beta1 == 0.0 || h->beta1 >= 0x1p-9);
     // Blocks of one thread block.  32-bit moments: one warp takes as many as leave every place for a thread block four of them one
     // after the other, so that the SMs end together, and at most 4 (2^28 f32: 1, 2, 4, 8, 16 take 1214, 1115, 1097, 1114, 1125 us).
