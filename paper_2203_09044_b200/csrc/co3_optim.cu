@@ -641,8 +641,8 @@ __device__ __forceinline__ bool block_whole(const StepArgs& a, const Step& s, ui
 // order of blocks, and neither way through a block, changes a bit of them.
 // 32-bit moments: 28 bytes an element (f32) against 40 instructions, so memory binds: 2^28 f32 in 1091 us, 6.9 TB/s, and 124M with bf16
 // gradient and copy in 519 us, 6.7 TB/s, both above the copy rate of 6.55.  11.2M in 62 tensors: 52 us (5.9 TB/s; it begins and ends).
-// 8-bit moments: 16 bytes (f32) or 10 (bf16) against 49 instructions, which leave the issue slots 83% busy: 2^28 f32 weights with bf16
-// gradient and copy in 667 us, 6.4 TB/s; 124M bf16 in 199 us, 6.25 TB/s, and more under the power limit, which takes clocks away.
+// 8-bit moments: 16 bytes (f32) or 10 (bf16) against 49 instructions, which leave the issue slots 81% busy: 2^28 f32 weights with bf16
+// gradient and copy in 667 us, 6.4 TB/s; 124M bf16 in 203 us, 6.15 TB/s, and more under the power limit, which takes clocks away.
 template <int BITS, class W, class G, bool ANY>
 __global__ void __launch_bounds__(32 * WARPS, STEP_CTAS<BITS>) adamw_kernel(const __grid_constant__ StepArgs a) {
     __shared__ uint8_t tops[2 * STRETCH];                 // the block exponents of the first moments, then of the second
