@@ -485,6 +485,109 @@ int co3_adamw_steps_export(co3_adamw* h, int64_t* steps);
 int co3_adamw_steps_import(co3_adamw* h, int64_t steps);
 int64_t co3_adamw_launch_count(const co3_adamw* h);
 
+/* ---- The two ends of a language model ----------------------------------------------------------------------
+ * (No counterpart in the paper.)  Operators whose backward pass reduces over tokens, for models whose gradients the calls above encode:
+ * embedding lookup, layer norm, and losses over a large vocabulary.  A batch is [n_users][n_tokens]; every user has weight gradients
+ * of its own, written into that user's row of a gradient array.
+ *
+ * Each handle belongs to the device that was current when it was made and owns its scratch (one allocation); later calls allocate
+ * nothing, only enqueue kernels and may be captured into a graph and replayed.  Calls on one handle share its scratch: they are issued on
+ * one stream, or ordered by the caller, graphs that were captured from the same handle among them.  Each call needs the handle's device to
+ * be current.  Outputs must not share memory with anything else of the call.  Sums have a fixed order: the same inputs in the same layout
+ * give the same bits.
+ *
+ * Tokens are whole numbers of 32 or 64 bits.  One below zero is no token (the places behind the end of a shorter sequence): nothing that lies
+ * in its place is read into a result.  One that the vocabulary does not have counts as none, and is counted and raises CO3_FLAG_TOKEN in
+ * the handle's status. */
+#define CO3_I32 3
+#define CO3_I64 4
+#define CO3_FLAG_TOKEN 32u /* a token number at or beyond the vocabulary was met */
+
+typedef struct {          /* device, [users][tokens][dim], elements of a row side by side, strides in elements */
+    void* data;           /* aligned as its type                                                              */
+    int32_t type;         /* CO3_F32, CO3_BF16, CO3_F16                                                       */
+    int32_t reserved;     /* 0                                                                                */
+    int64_t user_stride, token_stride;
+} co3_array;
+
+typedef struct {          /* device, [users][tokens][top], strides in elements, entries of a token side by side   */
+    const void* data;
+    int32_t type;         /* CO3_I32 or CO3_I64                                                               */
+    int32_t top;          /* entries of a token: 1 but for a teacher's                                        */
+    int64_t user_stride, token_stride;
+} co3_tokens;
+
+typedef struct {          /* device, gradient of a weight: [users] pieces, user_stride elements apart (a segment of [U][ld] rows) */
+    void* data;           /* aligned as its type                                                              */
+    int32_t type;         /* CO3_F32, CO3_BF16, CO3_F16                                                       */
+    int32_t accumulate;   /* 0: written; 1: added to what is there                                            */
+    int64_t user_stride;
+} co3_param_grad;
+
+/* Embedding.  out[u][t] = scale table[token[u][t]], 0 where there is no token; dtable[u][v] = scale times the sum of dout[u][t] over the
+ * tokens of user u that are v, in 32 bits, in an order that the tokens alone fix.  The types of table, out, dout and dtable are free.
+ * table: device [vocab][dim] without gaps.  vocab, dim >= 1, below 2^31; n_tokens <= max_tokens. */
+typedef struct co3_embed co3_embed;
+int co3_embed_create(co3_embed** out, int64_t vocab, int64_t dim, int32_t n_users, int64_t max_tokens);
+void co3_embed_destroy(co3_embed* h);
+int co3_embed_forward(co3_embed* h, const co3_tokens* tokens, int64_t n_tokens, const void* table, int32_t table_type, float scale,
+                      const co3_array* out, void* cuda_stream);
+int co3_embed_backward(co3_embed* h, const co3_array* dout, const co3_tokens* tokens, int64_t n_tokens, float scale,
+                       const co3_param_grad* dtable, void* cuda_stream);
+/* Synchronises.  clear != 0 resets both. */
+int co3_embed_status(co3_embed* h, uint32_t* flags, uint64_t* bad_tokens, int32_t clear);
+int64_t co3_embed_launch_count(const co3_embed* h);
+
+/* Layer norm over the last dimension: mean and rstd = 1 / sqrt(variance + eps) of each row, in 32 bits, variance from the differences
+ * from the mean; y = (x - mean) rstd weight + bias.  Backward, with xh = (x - mean) rstd and g = weight dy:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),   dweight[u] = sum over the user's rows of dy xh,   dbias[u] = ... of dy.
+ * x, y, dy, dx have one type; weight and bias (weight_type, NULL: ones and zeros) may have another.  mean, rstd: device f32
+ * [n_users][n_tokens].  dx, dweight, dbias: NULL where not wanted.  dim from 1 to 16384.  y may be x, and dx may be dy or x, in the same
+ * layout; nothing else shares memory. */
+typedef struct co3_layernorm co3_layernorm;
+int co3_layernorm_create(co3_layernorm** out, int64_t dim, int32_t n_users, double eps);
+void co3_layernorm_destroy(co3_layernorm* h);
+int co3_layernorm_forward(co3_layernorm* h, const co3_array* x, const void* weight, const void* bias, int32_t weight_type, int64_t n_tokens,
+                          const co3_array* y, float* mean, float* rstd, void* cuda_stream);
+int co3_layernorm_backward(co3_layernorm* h, const co3_array* dy, const co3_array* x, const void* weight, int32_t weight_type, const float* mean,
+                           const float* rstd, int64_t n_tokens, const co3_array* dx, const co3_param_grad* dweight,
+                           const co3_param_grad* dbias, void* cuda_stream);
+int64_t co3_layernorm_launch_count(const co3_layernorm* h);
+
+/* Losses of a token over a large vocabulary, from the last hidden states and the weight of the last layer, without the logits
+ * z = hidden weight^T being kept: they are made in tiles that never leave the SM, and once more for the gradient, in pieces of the vocabulary.
+ *   cross entropy: targets.top = 1, teacher = NULL:   loss = lse - z_target,   lse = log sum_v exp z_v
+ *   distillation:  targets.top entries of a teacher with the logits `teacher` ([users][tokens][top], any type), temperature tau:
+ *                  q = softmax(teacher / tau) over the entries,   lse = log sum_v exp(z_v / tau),   loss = sum_k q_k (log q_k - z_k / tau + lse)
+ *                  An entry below zero is left out; one that stands twice counts twice.
+ * A token without a target (or with no entry whose teacher logit is above -infinity) has loss 0, lse 0 and no gradient, whatever its
+ * hidden state holds.
+ *   backward: c = dloss[u][t] scale (dloss NULL: scale over the number of the user's tokens that have a target, the gradient of their mean)
+ *   dz_v = c / tau (exp(z_v / tau - lse) - q_v);   dhidden = dz weight;   dweight[u] = sum over the user's tokens of dz_v hidden
+ * hidden, weight and dhidden have the handle's type (bf16 or f16: what the tensor cores take).  dz is rounded to that type before the two
+ * products; for dweight in 32 bits its remainder is carried along in a second number of that type (2^-17 of dz in bf16), which costs a
+ * second product.  Products are summed in 32 bits.  f16: dz is scaled by a power of two per user, so that none is lost below 2^-24.
+ * weight: device, vocab rows, weight_stride elements apart; its address and the stride are multiples of 16 bytes, dim is a multiple of 8.
+ * loss, lse, dloss: device f32 [n_users][n_tokens].  lse is what the forward call gave for the same inputs.  dhidden, dweight: NULL where
+ * not wanted.  top from 1 to max_top, which is at most 128. */
+typedef struct co3_token_loss co3_token_loss;
+typedef struct {
+    int64_t vocab, dim, max_tokens;
+    int32_t n_users;
+    int32_t type;         /* CO3_BF16 or CO3_F16                                                              */
+    int32_t grad_type;    /* of dweight: CO3_F32 or `type`                                                    */
+    int32_t max_top;
+} co3_token_loss_config;
+int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_config* cfg);
+void co3_token_loss_destroy(co3_token_loss* h);
+int co3_token_loss_forward(co3_token_loss* h, const co3_array* hidden, const void* weight, int64_t weight_stride, const co3_tokens* targets,
+                           const co3_array* teacher, float temperature, int64_t n_tokens, float* loss, float* lse, void* cuda_stream);
+int co3_token_loss_backward(co3_token_loss* h, const co3_array* hidden, const void* weight, int64_t weight_stride, const co3_tokens* targets,
+                            const co3_array* teacher, float temperature, int64_t n_tokens, const float* lse, const float* dloss, float scale,
+                            const co3_array* dhidden, const co3_param_grad* dweight, void* cuda_stream);
+int co3_token_loss_status(co3_token_loss* h, uint32_t* flags, uint64_t* bad_tokens, int32_t clear);
+int64_t co3_token_loss_launch_count(const co3_token_loss* h);
+
 const char* co3_strerror(int code);
 
 #ifdef __cplusplus

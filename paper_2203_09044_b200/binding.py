@@ -19,6 +19,7 @@ BIAS_CURRENT, BIAS_LAGGED, CODE_LAGGED, CODE_EMPIRICAL = 0, 1, 2, 3
 RULE_POLY, RULE_OPT = 0, 1
 FLAG_TIMEOUT = 8
 FLAG_INEXACT = 16
+FLAG_TOKEN = 32
 
 EXPORTS = [
     "co3_plan_create", "co3_plan_destroy", "co3_sizes", "co3_encode", "co3_decode_aggregate",
@@ -32,6 +33,10 @@ EXPORTS = [
     "co3_model_checksum", "co3_balanced_split",
     "co3_adamw_create", "co3_adamw_destroy", "co3_adamw_sizes", "co3_grad_norm", "co3_adamw_step", "co3_adamw_values",
     "co3_adamw_status", "co3_adamw_steps_export", "co3_adamw_steps_import", "co3_adamw_launch_count",
+    "co3_embed_create", "co3_embed_destroy", "co3_embed_forward", "co3_embed_backward", "co3_embed_status", "co3_embed_launch_count",
+    "co3_layernorm_create", "co3_layernorm_destroy", "co3_layernorm_forward", "co3_layernorm_backward", "co3_layernorm_launch_count",
+    "co3_token_loss_create", "co3_token_loss_destroy", "co3_token_loss_forward", "co3_token_loss_backward", "co3_token_loss_status",
+    "co3_token_loss_launch_count",
 ]
 ELIMIT = -7
 STATIC_MAX_ELEMENTS = 1 << 29
@@ -52,6 +57,7 @@ class Config(C.Structure):
 
 
 F32, BF16, F16, NONE = 0, 1, 2, -1
+I32, I64 = 3, 4
 STATE_BLOCK = 256          # elements of a tensor that share an exponent in 8-bit moments
 
 
@@ -64,6 +70,23 @@ class AdamwConfig(C.Structure):
 
 class AdamwState(C.Structure):
     _fields_ = [("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p)]
+
+
+class Array(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("reserved", C.c_int32), ("user_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("top", C.c_int32), ("user_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class ParamGrad(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("accumulate", C.c_int32), ("user_stride", C.c_int64)]
+
+
+class TokenLossConfig(C.Structure):
+    _fields_ = [("vocab", C.c_int64), ("dim", C.c_int64), ("max_tokens", C.c_int64), ("n_users", C.c_int32), ("type", C.c_int32),
+                ("grad_type", C.c_int32), ("max_top", C.c_int32)]
 
 
 HDR_DTYPE = np.dtype([("bias", np.int8), ("ibeta", np.int8), ("ir", np.int16)])
@@ -178,6 +201,23 @@ def lib():
     L.co3_adamw_steps_import.argtypes = [vp, C.c_int64]
     L.co3_adamw_launch_count.restype = C.c_int64
     L.co3_adamw_launch_count.argtypes = [vp]
+    arr, tok, pgrad, i64, i32, f32 = C.POINTER(Array), C.POINTER(Tokens), C.POINTER(ParamGrad), C.c_int64, C.c_int32, C.c_float
+    L.co3_embed_create.argtypes = [C.POINTER(vp), i64, i64, i32, i64]
+    L.co3_embed_forward.argtypes = [vp, tok, i64, vp, i32, f32, arr, vp]
+    L.co3_embed_backward.argtypes = [vp, arr, tok, i64, f32, pgrad, vp]
+    L.co3_layernorm_create.argtypes = [C.POINTER(vp), i64, i32, C.c_double]
+    L.co3_layernorm_forward.argtypes = [vp, arr, vp, vp, i32, i64, arr, vp, vp, vp]
+    L.co3_layernorm_backward.argtypes = [vp, arr, arr, vp, i32, vp, vp, i64, arr, pgrad, pgrad, vp]
+    L.co3_token_loss_create.argtypes = [C.POINTER(vp), C.POINTER(TokenLossConfig)]
+    L.co3_token_loss_forward.argtypes = [vp, arr, vp, i64, tok, arr, f32, i64, vp, vp, vp]
+    L.co3_token_loss_backward.argtypes = [vp, arr, vp, i64, tok, arr, f32, i64, vp, vp, f32, arr, pgrad, vp]
+    for name in ("embed", "token_loss"):
+        getattr(L, f"co3_{name}_status").argtypes = [vp, C.POINTER(C.c_uint32), C.POINTER(C.c_uint64), i32]
+    for name in ("embed", "layernorm", "token_loss"):
+        getattr(L, f"co3_{name}_destroy").restype = None
+        getattr(L, f"co3_{name}_destroy").argtypes = [vp]
+        getattr(L, f"co3_{name}_launch_count").restype = i64
+        getattr(L, f"co3_{name}_launch_count").argtypes = [vp]
     L.co3_strerror.restype = C.c_char_p
     L.co3_strerror.argtypes = [C.c_int]
     _lib = L
@@ -866,3 +906,280 @@ class AdamW(GradNorm):
         rc = lib().co3_adamw_steps_import(self.handle, int(steps))
         if rc != OK:
             raise Co3Error(rc, "co3_adamw_steps_import")
+
+
+# ---- the two ends of a language model: embedding, layer norm, losses over the vocabulary -----------------------------
+class _Operator:
+    """A handle of the library on the current CUDA device, for batches [users][tokens] (with one user also [tokens]).  The calls only enqueue
+    kernels, on the current stream or the one given, and share the handle's scratch: use one handle on one stream at a time.  They are not
+    recorded by autograd; what a call writes is marked as changed."""
+
+    _kind, _status = None, False
+    _record, _empty = staticmethod(GradNorm._record), GradNorm._empty
+
+    def _create(self, make, n_users):
+        import torch
+        self.torch, self._lib, self.n_users = torch, lib(), int(n_users)
+        self._increment_version = torch._C._increment_version
+        h = C.c_void_p()
+        rc = make(C.byref(h))
+        if rc != OK:
+            raise Co3Error(rc, f"co3_{self._kind}_create")
+        self.handle = h
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self._current_stream = functools.partial(torch._C._cuda_getCurrentRawStream, self.device.index)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            getattr(self._lib, f"co3_{self._kind}_destroy")(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def launch_count(self):
+        return int(getattr(self._lib, f"co3_{self._kind}_launch_count")(self.handle))
+
+    def _get_status(self, clear):
+        f, n = C.c_uint32(), C.c_uint64()
+        rc = getattr(self._lib, f"co3_{self._kind}_status")(self.handle, C.byref(f), C.byref(n), int(clear))
+        if rc != OK:
+            raise Co3Error(rc, f"co3_{self._kind}_status")
+        return int(f.value), int(n.value)
+
+    def _batch(self, t, dim, what, like=None):
+        """co3_array of a tensor [users][tokens][dim]; `like`: the leading sizes that it has to have."""
+        shape, strides = t.shape, t.stride()
+        if t.device != self.device:
+            raise ValueError(f"{what}: a tensor on {self.device} expected, got one on {t.device}")
+        if len(shape) == 2 and self.n_users == 1:
+            tokens, us, ts = shape[0], 0, strides[0]
+        elif len(shape) == 3 and shape[0] == self.n_users:
+            tokens, us, ts = shape[1], strides[0], strides[1]
+        else:
+            raise ValueError(f"{what}: [{self.n_users}, tokens, {dim}] expected, got {tuple(shape)}")
+        if shape[-1] != dim or (dim > 1 and strides[-1] != 1):
+            raise ValueError(f"{what}: rows of {dim} elements side by side expected, got shape {tuple(shape)}, strides {strides}")
+        if like is not None and shape[:-1] != like:
+            raise ValueError(f"{what}: {tuple(like)} rows expected, got {tuple(shape[:-1])}")
+        return Array(t.data_ptr(), _type_code(t.dtype), 0, us, ts), tokens
+
+    def _tokens(self, t, what="tokens", like=None, top=None):
+        """co3_tokens of whole numbers [users][tokens], or [users][tokens][top]."""
+        torch = self.torch
+        if t.dtype not in (torch.int32, torch.int64) or t.device != self.device:
+            raise ValueError(f"{what}: int32 or int64 on {self.device} expected, got {t.dtype} on {t.device}")
+        shape, strides = t.shape, t.stride()
+        lead = shape if top is None else shape[:-1]
+        if top is not None and (len(shape) < 2 or (top > 1 and strides[-1] != 1)):
+            raise ValueError(f"{what}: entries of a token side by side expected, got shape {tuple(shape)}, strides {strides}")
+        if len(lead) == 1 and self.n_users == 1:
+            us, ts = 0, strides[0]
+        elif len(lead) == 2 and lead[0] == self.n_users:
+            us, ts = strides[0], strides[1]
+        else:
+            raise ValueError(f"{what}: [{self.n_users}, tokens] expected, got {tuple(lead)}")
+        if like is not None and tuple(lead) != tuple(like):
+            raise ValueError(f"{what}: {tuple(like)} expected, got {tuple(lead)}")
+        return Tokens(t.data_ptr(), I32 if t.dtype == torch.int32 else I64, 1 if top is None else top, us, ts), lead
+
+    def _grad(self, t, n, accumulate, what):
+        """co3_param_grad of a tensor that holds n elements for each user, each user's in one piece."""
+        if t.device != self.device or t.numel() != self.n_users * n:
+            raise ValueError(f"{what}: {self.n_users} times {n} elements on {self.device} expected, got {tuple(t.shape)} on {t.device}")
+        shape, strides = t.shape, t.stride()
+        if self.n_users > 1 and (not shape or shape[0] != self.n_users):
+            raise ValueError(f"{what}: [{self.n_users}, ...] expected, got {tuple(shape)}")
+        at = 1
+        for size, stride in zip(reversed(shape[1:] if self.n_users > 1 else shape), reversed(strides[1:] if self.n_users > 1 else strides)):
+            if size != 1 and stride != at and n:
+                raise ValueError(f"{what}: each user's part in one piece expected, got shape {tuple(shape)}, strides {strides}")
+            at *= size
+        return ParamGrad(t.data_ptr(), _type_code(t.dtype), int(accumulate), strides[0] if self.n_users > 1 else n)
+
+    def _vector(self, t, n, what):
+        """Pointer and type of a weight of n elements, or (None, F32)."""
+        if t is None:
+            return None, F32
+        if t.numel() != n or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{what}: {n} contiguous elements on {self.device} expected, got {tuple(t.shape)} on {t.device}")
+        return t.data_ptr(), _type_code(t.dtype)
+
+    def _per_token(self, t, like, what):
+        if t.dtype is not self.torch.float32 or t.shape != like or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous float32 {tuple(like)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _done(self, rc, call, written):
+        if rc != OK:
+            raise Co3Error(rc, call)
+        self._increment_version(written)
+
+    def _on(self, stream, tensors):
+        return self._current_stream() if stream is None else self._record(stream, tensors)
+
+
+class Embedding(_Operator):
+    """Embedding lookup and its gradient (co3_embed_*).  tokens: the most that a user has in a call."""
+
+    _kind = "embed"
+
+    def __init__(self, vocab, dim, n_users=1, tokens=0):
+        self.vocab, self.dim = int(vocab), int(dim)
+        self._create(lambda h: lib().co3_embed_create(h, self.vocab, self.dim, int(n_users), int(tokens)), n_users)
+
+    def status(self, clear=False):
+        """(flags, token numbers met that the vocabulary does not have); synchronises."""
+        return self._get_status(clear)
+
+    def forward(self, tokens, table, scale=1.0, out=None, out_dtype=None, stream=None):
+        """scale * table[token], zeros where a token is below zero: [*tokens.shape, dim], in out_dtype (the table's if None)."""
+        k, lead = self._tokens(tokens)
+        if tuple(table.shape) != (self.vocab, self.dim) or not table.is_contiguous() or table.device != self.device:
+            raise ValueError(f"table: contiguous [{self.vocab}, {self.dim}] on {self.device} expected, got {tuple(table.shape)} on {table.device}")
+        if out is None:
+            out = self._empty((*lead, self.dim), out_dtype or table.dtype, stream)
+        elif out_dtype not in (None, out.dtype):
+            raise ValueError(f"out: {out_dtype} expected, got {out.dtype}")
+        o, n = self._batch(out, self.dim, "out", lead)
+        s = self._on(stream, [tokens, table, out])
+        self._done(self._lib.co3_embed_forward(self.handle, k, n, table.data_ptr(), _type_code(table.dtype), scale, o, s), "co3_embed_forward", [out])
+        return out
+
+    def backward(self, dout, tokens, dtable, scale=1.0, accumulate=False, stream=None):
+        """Gradient of the table for each user into dtable: [users, vocab * dim] or [users, vocab, dim], each user's part in one piece
+        (a segment of gradient rows)."""
+        k, lead = self._tokens(tokens)
+        g, n = self._batch(dout, self.dim, "dout", lead)
+        t = self._grad(dtable, self.vocab * self.dim, accumulate, "dtable")
+        s = self._on(stream, [dout, tokens, dtable])
+        self._done(self._lib.co3_embed_backward(self.handle, g, k, n, scale, t, s), "co3_embed_backward", [dtable])
+        return dtable
+
+
+class LayerNorm(_Operator):
+    """Layer norm over the last dimension, forward and backward (co3_layernorm_*)."""
+
+    _kind = "layernorm"
+
+    def __init__(self, dim, n_users=1, eps=1e-5):
+        self.dim, self.eps = int(dim), float(eps)
+        self._create(lambda h: lib().co3_layernorm_create(h, self.dim, int(n_users), self.eps), n_users)
+
+    def forward(self, x, weight=None, bias=None, y=None, mean=None, rstd=None, stream=None):
+        """(y, mean, rstd); y has x's type, mean and rstd are float32, one for each row."""
+        a, n = self._batch(x, self.dim, "x")
+        lead = x.shape[:-1]
+        (w, wt), (b, bt) = self._vector(weight, self.dim, "weight"), self._vector(bias, self.dim, "bias")
+        if weight is not None and bias is not None and wt != bt:
+            raise ValueError(f"weight and bias of one type expected, got {weight.dtype} and {bias.dtype}")
+        if y is None:
+            y = self._empty(x.shape, x.dtype, stream)
+        if mean is None:
+            mean = self._empty(lead, self.torch.float32, stream)
+        if rstd is None:
+            rstd = self._empty(lead, self.torch.float32, stream)
+        o, _ = self._batch(y, self.dim, "y", lead)
+        m, r = self._per_token(mean, lead, "mean"), self._per_token(rstd, lead, "rstd")
+        s = self._on(stream, [x, weight, bias, y, mean, rstd])
+        self._done(self._lib.co3_layernorm_forward(self.handle, a, w, b, wt if weight is not None else bt, n, o, m, r, s), "co3_layernorm_forward", [y, mean, rstd])
+        return y, mean, rstd
+
+    def backward(self, dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, accumulate=False, want_dx=True, stream=None):
+        """dx (None if not wanted); the users' gradients of weight and bias go into dweight and dbias ([users, dim], any float type) where
+        given."""
+        a, n = self._batch(x, self.dim, "x")
+        lead = x.shape[:-1]
+        g, _ = self._batch(dy, self.dim, "dy", lead)
+        w, wt = self._vector(weight, self.dim, "weight")
+        m, r = self._per_token(mean, lead, "mean"), self._per_token(rstd, lead, "rstd")
+        if dx is None and want_dx:
+            dx = self._empty(x.shape, x.dtype, stream)
+        o = None if dx is None else self._batch(dx, self.dim, "dx", lead)[0]
+        dw = None if dweight is None else self._grad(dweight, self.dim, accumulate, "dweight")
+        db = None if dbias is None else self._grad(dbias, self.dim, accumulate, "dbias")
+        s = self._on(stream, [dy, x, weight, mean, rstd, dx, dweight, dbias])
+        self._done(self._lib.co3_layernorm_backward(self.handle, g, a, w, wt, m, r, n, o, dw, db, s), "co3_layernorm_backward",
+                   [t for t in (dx, dweight, dbias) if t is not None])
+        return dx
+
+
+class TokenLoss(_Operator):
+    """Losses of tokens over a large vocabulary from the last hidden states, with their gradients, without the logits being kept
+    (co3_token_loss_*).  dtype: of hidden states and weight, bfloat16 or float16.  grad_dtype: of the weight's gradient, float32 or dtype.
+    tokens: the most that a user has in a call; top: the most entries that a teacher gives for a token."""
+
+    _kind = "token_loss"
+
+    def __init__(self, vocab, dim, n_users=1, tokens=0, dtype=None, grad_dtype=None, top=1):
+        import torch
+        self.vocab, self.dim, self.dtype, self.grad_dtype = int(vocab), int(dim), dtype or torch.bfloat16, grad_dtype or torch.float32
+        cfg = TokenLossConfig(self.vocab, self.dim, int(tokens), int(n_users), _type_code(self.dtype), _type_code(self.grad_dtype), int(top))
+        self._create(lambda h: lib().co3_token_loss_create(h, C.byref(cfg)), n_users)
+
+    def status(self, clear=False):
+        """(flags, target numbers met that the vocabulary does not have); synchronises."""
+        return self._get_status(clear)
+
+    def loss(self, hidden, weight, targets, loss=None, lse=None, stream=None):
+        """Cross entropy: (loss, lse), float32 like targets; 0 where a target is below zero."""
+        return self._forward(hidden, weight, targets, None, 1.0, loss, lse, stream)
+
+    def loss_grad(self, hidden, weight, targets, lse, dloss=None, scale=1.0, dhidden=None, dweight=None, accumulate=False, want_dhidden=True,
+                  stream=None):
+        """dhidden (None if not wanted); the users' gradients of the weight go into dweight where given ([users, vocab * dim], see
+        Embedding.backward).  lse: what loss() gave.  dloss: gradient of each token's loss; None: of the mean over each user's tokens
+        that have a target."""
+        return self._backward(hidden, weight, targets, None, 1.0, lse, dloss, scale, dhidden, dweight, accumulate, want_dhidden, stream)
+
+    def distill(self, hidden, weight, index, logits, temperature=1.0, loss=None, lse=None, stream=None):
+        """Divergence from a teacher's top logits: index (whole numbers) and logits [*, tokens, top]; (loss, lse) as loss()."""
+        return self._forward(hidden, weight, index, logits, temperature, loss, lse, stream)
+
+    def distill_grad(self, hidden, weight, index, logits, lse, dloss=None, temperature=1.0, scale=1.0, dhidden=None, dweight=None, accumulate=False,
+                     want_dhidden=True, stream=None):
+        return self._backward(hidden, weight, index, logits, temperature, lse, dloss, scale, dhidden, dweight, accumulate, want_dhidden, stream)
+
+    def _inputs(self, hidden, weight, targets, logits):
+        h, n = self._batch(hidden, self.dim, "hidden")
+        if hidden.dtype != self.dtype or weight.dtype != self.dtype:
+            raise TypeError(f"hidden and weight in {self.dtype} expected, got {hidden.dtype} and {weight.dtype}")
+        if tuple(weight.shape) != (self.vocab, self.dim) or weight.device != self.device or weight.stride(1) != 1:
+            raise ValueError(f"weight: rows of [{self.vocab}, {self.dim}] on {self.device} expected, got {tuple(weight.shape)}, strides {weight.stride()}, on {weight.device}")
+        lead = hidden.shape[:-1]
+        if logits is None:
+            k, _ = self._tokens(targets, "targets", lead)
+            return h, n, lead, k, None
+        k, _ = self._tokens(targets, "index", lead, targets.shape[-1] if targets.dim() else 1)
+        return h, n, lead, k, self._batch(logits, targets.shape[-1], "logits", lead)[0]
+
+    def _stride(self, weight):
+        return weight.stride(0) if self.vocab > 1 else self.dim
+
+    def _forward(self, hidden, weight, targets, logits, temperature, loss, lse, stream):
+        h, n, lead, k, t = self._inputs(hidden, weight, targets, logits)
+        if loss is None:
+            loss = self._empty(lead, self.torch.float32, stream)
+        if lse is None:
+            lse = self._empty(lead, self.torch.float32, stream)
+        p, q = self._per_token(loss, lead, "loss"), self._per_token(lse, lead, "lse")
+        s = self._on(stream, [hidden, weight, targets, logits, loss, lse])
+        self._done(self._lib.co3_token_loss_forward(self.handle, h, weight.data_ptr(), self._stride(weight), k, t, temperature, n, p, q, s),
+                   "co3_token_loss_forward", [loss, lse])
+        return loss, lse
+
+    def _backward(self, hidden, weight, targets, logits, temperature, lse, dloss, scale, dhidden, dweight, accumulate, want_dhidden, stream):
+        h, n, lead, k, t = self._inputs(hidden, weight, targets, logits)
+        p = self._per_token(lse, lead, "lse")
+        q = None if dloss is None else self._per_token(dloss, lead, "dloss")
+        if dhidden is None and want_dhidden:
+            dhidden = self._empty(hidden.shape, self.dtype, stream)
+        o = None if dhidden is None else self._batch(dhidden, self.dim, "dhidden", lead)[0]
+        w = None if dweight is None else self._grad(dweight, self.vocab * self.dim, accumulate, "dweight")
+        s = self._on(stream, [hidden, weight, targets, logits, lse, dloss, dhidden, dweight])
+        self._done(self._lib.co3_token_loss_backward(self.handle, h, weight.data_ptr(), self._stride(weight), k, t, temperature, n, p, q, scale, o, w, s),
+                   "co3_token_loss_backward", [x for x in (dhidden, dweight) if x is not None])
+        return dhidden
