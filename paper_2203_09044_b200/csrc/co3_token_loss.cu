@@ -17,13 +17,14 @@ namespace {
 
 constexpr int TILE = 256;                     // rows and columns of a pair's tile
 constexpr int KB = 64;                        // depth of a stage: 128 bytes, one swizzle span
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr int HALF_BYTES = 128 * KB * 2;      // one operand's part of a thread block and stage
 constexpr int STAGE_BYTES = 2 * HALF_BYTES;
-constexpr int GEMM_THREADS = 384;             // TMA, MMA, tensor memory, idle; eight warps for the tiles' ends
+constexpr int FIRST_EPI = 2;                  // warps: loads, products, then eight for the tiles' ends
+constexpr int GEMM_THREADS = 320;
 constexpr int EPI_WARPS = 8;
-constexpr int TRANSPOSE_BYTES = EPI_WARPS * 32 * 33 * 4;
-constexpr int GEMM_SHARED = 1024 + STAGES * STAGE_BYTES + TRANSPOSE_BYTES + 256;
+constexpr int OUT_BYTES = EPI_WARPS * 2 * 4096;          // two boxes of 32 x 128 bytes a warp, or 32 x 33 numbers
+constexpr int GEMM_SHARED = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + 256;
 constexpr int ALIGN_ROWS = 64;                // a user's packed rows begin at a multiple of these
 constexpr int MAX_TOP = 128;
 constexpr int SPAN = 128;                     // columns of one set of statistics
@@ -47,6 +48,7 @@ struct Packed {                               // what the packing leaves, on the
 
 struct GemmArgs {
     CUtensorMap a, b, a_low;                  // a_low: the remainders of dz
+    CUtensorMap out, out_low;                 // what a tile's end stores: dz and its remainder, or dweight
     Packed p;
     OpsStatus* status;
     int users, vocab, dim;
@@ -58,12 +60,10 @@ struct GemmArgs {
     float* dots;                              // [spans][rows]
     const int32_t* entry; const float* entry_q; const uint8_t* entry_first;      // [tokens][top], [tokens][top], [tokens][spans]
     int top, spans;
-    void *dz, *dz_low;
-    int64_t dz_pitch;
     float* partial;                           // [splits][rows][dim]
     int add;                                  // to what partial holds
     co3_param_grad dw;
-    int dw_wide;                              // rows of dweight begin at multiples of 16 bytes
+    int dw_wide;                              // rows of dweight begin at multiples of 16 bytes and are written
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -107,19 +107,28 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
+// 32 columns of the warp's 32 rows.  They are there after tmem_loaded or tmem_loaded_too, which name the same registers, so that nothing is
+// done with them before.
 __device__ __forceinline__ void tmem_load32(uint32_t at, float* x) {
-    uint32_t r[32];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
                  : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_loaded(float* x) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]) :: "memory");
+}
+__device__ __forceinline__ void tmem_loaded_too(float* x) {
+    asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]) :: "memory");
 }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float exp2_in_order(float x) {          // not moved ahead of earlier stores: registers
+    float y;
+    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -167,7 +176,7 @@ template <int MODE> __device__ __forceinline__ bool tile_at(const GemmArgs& a, i
     return true;
 }
 
-// ---- the tiles' ends: warp `part` of four has 32 rows, `half` says which 128 of the 256 columns ------------------------------------
+// ---- the tiles' ends: warp `part` of four has 32 rows, `half` says which 128 of the 256 columns; a lane has a row -------------------
 // The entries of a row that lie in its 128 columns, in order.
 template <bool ONE> struct Entries {
     const int32_t* entry; const float* q;
@@ -201,176 +210,196 @@ template <bool ONE> struct Entries {
     }
 };
 
-template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a, const TileWork& w, int rows, uint32_t tmem, int64_t row, int half) {
-    const int first = w.n + half * SPAN;      // the piece is the whole vocabulary
-    if (first >= a.vocab) return;             // for the whole warp
-    Entries<ONE> e;
-    e.begin(a, row < rows, row, first);
-    float top = -INFINITY, sum = 0.0f, dot = 0.0f;
-#pragma unroll 1
-    for (int c = 0; c < SPAN; c += 32) {
-        float x[32];
-        __syncwarp();
-        tmem_load32(tmem + half * SPAN + c, x);
-        const int v = first + c;
-        while (e.next < v + 32) {
-            float z = 0.0f;
+// The entries among columns C .. C + 31 of the 128.  Written so that no index into the array is left, which would put it into local memory
+// (the kernel of the statistics then took 1.5 times as long).
+__device__ __forceinline__ void take_if(int at, int k, float x, float& z) {
+    asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\tselp.f32 %0, %3, %0, p;\n\t}" : "+f"(z) : "r"(at), "r"(k), "f"(x));
+}
+__device__ __forceinline__ void subtract_if(int at, int k, float q, float& x) {
+    asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p sub.rn.f32 %0, %0, %3;\n\t}" : "+f"(x) : "r"(at), "r"(k), "f"(q));
+}
+template <int C, bool ONE> __device__ __forceinline__ void take_entries(const float (&x)[SPAN], int first, Entries<ONE>& e, float& dot) {
+    while (e.next < first + C + 32) {
+        float z = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) if (e.next - v == k) z = x[k];
-            dot = fmaf(e.next_q, z, dot);
-            e.advance();
-        }
-        if (v + 32 > a.vocab)
-#pragma unroll
-            for (int k = 0; k < 32; ++k) if (v + k >= a.vocab) x[k] = -INFINITY;
-        float m = x[0];
-#pragma unroll
-        for (int k = 1; k < 32; ++k) m = fmaxf(m, x[k]);
-        m = fmaxf(top, m * a.scale);
-        const float from = m == -INFINITY ? 0.0f : m;     // nothing but -infinity so far: its exponentials are 0
-        sum *= exp2_fast(top - from);
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 32; ++k) s[k & 3] += exp2_fast(fmaf(x[k], a.scale, -from));
-        sum += (s[0] + s[1]) + (s[2] + s[3]);
-        top = m;
+        for (int k = 0; k < 32; ++k) take_if(e.next - first - C, k, x[C + k], z);
+        dot = fmaf(e.next_q, z, dot);
+        e.advance();
     }
+}
+template <int C, bool ONE> __device__ __forceinline__ void subtract_entries(float (&x)[SPAN], int first, Entries<ONE>& e) {
+    while (e.next < first + C + 32) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) subtract_if(e.next - first - C, k, e.next_q, x[C + k]);
+        e.advance();
+    }
+}
+
+template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int half, Entries<ONE>& e) {
+    const int first = w.n + half * SPAN;      // the piece is the whole vocabulary
+    if (first >= a.vocab) return;
+    float dot = 0.0f;
+    take_entries<0>(x, first, e, dot); take_entries<32>(x, first, e, dot); take_entries<64>(x, first, e, dot); take_entries<96>(x, first, e, dot);
+    if (first + SPAN > a.vocab)
+#pragma unroll
+        for (int k = 0; k < SPAN; ++k) if (first + k >= a.vocab) x[k] = -INFINITY;
+    float m[4] = {x[0], x[1], x[2], x[3]}, s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 4; k < SPAN; ++k) m[k & 3] = fmaxf(m[k & 3], x[k]);
+    const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a.scale;
+    const float from = top == -INFINITY ? 0.0f : top;     // nothing but -infinity: its exponentials are 0
+#pragma unroll
+    for (int k = 0; k < SPAN; ++k) s[k & 3] += exp2_fast(fmaf(x[k], a.scale, -from));
     if (row < rows) {
         const int64_t at = (int64_t)(first / SPAN) * a.rows + row;
-        a.stats[at] = make_float2(top, sum);
+        a.stats[at] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
         a.dots[at] = dot;
     }
 }
 
-// Sixteen bits of the handle's type.
-template <class T> __device__ __forceinline__ uint32_t pack_dz(float a, float b, bool low, uint32_t& rest) {
-    const uint32_t r = T::pack2(a, b);
-    if (low) {
-        float x, y;
-        T::unpack2(r, x, y);
-        rest = T::pack2(a - x, b - y);
+// Stores of a warp go by way of shared memory: 32 rows of 128 bytes in two buffers, in the order of the 128-byte swizzle, from where
+// TMA takes them.  (Stored from registers, 16 bytes a lane and a row each, dz of 3456 x 25136 in two numbers took 305 us.)
+struct OutBox {
+    uint32_t at;                              // the warp's two buffers
+    int turn;
+    // Waits until the buffer's last box has been read.
+    __device__ __forceinline__ uint32_t begin() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        return at + (turn++ & 1) * 4096;
     }
-    return r;
+    static __device__ __forceinline__ void put(uint32_t box, int piece, uint4 u) {            // 16 bytes of the lane's row
+        const uint32_t lane = threadIdx.x & 31;
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(box + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+    }
+    static __device__ __forceinline__ void send(uint32_t box, const CUtensorMap* map, int x, int y, int z, bool flat) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            if (flat) asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" :: "l"(map), "r"(x), "r"(y), "r"(box) : "memory");
+            else asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(box) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+    static __device__ __forceinline__ void finish() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+};
+
+// Columns I .. I + 63 of the 128.
+template <int I, class T, bool ONE, bool LOW>
+__device__ __forceinline__ void dz_half(const GemmArgs& a, float (&x)[SPAN], int first, int column, int row0, float lse, float c, Entries<ONE>& e, OutBox& out) {
+#pragma unroll
+    for (int k = I; k < I + 64; ++k) x[k] = exp2_in_order(fmaf(x[k], a.scale, -lse));
+    subtract_entries<I>(x, first, e);
+    subtract_entries<I + 32>(x, first, e);
+    if (c == 0.0f)                            // rows between users, and tokens without weight: 0 whatever the logits are
+#pragma unroll
+        for (int k = I; k < I + 64; ++k) x[k] = 0.0f;
+    if (first + SPAN > a.vocab)
+#pragma unroll
+        for (int k = I; k < I + 64; ++k) if (first + k >= a.vocab) x[k] = 0.0f;
+    const uint32_t box = out.begin();
+#pragma unroll
+    for (int k = I; k < I + 64; k += 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[k + j] *= c;
+        const uint4 u = T::pack(x + k);
+        OutBox::put(box, (k - I) / 8, u);
+        if (LOW) {
+            float y[8];
+            T::unpack(u, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[k + j] -= y[j];
+        }
+    }
+    OutBox::send(box, &a.out, column + I, row0, 0, true);
+    if (LOW) {
+        const uint32_t low = out.begin();
+#pragma unroll
+        for (int k = I; k < I + 64; k += 8) OutBox::put(low, (k - I) / 8, T::pack(x + k));
+        OutBox::send(low, &a.out_low, column + I, row0, 0, true);
+    }
 }
 
-template <class T, bool ONE, bool LOW> __device__ __forceinline__ void end_dz(const GemmArgs& a, const TileWork& w, int rows, uint32_t tmem, int64_t row, int half) {
+template <class T, bool ONE, bool LOW>
+__device__ __forceinline__ void end_dz(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int row0, int half, Entries<ONE>& e, OutBox& out) {
     const int column = w.n + half * SPAN, first = a.v0 + column;
     const bool here = row < rows;
-    Entries<ONE> e;
-    e.begin(a, here && first < a.vocab, row, first);
     const float lse = here ? a.p.row_lse[row] : 0.0f, c = here ? a.p.row_c[row] : 0.0f;
-#pragma unroll 1
-    for (int k0 = 0; k0 < SPAN; k0 += 32) {
-        float x[32];
-        __syncwarp();
-        tmem_load32(tmem + half * SPAN + k0, x);
-        const int v = first + k0;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = exp2_fast(fmaf(x[k], a.scale, -lse));
-        while (e.next < v + 32) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) if (e.next - v == k) x[k] -= e.next_q;
-            e.advance();
-        }
-        // a factor of 0 (rows between users, and tokens without weight) leaves 0 whatever the logits are
-#pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = c == 0.0f || v + k >= a.vocab ? 0.0f : x[k] * c;
-        if (here) {
-            uint4* to = (uint4*)((uint16_t*)a.dz + row * a.dz_pitch + column + k0);
-            uint4* low = (uint4*)((uint16_t*)a.dz_low + row * a.dz_pitch + column + k0);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint4 u, r = make_uint4(0, 0, 0, 0);
-                u.x = pack_dz<T>(x[8 * k], x[8 * k + 1], LOW, r.x);
-                u.y = pack_dz<T>(x[8 * k + 2], x[8 * k + 3], LOW, r.y);
-                u.z = pack_dz<T>(x[8 * k + 4], x[8 * k + 5], LOW, r.z);
-                u.w = pack_dz<T>(x[8 * k + 6], x[8 * k + 7], LOW, r.w);
-                to[k] = u;
-                if (LOW) low[k] = r;
-            }
-        }
-    }
+    dz_half<0, T, ONE, LOW>(a, x, first, column, row0, lse, c, e, out);
+    dz_half<64, T, ONE, LOW>(a, x, first, column, row0, lse, c, e, out);
 }
 
-__device__ __forceinline__ void end_dhidden(const GemmArgs& a, const TileWork& w, int rows, uint32_t tmem, int64_t row, int half) {
+__device__ __forceinline__ void end_dhidden(const GemmArgs& a, const TileWork& w, int rows, const float (&x)[SPAN], int64_t row, int half) {
     const int first = w.n + half * SPAN;
-    float* to = a.partial + ((int64_t)w.split * a.rows + row) * a.dim;
-    const bool empty = w.k0 >= w.k1;
-#pragma unroll 1
-    for (int c = 0; c < SPAN; c += 32) {
-        const int column = first + c;
-        if (column >= a.dim) break;           // for the whole warp
-        float x[32];
-        __syncwarp();
-        tmem_load32(tmem + half * SPAN + c, x);
-        if (row >= rows) continue;
+    if (row >= rows) return;
+    float* to = a.partial + ((int64_t)w.split * a.rows + row) * a.dim + first;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (column + 4 * k >= a.dim) continue;        // dim is a multiple of 8
-            float4 s = empty ? make_float4(0, 0, 0, 0) : make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-            float4* p = (float4*)(to + column + 4 * k);
-            if (a.add) { const float4 o = *p; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
-            *p = s;
-        }
+    for (int k = 0; k < SPAN; k += 4) {
+        if (first + k >= a.dim) break;        // dim is a multiple of 8
+        float4 s = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+        float4* p = (float4*)(to + k);
+        if (a.add) { const float4 o = *p; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
+        *p = s;
     }
 }
 
 // D: the type of dweight.
-template <class D> __device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w, uint32_t tmem, int row0, int half, float (*turn)[33]) {
-    const int lane = threadIdx.x & 31, first = w.n + half * SPAN;
-    const bool empty = w.k0 >= w.k1;          // a user without a token that counts
-    const float down = empty ? 0.0f : 1.0f / a.p.up[w.user];
-    const int64_t v = (int64_t)a.v0 + row0;
-    typename D::type* base = (typename D::type*)a.dw.data + w.user * a.dw.user_stride;
-#pragma unroll 1
+template <class D>
+__device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w, float (&x)[SPAN], int row0, int half, float (*turn)[33], OutBox& out) {
+    const int lane = threadIdx.x & 31, first = w.n + half * SPAN, v = a.v0 + row0;
+    if (v >= a.vocab) return;
+    const float down = 1.0f / a.p.up[w.user];
+#pragma unroll
+    for (int k = 0; k < SPAN; ++k) x[k] *= down;
+    if (a.dw_wide) {
+        constexpr int BOX = 128 / sizeof(typename D::type);
+#pragma unroll
+        for (int c = 0; c < SPAN; c += BOX) {
+            if (first + c >= a.dim) break;
+            const uint32_t box = out.begin();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) OutBox::put(box, k, D::pack(x + c + k * D::EACH));
+            OutBox::send(box, &a.out, first + c, v, w.user, false);
+        }
+        return;
+    }
+    typename D::type* base = (typename D::type*)a.dw.data + w.user * a.dw.user_stride + (int64_t)v * a.dim;
+    const int count = a.vocab - v < 32 ? a.vocab - v : 32;
+#pragma unroll
     for (int c = 0; c < SPAN; c += 32) {
         const int column = first + c;
         if (column >= a.dim) break;
-        float x[32];
+        // turned round in shared memory, so that a store is one piece of a row
+#pragma unroll
+        for (int k = 0; k < 32; ++k) turn[lane][k] = x[c + k];
         __syncwarp();
-        tmem_load32(tmem + half * SPAN + c, x);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = empty ? 0.0f : x[k] * down;
-        if (a.dw_wide) {
-            if (v + lane < a.vocab && row0 + lane < a.columns) {
-                typename D::type* p = base + (v + lane) * a.dim + column;
-#pragma unroll
-                for (int k = 0; k < 32; k += D::EACH) {
-                    if (column + k >= a.dim) continue;
-                    if (a.dw.accumulate) {
-                        float o[8];
-                        D::unpack(*(const uint4*)(p + k), o);
-#pragma unroll
-                        for (int j = 0; j < D::EACH; ++j) x[k + j] += o[j];
-                    }
-                    *(uint4*)(p + k) = D::pack(x + k);
-                }
-            }
-        } else {                              // by way of shared memory, so that a store is one piece of a row
-#pragma unroll
-            for (int k = 0; k < 32; ++k) turn[lane][k] = x[k];
-            __syncwarp();
-            if (column + lane < a.dim)
+        if (column + lane < a.dim) {
+            typename D::type* p = base + column + lane;
+            if (a.dw.accumulate)
 #pragma unroll 8
-                for (int r = 0; r < 32; ++r) {
-                    if (v + r >= a.vocab || row0 + r >= a.columns) break;
-                    typename D::type* p = base + (v + r) * a.dim + column + lane;
-                    const float y = turn[r][lane];
-                    *p = D::put(a.dw.accumulate ? D::get(*p) + y : y);
-                }
-            __syncwarp();
+                for (int r = 0; r < count; ++r, p += a.dim) *p = D::put(D::get(*p) + turn[r][lane]);
+            else
+#pragma unroll 8
+                for (int r = 0; r < count; ++r, p += a.dim) *p = D::put(turn[r][lane]);
         }
+        __syncwarp();
     }
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------------------
+// Stages of depth that an accumulator takes: the tensor cores cut a sum's last bits off at each 16 of depth (0.2 .. 0.7 units in the
+// last place of 32 bits, always towards zero), so sums over more are added up in registers, rounded to nearest (z over 4096: 4.5e-6 of it in one
+// sum).  dhidden is rounded to 16 bits in the end.
+template <int MODE> constexpr int CHUNK = MODE == DHIDDEN ? 1 << 20 : 16;
+
 template <int MODE, class T, class D, bool ONE, bool LOW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs a) {
     constexpr bool A_ALONG = MODE != DWEIGHT, B_ALONG = MODE == STATS || MODE == DZ;       // whether the depth runs along the matrix' rows
     extern __shared__ uint8_t raw[];
     uint8_t* const stages = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    float(*const turn)[33] = (float(*)[33])(stages + STAGES * STAGE_BYTES);
-    uint64_t* const bars = (uint64_t*)(stages + STAGES * STAGE_BYTES + TRANSPOSE_BYTES);
+    uint64_t* const bars = (uint64_t*)(stages + STAGES * STAGE_BYTES + OUT_BYTES);
     const uint32_t full = shared_at(bars), empty = full + 8 * STAGES, done = empty + 8 * STAGES, free_ = done + 16, drained = free_ + 16;
     volatile uint32_t* const tmem_at = (volatile uint32_t*)(bars + 2 * STAGES + 5);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -382,7 +411,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
         bar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) {
+    if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(shared_at((const void*)tmem_at)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
@@ -440,48 +469,89 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
             const uint32_t kind = std::is_same<T, OBf16>::value ? 1 : 0;
             const uint32_t desc = 1u << 4 | kind << 7 | kind << 10 | (A_ALONG ? 0u : 1u << 15) | (B_ALONG ? 0u : 1u << 16) | (TILE >> 3) << 17 | (TILE >> 4) << 24;
             uint32_t s = 0, phase = 0, turn_no = 0;
-            for (int64_t i = pair; fine && tile_at<MODE>(a, rows, i, w); i += pairs, ++turn_no) {
-                const uint32_t buffer = turn_no & 1, to = tmem + buffer * TILE;
-                if (!(fine = bar_wait(free_ + 8 * buffer, (turn_no >> 1 & 1) ^ 1))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(fine = bar_wait(full + 8 * s, phase))) break;
+            for (int64_t i = pair; fine && tile_at<MODE>(a, rows, i, w); i += pairs) {
+                int k = w.k0;
+                do {                          // once for a tile without depth
+                    const uint32_t buffer = turn_no & 1, to = tmem + buffer * TILE;
+                    if (!(fine = bar_wait(free_ + 8 * buffer, (turn_no >> 1 & 1) ^ 1))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t at = shared_at(stages) + s * STAGE_BYTES;
-                    const uint64_t da = operand_desc<A_ALONG>(at), db = operand_desc<B_ALONG>(at + HALF_BYTES);
+                    const int k2 = w.k1 - k < CHUNK<MODE> ? w.k1 : k + CHUNK<MODE>;
+                    for (bool add = false; k < k2; ++k) {
+                        if (!(fine = bar_wait(full + 8 * s, phase))) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t at = shared_at(stages) + s * STAGE_BYTES;
+                        const uint64_t da = operand_desc<A_ALONG>(at), db = operand_desc<B_ALONG>(at + HALF_BYTES);
 #pragma unroll
-                    for (int j = 0; j < KB / 16; ++j)     // 16 deep: 32 bytes along the rows, or sixteen rows
-                        mma(to, da + j * (A_ALONG ? 32 >> 4 : 2048 >> 4), db + j * (B_ALONG ? 32 >> 4 : 2048 >> 4), desc, k > w.k0 || j > 0);
-                    mma_commit(empty + 8 * s);
-                    if (++s == STAGES) { s = 0; phase ^= 1; }
-                }
-                if (!fine) break;
-                mma_commit(done + 8 * buffer);
+                        for (int j = 0; j < KB / 16; ++j) {   // 16 deep: 32 bytes along the rows, or sixteen rows
+                            mma(to, da + j * (A_ALONG ? 32 >> 4 : 2048 >> 4), db + j * (B_ALONG ? 32 >> 4 : 2048 >> 4), desc, add);
+                            add = true;
+                        }
+                        mma_commit(empty + 8 * s);
+                        if (++s == STAGES) { s = 0; phase ^= 1; }
+                    }
+                    if (!fine) break;
+                    mma_commit(done + 8 * buffer);
+                    ++turn_no;
+                } while (k < w.k1);
             }
             // no product is under way when the memory is given back
             asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(drained) : "memory");
             fine &= bar_wait(drained, 0);
         }
-    } else if (warp >= 4) {
-        const int part = warp & 3, half = (warp - 4) >> 2;
+    } else {
+        const int part = warp & 3, half = (warp - FIRST_EPI) >> 2;         // a warp reads the quarter of the lanes that its number gives
         uint32_t turn_no = 0;
         const uint32_t far_free = at_rank(free_, 0);
-        for (int64_t i = pair; tile_at<MODE>(a, rows, i, w); i += pairs, ++turn_no) {
-            const uint32_t buffer = turn_no & 1;
-            if (!(fine = bar_wait(done + 8 * buffer, turn_no >> 1 & 1))) break;
-            __syncwarp();
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint8_t* const mine = stages + STAGES * STAGE_BYTES + (warp - FIRST_EPI) * 8192;
+        OutBox out = {shared_at(mine), 0};
+        for (int64_t i = pair; fine && tile_at<MODE>(a, rows, i, w); i += pairs) {
             const int in_tile = (int)rank * 128 + part * 32;
-            const uint32_t at = tmem + buffer * TILE + ((uint32_t)part << 21);            // lane 32 part
             const int64_t row = (int64_t)w.m + in_tile + lane;
-            if constexpr (MODE == STATS) end_stats<ONE>(a, w, rows, at, row, half);
-            if constexpr (MODE == DZ) end_dz<T, ONE, LOW>(a, w, rows, at, row, half);
-            if constexpr (MODE == DHIDDEN) end_dhidden(a, w, rows, at, row, half);
-            if constexpr (MODE == DWEIGHT) end_dweight<D>(a, w, at, w.m + in_tile, half, turn + (warp - 4) * 32);
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            Entries<ONE> e;                   // looked for while the products run
+            if constexpr (MODE == STATS || MODE == DZ) {
+                const int first = a.v0 + w.n + half * SPAN;
+                e.begin(a, row < rows && first < a.vocab, row, first);
+            }
+            float x[SPAN];
+            int k = w.k0;
+            do {
+                const uint32_t buffer = turn_no & 1;
+                if (!(fine = bar_wait(done + 8 * buffer, turn_no >> 1 & 1))) break;
+                __syncwarp();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t at = tmem + buffer * TILE + half * SPAN + ((uint32_t)part << 21);        // lane 32 part
+                if (k == w.k0) {
+#pragma unroll
+                    for (int c = 0; c < SPAN; c += 32) tmem_load32(at + c, x + c);
+                    tmem_loaded(x);
+#pragma unroll
+                    for (int c = 32; c < SPAN; c += 32) tmem_loaded_too(x + c);
+                } else
+#pragma unroll
+                    for (int c = 0; c < SPAN; c += 32) {
+                        float y[32];
+                        tmem_load32(at + c, y);
+                        tmem_loaded(y);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[c + j] += y[j];
+                    }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(far_free + 8 * buffer);
+                ++turn_no;
+                k = w.k1 - k < CHUNK<MODE> ? w.k1 : k + CHUNK<MODE>;
+            } while (k < w.k1);
+            if (!fine) break;
+            if (w.k0 >= w.k1)                 // no depth (a user without a token that counts): the sums are 0
+#pragma unroll
+                for (int j = 0; j < SPAN; ++j) x[j] = 0.0f;
+            if constexpr (MODE == STATS) end_stats<ONE>(a, w, rows, x, row, half, e);
+            if constexpr (MODE == DZ) end_dz<T, ONE, LOW>(a, w, rows, x, row, w.m + in_tile, half, e, out);
+            if constexpr (MODE == DHIDDEN) end_dhidden(a, w, rows, x, row, half);
+            if constexpr (MODE == DWEIGHT) end_dweight<D>(a, w, x, w.m + in_tile, half, (float(*)[33])mine, out);
             __syncwarp();
-            if (lane == 0) bar_arrive_cluster(far_free + 8 * buffer);
         }
+        if (MODE == DZ || MODE == DWEIGHT) OutBox::finish();
     }
     if (!fine) atomicOr(&a.status->flags, CO3_FLAG_TIMEOUT);
     __syncwarp();
@@ -489,7 +559,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
     __syncthreads();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
 }
 
 // ---- before and after the products -----------------------------------------------------------------------------------------
@@ -828,7 +898,7 @@ struct co3_token_loss {
     int users, type, grad_type, max_top, device, pairs, spans, max_splits;
     int64_t piece;                            // columns of dz that are held at a time
     EncodeTiled encode;
-    CUtensorMap map_hidden, map_dz, map_low;
+    CUtensorMap map_hidden, map_dz, map_low, map_dz_out, map_low_out;
     void* slab;
     OpsStatus* status;
     Packed p;
@@ -840,12 +910,25 @@ struct co3_token_loss {
 
 namespace {
 
-// A matrix of 16-bit numbers in boxes of 64 x 64.
-bool make_map(const co3_token_loss* h, CUtensorMap* map, const void* data, int64_t columns, int64_t rows, int64_t stride) {
+CUtensorMapDataType map_type(int type) {
+    return type == CO3_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == CO3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+}
+// A matrix of 16-bit numbers in boxes of 64 columns: 64 rows to load, 32 to store.
+bool make_map(const co3_token_loss* h, CUtensorMap* map, const void* data, int64_t columns, int64_t rows, int64_t stride, int box_rows = 64) {
     const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t box[2] = {64, 64}, one[2] = {1, 1};
-    return h->encode(map, h->type == CO3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, (void*)data, dims, strides, box, one,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    return h->encode(map, map_type(h->type), 2, (void*)data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// dweight in boxes of 128 bytes and 32 rows.
+bool make_grad_map(const co3_token_loss* h, CUtensorMap* map, const co3_param_grad* g) {
+    const int width = type_width(g->type);
+    const cuuint64_t dims[3] = {(cuuint64_t)h->dim, (cuuint64_t)h->vocab, (cuuint64_t)h->users};
+    const cuuint64_t strides[2] = {(cuuint64_t)(h->dim * width), (cuuint64_t)((h->users > 1 ? g->user_stride : h->dim * h->vocab) * width)};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / width), 32, 1}, one[3] = {1, 1, 1};
+    return strides[1] < (cuuint64_t)1 << 40 &&
+           h->encode(map, map_type(g->type), 3, g->data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <class K> bool big_shared(K kernel) {
@@ -925,7 +1008,7 @@ int begin_call(co3_token_loss* h, const co3_array* hidden, const void* weight, i
     if (!make_map(h, &a.b, weight, h->dim, h->vocab, weight_stride)) return CO3_EINVAL;
     a.p = h->p; a.status = h->status; a.users = h->users; a.vocab = (int)h->vocab; a.dim = (int)h->dim; a.splits = 1; a.terms = 1; a.rows = h->rows;
     a.scale = LOG2E / temperature; a.stats = h->stats; a.dots = h->dots; a.entry = h->entry; a.entry_q = h->q; a.entry_first = h->first; a.top = k.top;
-    a.spans = h->spans; a.dz = h->dz; a.dz_low = h->low; a.dz_pitch = h->piece; a.partial = h->partial;
+    a.spans = h->spans; a.partial = h->partial;
     return CO3_OK;
 }
 
@@ -958,10 +1041,17 @@ template <class T> int forward_of(co3_token_loss* h, Call& c, float temperature,
 template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* dhidden, const co3_param_grad* dweight, int64_t n_tokens, cudaStream_t st) {
     const bool low = dweight && dweight->type == CO3_F32;
     const int64_t mt = up_to(c.rows, TILE) / TILE, nt = up_to(h->dim, TILE) / TILE;
-    int rc = CO3_OK, splits = 1;
+    int rc = CO3_OK, splits = 1, wide = 0;
+    CUtensorMap map_dw;
+    if (dweight) {
+        const int width = type_width(dweight->type);
+        wide = !dweight->accumulate && aligned_to(dweight->data, 16) && h->dim * width % 16 == 0 && (h->users == 1 || dweight->user_stride * width % 16 == 0) &&
+               make_grad_map(h, &map_dw, dweight);
+    }
     if (dhidden) splits = splits_of(h, mt * nt, up_to(h->piece < h->vocab ? h->piece : h->vocab, KB) / KB);
     for (int64_t v0 = 0; v0 < h->vocab && rc == CO3_OK; v0 += h->piece) {
         GemmArgs a = c.g;
+        a.out = h->map_dz_out; a.out_low = h->map_low_out;
         a.v0 = (int)v0;
         a.columns = (int)(h->vocab - v0 < h->piece ? h->vocab - v0 : h->piece);
         const int64_t ct = up_to(a.columns, TILE) / TILE;
@@ -975,9 +1065,9 @@ template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* 
         }
         if (rc == CO3_OK && dweight) {
             GemmArgs b = a;
-            const int width = type_width(dweight->type);
+            if (wide) b.out = map_dw;
             b.a = h->map_dz; b.a_low = h->map_low; b.b = h->map_hidden; b.terms = low ? 2 : 1; b.dw = *dweight;
-            b.dw_wide = aligned_to(dweight->data, 16) && h->dim * width % 16 == 0 && (h->users == 1 || dweight->user_stride * width % 16 == 0);
+            b.dw_wide = wide;
             rc = gemm(h, low ? gemm_kernel<DWEIGHT, T, OF32, true, false> : gemm_kernel<DWEIGHT, T, T, true, false>, ct * nt * h->users, b, st);
         }
     }
@@ -1056,7 +1146,8 @@ extern "C" int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_
             h->entry = (int32_t*)(base + o_e); h->q = (float*)(base + o_q); h->constant = (float*)(base + o_k); h->first = (uint8_t*)(base + o_f); h->mass = (uint8_t*)(base + o_m);
             if (cudaMemset(h->status, 0, sizeof(OpsStatus)) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess ||
                 !make_map(h, &h->map_hidden, h->hidden, h->dim, h->rows, h->dim) || !make_map(h, &h->map_dz, h->dz, h->piece, h->rows, h->piece) ||
-                (h->grad_type == CO3_F32 && !make_map(h, &h->map_low, h->low, h->piece, h->rows, h->piece))) rc = CO3_ECUDA;
+                !make_map(h, &h->map_dz_out, h->dz, h->piece, h->rows, h->piece, 32) ||
+                (h->grad_type == CO3_F32 && (!make_map(h, &h->map_low, h->low, h->piece, h->rows, h->piece) || !make_map(h, &h->map_low_out, h->low, h->piece, h->rows, h->piece, 32)))) rc = CO3_ECUDA;
         }
     }
     if (rc != CO3_OK) { (void)cudaGetLastError(); co3_token_loss_destroy(h); return rc; }
