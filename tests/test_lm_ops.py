@@ -697,6 +697,41 @@ def test_outputs_are_marked_as_changed():
     assert loss._version > v
 
 
+@pytest.mark.parametrize("teacher", [0, 3])
+def test_the_training_loop_of_tokens(teacher):
+    """It runs, encodes and decodes, and its rows hold the users' gradients."""
+    from paper_2203_09044_b200 import train_step
+    losses = train_step.run_tokens(iterations=4, n_users=3, vocab=300, dim=64, tokens=40, teacher=teacher)
+    assert len(losses) == 4 and all(math.isfinite(x) for x in losses)
+    g = gen(5)
+    model = train_step.TokenModel(300, 64, 3, 40, top=max(1, teacher), seed=1)
+    inputs, targets = train_step.token_batch(torch.randint(0, 300, (300, 4), generator=g, device="cuda"), 3, 40, g)
+    rows = torch.full((3, model.d + 3), NAN, device="cuda")
+    entries = None
+    if teacher:
+        index = torch.randint(0, 300, (3, 40, teacher), generator=g, device="cuda").masked_fill((inputs < 0)[..., None], -1)
+        entries = index, normal(g, 3, 40, teacher)
+    loss = model.gradients(inputs, targets, rows, entries)
+    for i in range(3):
+        on = inputs[i] >= 0
+        table, scale, shift, head = (c.double().requires_grad_() for c in model.copies)
+        y = torch.nn.functional.layer_norm(table[inputs[i][on]], (64,), scale, shift, 1e-5)
+        logp = torch.log_softmax(y @ head.T, 1)
+        if teacher:
+            q = shares(entries[1][i][on], index[i][on], 1.0)
+            each = (q * (q.log() - logp.gather(1, index[i][on]))).sum(1)
+        else:
+            each = -logp.gather(1, targets[i][on][:, None])[:, 0]
+        assert not loss[i][~on].any()
+        # hidden states in 8 bits: 2^-8 of |y|, times a row of the head, for the target and the mean over the others
+        assert ((loss[i][on].double() - each).abs() <= 2 * u(BF16) * (y.abs() @ head.abs().T).amax(1) + 1e-5).all()
+        each.mean().backward()
+        for part, grad in zip(model.segments(rows), (table.grad, scale.grad, shift.grad, head.grad)):
+            # roundings to 8 bits on the way: hidden, dz, dhidden, dx
+            assert (part[i].double() - grad.reshape(-1)).norm() <= 5 * u(BF16) * grad.norm()
+    assert rows[:, model.d:].isnan().all()
+
+
 # ---- refusals -----------------------------------------------------------------------------------------------------------------
 def refused(call, *errors):
     with pytest.raises(errors or (ValueError, TypeError, b.Co3Error)):
