@@ -909,6 +909,16 @@ class AdamW(GradNorm):
 
 
 # ---- the two ends of a language model: embedding, layer norm, losses over the vocabulary -----------------------------
+_token_kinds = {}
+
+
+def _token_codes(dtype):
+    if not _token_kinds:
+        import torch
+        _token_kinds.update({torch.int32: I32, torch.int64: I64})
+    return _token_kinds.get(dtype)
+
+
 class _Operator:
     """A handle of the library on the current CUDA device, for batches [users][tokens] (with one user also [tokens]).  The calls only enqueue
     kernels, on the current stream or the one given, and share the handle's scratch: use one handle on one stream at a time.  They are not
@@ -919,7 +929,8 @@ class _Operator:
 
     def _create(self, make, n_users):
         import torch
-        self.torch, self._lib, self.n_users = torch, lib(), int(n_users)
+        self.torch, self._lib, self.n_users, self._float32 = torch, lib(), int(n_users), torch.float32
+        self._shapes, self._empty_like = {}, torch.empty_like
         self._increment_version = torch._C._increment_version
         h = C.c_void_p()
         rc = make(C.byref(h))
@@ -950,55 +961,77 @@ class _Operator:
             raise Co3Error(rc, f"co3_{self._kind}_status")
         return int(f.value), int(n.value)
 
+    def _new(self, shape, dtype, stream):
+        """Memory for an output, of a shape and type that this object keeps a view of one element of: asking for a tensor like that one is the
+        quickest way to memory (0.9 us, 2.4 from a shape and a type)."""
+        if stream is not None:
+            return self._empty(shape, dtype, stream)
+        like = self._shapes.get((shape, dtype))
+        if like is None:
+            if len(self._shapes) >= 64:
+                self._shapes.clear()
+            like = self._shapes[shape, dtype] = self.torch.empty(1, dtype=dtype, device=self.device).expand(shape)
+        return self._empty_like(like)
+
     def _batch(self, t, dim, what, like=None):
-        """co3_array of a tensor [users][tokens][dim]; `like`: the leading sizes that it has to have."""
-        shape, strides = t.shape, t.stride()
+        """co3_array of a tensor [users][tokens][dim] and its tokens; `like`: the leading sizes that it has to have."""
+        shape, users = t.shape, self.n_users
+        if len(shape) == 3 and shape[0] == users and shape[2] == dim and t.device == self.device and t.is_contiguous() and (like is None or shape[:2] == like):
+            return Array(t.data_ptr(), _type_code(t.dtype), 0, shape[1] * dim, dim), shape[1]
+        strides = t.stride()
         if t.device != self.device:
             raise ValueError(f"{what}: a tensor on {self.device} expected, got one on {t.device}")
-        if len(shape) == 2 and self.n_users == 1:
+        if len(shape) == 2 and users == 1:
             tokens, us, ts = shape[0], 0, strides[0]
-        elif len(shape) == 3 and shape[0] == self.n_users:
+        elif len(shape) == 3 and shape[0] == users:
             tokens, us, ts = shape[1], strides[0], strides[1]
         else:
-            raise ValueError(f"{what}: [{self.n_users}, tokens, {dim}] expected, got {tuple(shape)}")
+            raise ValueError(f"{what}: [{users}, tokens, {dim}] expected, got {tuple(shape)}")
         if shape[-1] != dim or (dim > 1 and strides[-1] != 1):
             raise ValueError(f"{what}: rows of {dim} elements side by side expected, got shape {tuple(shape)}, strides {strides}")
         if like is not None and shape[:-1] != like:
             raise ValueError(f"{what}: {tuple(like)} rows expected, got {tuple(shape[:-1])}")
         return Array(t.data_ptr(), _type_code(t.dtype), 0, us, ts), tokens
 
+    def _own_batch(self, t, dim, n):
+        """... of one that was made here."""
+        return Array(t.data_ptr(), _type_code(t.dtype), 0, n * dim, dim)
+
     def _tokens(self, t, what="tokens", like=None, top=None):
         """co3_tokens of whole numbers [users][tokens], or [users][tokens][top]."""
-        torch = self.torch
-        if t.dtype not in (torch.int32, torch.int64) or t.device != self.device:
+        kind = _token_codes(t.dtype)
+        if kind is None or t.device != self.device:
             raise ValueError(f"{what}: int32 or int64 on {self.device} expected, got {t.dtype} on {t.device}")
         shape, strides = t.shape, t.stride()
         lead = shape if top is None else shape[:-1]
         if top is not None and (len(shape) < 2 or (top > 1 and strides[-1] != 1)):
             raise ValueError(f"{what}: entries of a token side by side expected, got shape {tuple(shape)}, strides {strides}")
-        if len(lead) == 1 and self.n_users == 1:
-            us, ts = 0, strides[0]
-        elif len(lead) == 2 and lead[0] == self.n_users:
+        if len(lead) == 2 and lead[0] == self.n_users:
             us, ts = strides[0], strides[1]
+        elif len(lead) == 1 and self.n_users == 1:
+            us, ts = 0, strides[0]
         else:
             raise ValueError(f"{what}: [{self.n_users}, tokens] expected, got {tuple(lead)}")
-        if like is not None and tuple(lead) != tuple(like):
+        if like is not None and lead != like:
             raise ValueError(f"{what}: {tuple(like)} expected, got {tuple(lead)}")
-        return Tokens(t.data_ptr(), I32 if t.dtype == torch.int32 else I64, 1 if top is None else top, us, ts), lead
+        return Tokens(t.data_ptr(), kind, 1 if top is None else top, us, ts), lead
 
     def _grad(self, t, n, accumulate, what):
         """co3_param_grad of a tensor that holds n elements for each user, each user's in one piece."""
-        if t.device != self.device or t.numel() != self.n_users * n:
-            raise ValueError(f"{what}: {self.n_users} times {n} elements on {self.device} expected, got {tuple(t.shape)} on {t.device}")
+        users = self.n_users
+        if t.device != self.device or t.numel() != users * n:
+            raise ValueError(f"{what}: {users} times {n} elements on {self.device} expected, got {tuple(t.shape)} on {t.device}")
+        if t.is_contiguous() and (users == 1 or t.shape[0] == users):
+            return ParamGrad(t.data_ptr(), _type_code(t.dtype), bool(accumulate), n)
         shape, strides = t.shape, t.stride()
-        if self.n_users > 1 and (not shape or shape[0] != self.n_users):
-            raise ValueError(f"{what}: [{self.n_users}, ...] expected, got {tuple(shape)}")
+        if users > 1 and (not shape or shape[0] != users):
+            raise ValueError(f"{what}: [{users}, ...] expected, got {tuple(shape)}")
         at = 1
-        for size, stride in zip(reversed(shape[1:] if self.n_users > 1 else shape), reversed(strides[1:] if self.n_users > 1 else strides)):
-            if size != 1 and stride != at and n:
+        for i in range(len(shape) - 1, 0 if users > 1 else -1, -1):
+            if shape[i] != 1 and strides[i] != at and n:
                 raise ValueError(f"{what}: each user's part in one piece expected, got shape {tuple(shape)}, strides {strides}")
-            at *= size
-        return ParamGrad(t.data_ptr(), _type_code(t.dtype), int(accumulate), strides[0] if self.n_users > 1 else n)
+            at *= shape[i]
+        return ParamGrad(t.data_ptr(), _type_code(t.dtype), bool(accumulate), strides[0] if users > 1 else n)
 
     def _vector(self, t, n, what):
         """Pointer and type of a weight of n elements, or (None, F32)."""
@@ -1009,17 +1042,25 @@ class _Operator:
         return t.data_ptr(), _type_code(t.dtype)
 
     def _per_token(self, t, like, what):
-        if t.dtype is not self.torch.float32 or t.shape != like or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not self._float32 or t.shape != like or t.device != self.device or not t.is_contiguous():
             raise ValueError(f"{what}: contiguous float32 {tuple(like)} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
-    def _done(self, rc, call, written):
-        if rc != OK:
-            raise Co3Error(rc, call)
-        self._increment_version(written)
+    def _output(self, t, lead, what, stream):
+        """A float32 output of a number a token, the one given or a new one, and its pointer."""
+        if t is not None:
+            return t, self._per_token(t, lead, what)
+        t = self._new(lead, self._float32, stream)
+        return t, t.data_ptr()
 
     def _on(self, stream, tensors):
         return self._current_stream() if stream is None else self._record(stream, tensors)
+
+    def _changed(self, *given):
+        """What the caller gave to be written."""
+        given = [t for t in given if t is not None]
+        if given:
+            self._increment_version(given)
 
 
 class Embedding(_Operator):
@@ -1038,15 +1079,21 @@ class Embedding(_Operator):
     def forward(self, tokens, table, scale=1.0, out=None, out_dtype=None, stream=None):
         """scale * table[token], zeros where a token is below zero: [*tokens.shape, dim], in out_dtype (the table's if None)."""
         k, lead = self._tokens(tokens)
-        if tuple(table.shape) != (self.vocab, self.dim) or not table.is_contiguous() or table.device != self.device:
+        if table.shape != (self.vocab, self.dim) or not table.is_contiguous() or table.device != self.device:
             raise ValueError(f"table: contiguous [{self.vocab}, {self.dim}] on {self.device} expected, got {tuple(table.shape)} on {table.device}")
+        given, n = out, lead[-1]
         if out is None:
-            out = self._empty((*lead, self.dim), out_dtype or table.dtype, stream)
-        elif out_dtype not in (None, out.dtype):
-            raise ValueError(f"out: {out_dtype} expected, got {out.dtype}")
-        o, n = self._batch(out, self.dim, "out", lead)
-        s = self._on(stream, [tokens, table, out])
-        self._done(self._lib.co3_embed_forward(self.handle, k, n, table.data_ptr(), _type_code(table.dtype), scale, o, s), "co3_embed_forward", [out])
+            out = self._new((*lead, self.dim), out_dtype or table.dtype, stream)
+            o = self._own_batch(out, self.dim, n)
+        else:
+            if out_dtype not in (None, out.dtype):
+                raise ValueError(f"out: {out_dtype} expected, got {out.dtype}")
+            o, _ = self._batch(out, self.dim, "out", lead)
+        s = self._on(stream, (tokens, table, out))
+        rc = self._lib.co3_embed_forward(self.handle, k, n, table.data_ptr(), _type_code(table.dtype), scale, o, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_embed_forward")
+        self._changed(given)
         return out
 
     def backward(self, dout, tokens, dtable, scale=1.0, accumulate=False, stream=None):
@@ -1055,8 +1102,11 @@ class Embedding(_Operator):
         k, lead = self._tokens(tokens)
         g, n = self._batch(dout, self.dim, "dout", lead)
         t = self._grad(dtable, self.vocab * self.dim, accumulate, "dtable")
-        s = self._on(stream, [dout, tokens, dtable])
-        self._done(self._lib.co3_embed_backward(self.handle, g, k, n, scale, t, s), "co3_embed_backward", [dtable])
+        s = self._on(stream, (dout, tokens, dtable))
+        rc = self._lib.co3_embed_backward(self.handle, g, k, n, scale, t, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_embed_backward")
+        self._changed(dtable)
         return dtable
 
 
@@ -1071,39 +1121,52 @@ class LayerNorm(_Operator):
 
     def forward(self, x, weight=None, bias=None, y=None, mean=None, rstd=None, stream=None):
         """(y, mean, rstd); y has x's type, mean and rstd are float32, one for each row."""
-        a, n = self._batch(x, self.dim, "x")
+        dim = self.dim
+        a, n = self._batch(x, dim, "x")
         lead = x.shape[:-1]
-        (w, wt), (b, bt) = self._vector(weight, self.dim, "weight"), self._vector(bias, self.dim, "bias")
-        if weight is not None and bias is not None and wt != bt:
+        w, wt = self._vector(weight, dim, "weight")
+        b, bt = self._vector(bias, dim, "bias")
+        if weight is None:
+            wt = bt
+        elif bias is not None and wt != bt:
             raise ValueError(f"weight and bias of one type expected, got {weight.dtype} and {bias.dtype}")
+        given = y, mean, rstd
         if y is None:
-            y = self._empty(x.shape, x.dtype, stream)
-        if mean is None:
-            mean = self._empty(lead, self.torch.float32, stream)
-        if rstd is None:
-            rstd = self._empty(lead, self.torch.float32, stream)
-        o, _ = self._batch(y, self.dim, "y", lead)
-        m, r = self._per_token(mean, lead, "mean"), self._per_token(rstd, lead, "rstd")
-        s = self._on(stream, [x, weight, bias, y, mean, rstd])
-        self._done(self._lib.co3_layernorm_forward(self.handle, a, w, b, wt if weight is not None else bt, n, o, m, r, s), "co3_layernorm_forward", [y, mean, rstd])
+            y = self._new(x.shape, x.dtype, stream)
+            o = self._own_batch(y, dim, n)
+        else:
+            o, _ = self._batch(y, dim, "y", lead)
+        mean, m = self._output(mean, lead, "mean", stream)
+        rstd, r = self._output(rstd, lead, "rstd", stream)
+        s = self._on(stream, (x, weight, bias, y, mean, rstd))
+        rc = self._lib.co3_layernorm_forward(self.handle, a, w, b, wt, n, o, m, r, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_layernorm_forward")
+        self._changed(*given)
         return y, mean, rstd
 
     def backward(self, dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, accumulate=False, want_dx=True, stream=None):
         """dx (None if not wanted); the users' gradients of weight and bias go into dweight and dbias ([users, dim], any float type) where
         given."""
-        a, n = self._batch(x, self.dim, "x")
+        dim, given = self.dim, dx
+        a, n = self._batch(x, dim, "x")
         lead = x.shape[:-1]
-        g, _ = self._batch(dy, self.dim, "dy", lead)
-        w, wt = self._vector(weight, self.dim, "weight")
+        g, _ = self._batch(dy, dim, "dy", lead)
+        w, wt = self._vector(weight, dim, "weight")
         m, r = self._per_token(mean, lead, "mean"), self._per_token(rstd, lead, "rstd")
-        if dx is None and want_dx:
-            dx = self._empty(x.shape, x.dtype, stream)
-        o = None if dx is None else self._batch(dx, self.dim, "dx", lead)[0]
-        dw = None if dweight is None else self._grad(dweight, self.dim, accumulate, "dweight")
-        db = None if dbias is None else self._grad(dbias, self.dim, accumulate, "dbias")
-        s = self._on(stream, [dy, x, weight, mean, rstd, dx, dweight, dbias])
-        self._done(self._lib.co3_layernorm_backward(self.handle, g, a, w, wt, m, r, n, o, dw, db, s), "co3_layernorm_backward",
-                   [t for t in (dx, dweight, dbias) if t is not None])
+        o = None
+        if dx is not None:
+            o, _ = self._batch(dx, dim, "dx", lead)
+        elif want_dx:
+            dx = self._new(x.shape, x.dtype, stream)
+            o = self._own_batch(dx, dim, n)
+        dw = None if dweight is None else self._grad(dweight, dim, accumulate, "dweight")
+        db = None if dbias is None else self._grad(dbias, dim, accumulate, "dbias")
+        s = self._on(stream, (dy, x, weight, mean, rstd, dx, dweight, dbias))
+        rc = self._lib.co3_layernorm_backward(self.handle, g, a, w, wt, m, r, n, o, dw, db, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_layernorm_backward")
+        self._changed(given, dweight, dbias)
         return dx
 
 
@@ -1145,41 +1208,46 @@ class TokenLoss(_Operator):
 
     def _inputs(self, hidden, weight, targets, logits):
         h, n = self._batch(hidden, self.dim, "hidden")
-        if hidden.dtype != self.dtype or weight.dtype != self.dtype:
+        if hidden.dtype is not self.dtype or weight.dtype is not self.dtype:
             raise TypeError(f"hidden and weight in {self.dtype} expected, got {hidden.dtype} and {weight.dtype}")
-        if tuple(weight.shape) != (self.vocab, self.dim) or weight.device != self.device or weight.stride(1) != 1:
-            raise ValueError(f"weight: rows of [{self.vocab}, {self.dim}] on {self.device} expected, got {tuple(weight.shape)}, strides {weight.stride()}, on {weight.device}")
-        lead = hidden.shape[:-1]
+        strides = weight.stride()
+        if weight.shape != (self.vocab, self.dim) or weight.device != self.device or strides[1] != 1:
+            raise ValueError(f"weight: rows of [{self.vocab}, {self.dim}] on {self.device} expected, got {tuple(weight.shape)}, strides {strides}, on {weight.device}")
+        lead, t = hidden.shape[:-1], None
         if logits is None:
             k, _ = self._tokens(targets, "targets", lead)
-            return h, n, lead, k, None
-        k, _ = self._tokens(targets, "index", lead, targets.shape[-1] if targets.dim() else 1)
-        return h, n, lead, k, self._batch(logits, targets.shape[-1], "logits", lead)[0]
-
-    def _stride(self, weight):
-        return weight.stride(0) if self.vocab > 1 else self.dim
+        else:
+            top = targets.shape[-1] if targets.dim() else 1
+            k, _ = self._tokens(targets, "index", lead, top)
+            t, _ = self._batch(logits, top, "logits", lead)
+        return h, n, lead, k, t, weight.data_ptr(), strides[0] if self.vocab > 1 else self.dim
 
     def _forward(self, hidden, weight, targets, logits, temperature, loss, lse, stream):
-        h, n, lead, k, t = self._inputs(hidden, weight, targets, logits)
-        if loss is None:
-            loss = self._empty(lead, self.torch.float32, stream)
-        if lse is None:
-            lse = self._empty(lead, self.torch.float32, stream)
-        p, q = self._per_token(loss, lead, "loss"), self._per_token(lse, lead, "lse")
-        s = self._on(stream, [hidden, weight, targets, logits, loss, lse])
-        self._done(self._lib.co3_token_loss_forward(self.handle, h, weight.data_ptr(), self._stride(weight), k, t, temperature, n, p, q, s),
-                   "co3_token_loss_forward", [loss, lse])
+        h, n, lead, k, t, w, stride = self._inputs(hidden, weight, targets, logits)
+        given = loss, lse
+        loss, p = self._output(loss, lead, "loss", stream)
+        lse, q = self._output(lse, lead, "lse", stream)
+        s = self._on(stream, (hidden, weight, targets, logits, loss, lse))
+        rc = self._lib.co3_token_loss_forward(self.handle, h, w, stride, k, t, temperature, n, p, q, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_token_loss_forward")
+        self._changed(*given)
         return loss, lse
 
     def _backward(self, hidden, weight, targets, logits, temperature, lse, dloss, scale, dhidden, dweight, accumulate, want_dhidden, stream):
-        h, n, lead, k, t = self._inputs(hidden, weight, targets, logits)
+        h, n, lead, k, t, w, stride = self._inputs(hidden, weight, targets, logits)
         p = self._per_token(lse, lead, "lse")
         q = None if dloss is None else self._per_token(dloss, lead, "dloss")
-        if dhidden is None and want_dhidden:
-            dhidden = self._empty(hidden.shape, self.dtype, stream)
-        o = None if dhidden is None else self._batch(dhidden, self.dim, "dhidden", lead)[0]
-        w = None if dweight is None else self._grad(dweight, self.vocab * self.dim, accumulate, "dweight")
-        s = self._on(stream, [hidden, weight, targets, logits, lse, dloss, dhidden, dweight])
-        self._done(self._lib.co3_token_loss_backward(self.handle, h, weight.data_ptr(), self._stride(weight), k, t, temperature, n, p, q, scale, o, w, s),
-                   "co3_token_loss_backward", [x for x in (dhidden, dweight) if x is not None])
+        given, o = dhidden, None
+        if dhidden is not None:
+            o, _ = self._batch(dhidden, self.dim, "dhidden", lead)
+        elif want_dhidden:
+            dhidden = self._new(hidden.shape, self.dtype, stream)
+            o = self._own_batch(dhidden, self.dim, n)
+        d = None if dweight is None else self._grad(dweight, self.vocab * self.dim, accumulate, "dweight")
+        s = self._on(stream, (hidden, weight, targets, logits, lse, dloss, dhidden, dweight))
+        rc = self._lib.co3_token_loss_backward(self.handle, h, w, stride, k, t, temperature, n, p, q, scale, o, d, s)
+        if rc != OK:
+            raise Co3Error(rc, "co3_token_loss_backward")
+        self._changed(given, dweight)
         return dhidden

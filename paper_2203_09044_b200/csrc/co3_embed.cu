@@ -1,17 +1,19 @@
 // Embedding lookup, and its gradient by sorted tokens (co3_embed_*).
 //
 // Gradient, three kernels: (1) a cluster of thread blocks per user sorts the user's tokens with their places by radix, stably, while
-// the other SMs write the zeros of the table's gradient; (2) warps take 32 sorted places and 256 columns each, add the rows of equal
-// tokens in their order and write a token's row where its run ends within the 32; (3) what runs longer than that left is joined, in
-// order again.  No sum depends on the order of an atomic.
+// the other SMs write the zeros of the table's gradient; (2) warps take 32 sorted places each, add the rows of equal tokens in their
+// order and write a token's row where its run ends; a run that goes on into the next 32 places is finished by the warp in whose places it
+// began; (3) runs that go on for longer are added by parts, and these are joined, in order again.  No sum depends on the order of an atomic.
 #include "co3_ops.cuh"
 
 namespace {
 
-constexpr int SORT_THREADS = 1024, SORT_WARPS = 32, SORT_CLUSTER = 8;
+constexpr int SORT_THREADS = 1024, SORT_WARPS = 32, SORT_CLUSTER = 8, SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
+constexpr int SORT_SHARED = SORT_WARPS * SORT_BINS * 4;
+constexpr int HELD = 8;                       // keys of a lane that are loaded at once, and kept for both walks where there are no more
 constexpr int SORT_ALONE = 4096;              // tokens of a user that one thread block sorts by itself
 constexpr int RUN = 32;                       // sorted places of a warp
-constexpr int SLAB = 256;                     // columns of a warp: eight to a lane
+constexpr int SLAB = 256;                     // columns of a thread block that joins parts
 constexpr int PIECE = 1024;                   // columns of a row that a warp looks up at a time
 constexpr int JOIN_WARPS = 8;
 
@@ -94,7 +96,7 @@ struct SortArgs {
     int64_t vocab;
     uint32_t n_tokens, pitch;                 // of a user's part of the arrays
     int users, cluster, passes, digit_bits;
-    uint32_t *key[2], *place[2];              // [users][pitch]; the sorted ones end in [passes & 1]
+    uint2* sorted[2];                         // [users][pitch] key and place; they end in [passes & 1]
     uint32_t* n_valid;                        // [users]
     uint32_t* n_long;                         // runs that are longer than a warp's part: counted by the next kernel
     OpsStatus* status;
@@ -113,37 +115,55 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Zeros for the users' parts, by all fill blocks together; a part may begin and end at any element.
-__device__ void fill_zeros(const SortArgs& a, uint32_t block, uint32_t blocks) {
-    constexpr int64_t CHUNK = 64 * 1024;
-    const int64_t per_user = (a.zero_bytes + 15 + CHUNK - 1) / CHUNK, all = per_user * a.users;
-    for (int64_t i = block; i < all; i += blocks) {
-        const int64_t user = i / per_user, j = i - user * per_user;
-        uint8_t* const begin = a.zero + user * a.zero_stride, *const end = begin + a.zero_bytes;
-        uint8_t* const whole = (uint8_t*)((uintptr_t)begin & ~(uintptr_t)15);       // chunks count from here
-        uint8_t *p = whole + j * CHUNK, *q = p + CHUNK;
-        if (q > end) q = end;
-        if (p < begin) {                      // the first chunk's bytes before the first whole 16
-            uint8_t* const edge = whole + 16 < q ? whole + 16 : q;
-            for (uint8_t* b = begin + 2 * threadIdx.x; b < edge; b += 2 * SORT_THREADS) *(uint16_t*)b = 0;
-            p = whole + 16;
-        }
-        if (p >= q) continue;
-        const int64_t words = (q - p) / 16;
-        for (int64_t w = threadIdx.x; w < words; w += SORT_THREADS) ((uint4*)p)[w] = make_uint4(0, 0, 0, 0);
-        for (uint8_t* b = p + words * 16 + 2 * threadIdx.x; b < q; b += 2 * SORT_THREADS) *(uint16_t*)b = 0;
+// Zeros for chunk `number` of the users' parts, counted over the users; a part may begin and end at any element.  A chunk each to blocks
+// that come and go: 786 MB in 108 us, 7.3 TB/s; the same chunks dealt out to blocks that stay 129 us, since not all SMs store equally fast.
+constexpr int FILL_EACH = 4;
+constexpr int64_t FILL_CHUNK = FILL_EACH * SORT_THREADS * 32;
+__host__ __device__ inline int64_t fill_chunks(int64_t bytes) { return (bytes + 31 + FILL_CHUNK - 1) / FILL_CHUNK; }      // of a user
+__device__ void fill_zeros(const SortArgs& a, int64_t number) {
+    const int64_t per_user = fill_chunks(a.zero_bytes), user = number / per_user, j = number - user * per_user;
+    if (user >= a.users) return;
+    uint8_t* const begin = a.zero + user * a.zero_stride, *const end = begin + a.zero_bytes;
+    uint8_t* const whole = (uint8_t*)((uintptr_t)begin & ~(uintptr_t)31);           // chunks count from here
+    uint8_t *p = whole + j * FILL_CHUNK, *q = p + FILL_CHUNK;
+    if (p >= begin && q <= end) {
+#pragma unroll
+        for (int i = 0; i < FILL_EACH; ++i)
+            asm volatile("st.global.v8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" :: "l"(p + (i * SORT_THREADS + threadIdx.x) * 32), "r"(0) : "memory");
+        return;
     }
+    if (q > end) q = end;
+    if (p < begin) {                          // the first chunk's bytes before the first whole 32
+        uint8_t* const edge = whole + 32 < q ? whole + 32 : q;
+        for (uint8_t* b = begin + 2 * threadIdx.x; b < edge; b += 2 * SORT_THREADS) *(uint16_t*)b = 0;
+        p = whole + 32;
+    }
+    if (p >= q) return;
+    const int64_t words = (q - p) / 16;
+    for (int64_t w = threadIdx.x; w < words; w += SORT_THREADS) ((uint4*)p)[w] = make_uint4(0, 0, 0, 0);
+    for (uint8_t* b = p + words * 16 + 2 * threadIdx.x; b < q; b += 2 * SORT_THREADS) *(uint16_t*)b = 0;
+}
+
+// The lanes whose digits (of `bits` bits; lanes that are not here have the bit above set) are this lane's.
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits) {
+    uint32_t same = 0xffffffffu;
+    for (int b = 0; b <= bits; ++b) {
+        const bool set = digit >> b & 1;
+        const uint32_t with = __ballot_sync(0xffffffffu, set);
+        same &= set ? with : ~with;
+    }
+    return same;
 }
 
 __global__ void __launch_bounds__(SORT_THREADS, 2) sort_kernel(const __grid_constant__ SortArgs a) {
-    __shared__ uint32_t hist[SORT_WARPS][256];
-    __shared__ uint32_t totals[256 + 1], base[256], warp_sums[8];
+    extern __shared__ uint32_t hist[];        // [SORT_WARPS][bins]
+    __shared__ uint32_t totals[SORT_BINS + 1], base[SORT_BINS], warp_sums[SORT_BINS / 32];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t user = blockIdx.x / a.cluster, rank = blockIdx.x - user * a.cluster;
     let_next_start();
     wait_for_previous();
     if (user >= (uint32_t)a.users) {
-        fill_zeros(a, blockIdx.x - a.users * a.cluster, gridDim.x - a.users * a.cluster);
+        fill_zeros(a, (int64_t)blockIdx.x - a.users * a.cluster);
         return;
     }
     if (blockIdx.x == 0 && tid == 0) *a.n_long = 0;
@@ -153,79 +173,106 @@ __global__ void __launch_bounds__(SORT_THREADS, 2) sort_kernel(const __grid_cons
     const uint32_t begin = first < n ? (uint32_t)first : n, end = first + per_warp < n ? (uint32_t)(first + per_warp) : n;
     const uint32_t bins = 1u << a.digit_bits;
     const uint32_t below = (1u << lane) - 1u;
+    uint32_t* const mine = hist + warp * bins;
     for (int pass = 0; pass < a.passes; ++pass) {
-        const uint32_t *key_in = a.key[pass & 1] + (int64_t)user * a.pitch, *place_in = a.place[pass & 1] + (int64_t)user * a.pitch;
-        uint32_t *key_out = a.key[~pass & 1] + (int64_t)user * a.pitch, *place_out = a.place[~pass & 1] + (int64_t)user * a.pitch;
+        const uint2* in = a.sorted[pass & 1] + (int64_t)user * a.pitch;
+        uint2* out = a.sorted[~pass & 1] + (int64_t)user * a.pitch;
         const int shift = pass * a.digit_bits;
-        auto key_of = [&](uint32_t i) -> uint32_t {
-            if (pass) return __ldcg(key_in + i);
-            const int64_t token = token_at(a.tokens, user, i);
-            return token < 0 || token >= a.vocab ? (uint32_t)a.vocab : (uint32_t)token;      // those that are none come last
-        };
-        for (uint32_t b = lane; b < bins; b += 32) hist[warp][b] = 0;
-        if (tid == 0) totals[256] = 0;
-        __syncthreads();
-        uint32_t valid = 0;
-        for (uint32_t i = begin; i < end; i += 32) {
-            const bool here = i + lane < end;
-            const uint32_t key = here ? key_of(i + lane) : 0, digit = here ? key >> shift & (bins - 1) : 256;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            if (here && !(same & below)) hist[warp][digit] += __popc(same);
-            if (pass == 0) {
-                valid += __popc(__ballot_sync(0xffffffffu, here && key < (uint32_t)a.vocab));
-                if (here && key == (uint32_t)a.vocab && token_at(a.tokens, user, i + lane) >= a.vocab) {
-                    atomicAdd(&a.status->bad_tokens, 1ull);
-                    atomicOr(&a.status->flags, CO3_FLAG_TOKEN);
+        uint32_t held[HELD], place[HELD], nth[HELD], valid = 0;
+        // the next HELD * 32 keys of the warp; those of the first pass come from the tokens, and the ones that are none last
+        auto load = [&](uint32_t i0, bool count) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const uint32_t i = i0 + 32 * h + lane;
+                place[h] = i;
+                if (i >= end) held[h] = 0xFFFFFFFFu;
+                else if (pass) {
+                    const uint2 x = __ldcg(in + i);
+                    held[h] = x.x;
+                    place[h] = x.y;
+                } else {
+                    const int64_t token = token_at(a.tokens, user, i);
+                    held[h] = token < 0 || token >= a.vocab ? (uint32_t)a.vocab : (uint32_t)token;
+                    if (count && token >= a.vocab) { atomicAdd(&a.status->bad_tokens, 1ull); atomicOr(&a.status->flags, CO3_FLAG_TOKEN); }
+                    valid += count && held[h] != (uint32_t)a.vocab;
                 }
             }
-            __syncwarp();
+        };
+        for (uint32_t b = lane; b < bins; b += 32) mine[b] = 0;
+        if (tid == 0) totals[SORT_BINS] = 0;
+        __syncthreads();
+        for (uint32_t i0 = begin; i0 < end; i0 += 32 * HELD) {
+            load(i0, true);
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                if (i0 + 32 * h >= end) break;
+                const bool here = i0 + 32 * h + lane < end;
+                const uint32_t digit = here ? held[h] >> shift & (bins - 1) : bins, same = same_digit(digit, a.digit_bits);
+                const uint32_t ahead = here ? mine[digit] : 0;
+                nth[h] = ahead + __popc(same & below);
+                __syncwarp();
+                if (here && !(same & below)) mine[digit] = ahead + __popc(same);
+                __syncwarp();
+            }
         }
-        if (pass == 0 && lane == 0 && valid) atomicAdd(&totals[256], valid);
+        if (pass == 0) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) valid += __shfl_xor_sync(0xffffffffu, valid, o);
+            if (lane == 0 && valid) atomicAdd(&totals[SORT_BINS], valid);
+        }
         __syncthreads();
         if (tid < bins) {                     // where each warp's part of a digit begins within the block's
             uint32_t s = 0;
 #pragma unroll 8
-            for (int w = 0; w < SORT_WARPS; ++w) { const uint32_t c = hist[w][tid]; hist[w][tid] = s; s += c; }
+            for (int w = 0; w < SORT_WARPS; ++w) { const uint32_t c = hist[w * bins + tid]; hist[w * bins + tid] = s; s += c; }
             totals[tid] = s;
         }
         if (a.cluster > 1) cluster_barrier();
         else __syncthreads();
         uint32_t all = 0, before = 0;
         if (tid < bins) {
-            for (int r = 0; r < a.cluster; ++r) {
-                const uint32_t c = a.cluster > 1 ? peer_word(shared_at(&totals[tid]), r) : totals[tid];
-                if (r < (int)rank) before += c;
-                all += c;
+            if (a.cluster == 1) all = totals[tid];
+            else {
+                uint32_t c[SORT_CLUSTER];
+#pragma unroll
+                for (int r = 0; r < SORT_CLUSTER; ++r) c[r] = peer_word(shared_at(&totals[tid]), r);
+#pragma unroll
+                for (int r = 0; r < SORT_CLUSTER; ++r) { if (r < (int)rank) before += c[r]; all += c[r]; }
             }
         }
-        if (pass == 0 && rank == 0 && tid == 256) {
+        if (pass == 0 && rank == 0 && tid == SORT_THREADS - 1) {
             uint32_t s = 0;
-            for (int r = 0; r < a.cluster; ++r) s += a.cluster > 1 ? peer_word(shared_at(&totals[256]), r) : totals[256];
+            for (int r = 0; r < a.cluster; ++r) s += a.cluster > 1 ? peer_word(shared_at(&totals[SORT_BINS]), r) : totals[SORT_BINS];
             a.n_valid[user] = s;
         }
         uint32_t up = all;                    // places of the smaller digits, over all blocks
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, up, o); if ((int)lane >= o) up += v; }
-        if (warp < 8 && lane == 31) warp_sums[warp] = up;
+        if (warp < SORT_BINS / 32 && lane == 31) warp_sums[warp] = up;
         __syncthreads();
         if (tid < bins) {
             for (uint32_t w = 0; w < warp; ++w) before += warp_sums[w];
             base[tid] = before + up - all;
         }
         __syncthreads();
-        for (uint32_t i = begin; i < end; i += 32) {
-            const bool here = i + lane < end;
-            const uint32_t key = here ? key_of(i + lane) : 0, digit = here ? key >> shift & (bins - 1) : 256;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            const uint32_t ahead = here ? hist[warp][digit] : 0;
-            __syncwarp();
-            if (here) {
-                if (!(same & below)) hist[warp][digit] = ahead + __popc(same);
-                const uint32_t to = base[digit] + ahead + __popc(same & below);
-                __stcg(key_out + to, key);
-                __stcg(place_out + to, pass ? __ldcg(place_in + i + lane) : i + lane);
+        const bool again = per_warp > 32 * HELD;          // the ranks of the last HELD * 32 keys alone are still there
+        for (uint32_t i0 = begin; i0 < end; i0 += 32 * HELD) {
+            if (again) load(i0, false);
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                if (i0 + 32 * h >= end) break;
+                const bool here = i0 + 32 * h + lane < end;
+                const uint32_t digit = here ? held[h] >> shift & (bins - 1) : bins;
+                uint32_t to = here ? base[digit] + mine[digit] : 0;
+                if (again) {
+                    const uint32_t same = same_digit(digit, a.digit_bits);
+                    __syncwarp();
+                    if (here && !(same & below)) mine[digit] += __popc(same);
+                    __syncwarp();
+                    to += __popc(same & below);
+                } else to += nth[h];
+                if (here) __stcg(out + to, make_uint2(held[h], place[h]));
             }
-            __syncwarp();
         }
         if (a.cluster > 1) cluster_barrier();  // also: nobody reads another block's totals any more
         else __syncthreads();
@@ -236,7 +283,8 @@ __global__ void __launch_bounds__(SORT_THREADS, 2) sort_kernel(const __grid_cons
 struct SumArgs {
     const void* dout;
     int64_t gu, gt;
-    const uint32_t *key, *place, *n_valid;
+    const uint2* sorted;                      // [users][pitch] key and place
+    const uint32_t* n_valid;
     uint32_t pitch, chunks;                   // of a user
     uint32_t* n_long;
     uint32_t* long_runs;                      // [users * chunks]: user * chunks + chunk in which a longer run begins
@@ -247,31 +295,81 @@ struct SumArgs {
     float scale;
 };
 
-template <class T> __device__ __forceinline__ void put_sum(typename T::type* p, float x, bool add) {
-    *p = T::put(add ? T::get(*p) + x : x);
+// How a warp takes a row: WIDE eight neighbouring columns a lane, 16 bytes of 16-bit numbers; PAIRS two neighbouring ones, for few rows, and
+// for gradients that begin anywhere; SINGLES every 32nd, two of them, for rows that begin anywhere.
+enum Take { WIDE, PAIRS, SINGLES };
+template <int TAKE> constexpr int PER_LANE = TAKE == WIDE ? 8 : 2;
+template <int TAKE> constexpr int COLUMNS = 32 * PER_LANE<TAKE>;
+
+__device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {      // two sums in one instruction
+    asm("{\n\t.reg .b64 s, x;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 x, {%2, %3};\n\tadd.rn.f32x2 s, s, x;\n\tmov.b64 {%0, %1}, s;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
-// VEC: a lane has eight neighbouring columns, else every 32nd.
-template <class B, bool VEC> __device__ __forceinline__ void put_sums(const SumArgs& a, int64_t user, uint32_t token, int column, const float* s) {
+
+template <class A, int TAKE> struct RowPart {
+    typedef typename A::type type;
+    uint4 wide[TAKE == WIDE ? 8 / A::EACH : 1];
+    alignas(2 * sizeof(type)) type two[2];
+    __device__ __forceinline__ void load(const type* p, int columns) {        // columns: that are left from the lane's first
+        if (TAKE == WIDE) {
+            if (columns > 0)
+#pragma unroll
+                for (int i = 0; i < 8 / A::EACH; ++i) wide[i] = __ldcs((const uint4*)p + i);
+        } else if (TAKE == PAIRS) {
+            if (columns > 0) {
+                if (sizeof(type) == 2) *(uint32_t*)two = __ldcs((const uint32_t*)p);
+                else *(uint2*)two = __ldcs((const uint2*)p);
+            }
+        } else {
+            if (columns > 0) two[0] = p[0];
+            if (columns > 32) two[1] = p[32];
+        }
+    }
+    __device__ __forceinline__ void add(float* s) const {
+        if (TAKE == WIDE) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8 / A::EACH; ++i) A::unpack(wide[i], x + i * A::EACH);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) add_pair(s[k], s[k + 1], x[k], x[k + 1]);
+        } else { s[0] += A::get(two[0]); s[1] += A::get(two[1]); }
+    }
+};
+
+struct Sum8 { float x[8]; };
+
+// A run's sum: to the gradient, or (slot >= 0) to its part's place.  Not inlined: the loop over rows has eight of these.
+template <class B, int TAKE>
+__device__ __noinline__ void put_run(const SumArgs& a, uint32_t at, uint32_t user, uint32_t token, int slot, int column, Sum8 s) {
+    constexpr int N = PER_LANE<TAKE>, STEP = TAKE == SINGLES ? 32 : 1;
+    if (slot >= 0) {
+        float* p = a.part + ((int64_t)at * 2 + slot) * a.dim + column;
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (column + STEP * k < a.dim) p[STEP * k] = s.x[k];
+        return;
+    }
     typename B::type* p = (typename B::type*)a.to.data + user * a.to.user_stride + (int64_t)token * a.dim + column;
-    if (VEC) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) s.x[k] *= a.scale;
+    if (TAKE == WIDE) {                       // the gradient's rows begin at multiples of 16 bytes
         if (column >= a.dim) return;
-        float x[8];
+        if (a.to.accumulate) {
+            float o[8];
+            load8<B>(p, o);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
-        if (a.to.accumulate) load8<B>(p, x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = a.to.accumulate ? x[k] + s[k] * a.scale : s[k] * a.scale;
-        store8<B>(p, x);
+            for (int k = 0; k < 8; ++k) s.x[k] += o[k];
+        }
+        store8<B>(p, s.x);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (column + 32 * k < a.dim) put_sum<B>(p + 32 * k, s[k] * a.scale, a.to.accumulate);
+        for (int k = 0; k < N; ++k)
+            if (column + STEP * k < a.dim) p[STEP * k] = B::put(a.to.accumulate ? B::get(p[STEP * k]) + s.x[k] : s.x[k]);
     }
 }
 
-template <class A, class B, bool VEC>
+template <class A, class B, int TAKE>
 __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs a) {
-    constexpr int AT_ONCE = 8;                // rows whose loads are in flight
+    constexpr int AT_ONCE = 4;                // rows whose loads are in flight while as many are added (64k tokens: 4 take 204 us, 8 in more registers 210)
+    constexpr uint32_t NONE = 0xFFFFFFFFu;
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     let_next_start();
@@ -281,99 +379,102 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     const int slab = (int)(item - (int64_t)at * a.slabs);
     const uint32_t user = at / a.chunks, chunk = at - user * a.chunks, n = a.n_valid[user], i0 = chunk * RUN;
     if (i0 >= n) return;
-    const int count = n - i0 < RUN ? (int)(n - i0) : RUN;
-    const uint32_t* keys = a.key + (int64_t)user * a.pitch + i0;
-    const uint32_t key = lane < count ? keys[lane] : 0xFFFFFFFFu, place = lane < count ? a.place[(int64_t)user * a.pitch + i0 + lane] : 0;
-    const uint32_t before = i0 ? keys[-1] : 0xFFFFFFFFu, after = i0 + RUN < n ? keys[RUN] : 0xFFFFFFFFu;
-    const int column = slab * SLAB + (VEC ? lane * 8 : lane);
+    const uint2* sorted = a.sorted + (int64_t)user * a.pitch;
+    auto at_place = [&](uint32_t i) { return i < n ? sorted[i] : make_uint2(NONE, 0); };
+    const uint2 one = at_place(i0 + lane), two = at_place(i0 + RUN + lane);
+    const uint32_t key = one.x, key2 = two.x, far = i0 > RUN ? sorted[i0 - RUN - 1].x : NONE, before = i0 ? sorted[i0 - 1].x : NONE, beyond = at_place(i0 + 2 * RUN).x;
+    const uint32_t head = __shfl_sync(0xffffffffu, key, 0), tail = __shfl_sync(0xffffffffu, key, RUN - 1), next = __shfl_sync(0xffffffffu, key2, 0);
+    int total = n - i0 < RUN ? (int)(n - i0) : RUN, skip = 0, led = 0, last_slot = -1;       // led: places of a run that is added by parts
+    const bool began_before = before == head, all_one = began_before && tail == head;
+    if (began_before) {
+        const int same = __popc(__ballot_sync(0xffffffffu, key == head));
+        if (far == head || (all_one && next == head)) led = same;
+        else skip = same;                     // the warp before finishes it
+    }
+    if (next == tail && next != NONE && !all_one) {       // the last run goes on, and began here
+        const int more = __popc(__ballot_sync(0xffffffffu, key2 == tail));
+        if (more == RUN && beyond == tail) last_slot = 1;
+        else total = RUN + more;
+    }
+    if (skip >= total) return;
+    if (last_slot == 1 && slab == 0 && lane == 0) a.long_runs[atomicAdd(a.n_long, 1u)] = at;
+    // where a run ends: bit i of the 64 places
+    const uint32_t after = __shfl_down_sync(0xffffffffu, key, 1), after2 = __shfl_down_sync(0xffffffffu, key2, 1);
+    const uint64_t ends = (uint64_t)__ballot_sync(0xffffffffu, key2 != after2) << 32 | __ballot_sync(0xffffffffu, key != (lane == 31 ? next : after)) | 1ull << (total - 1);
+    const int column = slab * COLUMNS<TAKE> + (TAKE == SINGLES ? lane : lane * PER_LANE<TAKE>);
     const typename A::type* rows = (const typename A::type*)a.dout + user * a.gu + column;
-    float sum[8];
+    Sum8 sum;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
-    bool first = true;                        // still in the chunk's first run
-    for (int e0 = 0; e0 < count; e0 += AT_ONCE) {
-        float x[AT_ONCE][8];
-#pragma unroll
-        for (int e = 0; e < AT_ONCE; ++e) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[e][k] = 0.0f;
-            const uint32_t t = __shfl_sync(0xffffffffu, place, (e0 + e) & 31);
-            if (e0 + e < count) {
-                const typename A::type* row = rows + (int64_t)t * a.gt;
-                if (VEC) { if (column < a.dim) load8<A>(row, x[e]); }
-                else
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) if (column + 32 * k < a.dim) x[e][k] = A::get(row[32 * k]);
-            }
-        }
+    for (int k = 0; k < 8; ++k) sum.x[k] = 0.0f;
+    RowPart<A, TAKE> now[AT_ONCE], coming[AT_ONCE];
+    auto fetch = [&](RowPart<A, TAKE>(&x)[AT_ONCE], int e0) {
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) {
-            if (e0 + e >= count) break;
-            const uint32_t mine = __shfl_sync(0xffffffffu, key, e0 + e);
-            const uint32_t next = e0 + e + 1 < count ? __shfl_sync(0xffffffffu, key, (e0 + e + 1) & 31) : after;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += x[e][k];
-            const bool last = e0 + e + 1 == count;
-            if (next == mine && !last) continue;
-            const bool began_before = first && mine == before, goes_on = last && next == mine;
-            if (began_before || goes_on) {
-                float* part = a.part + ((int64_t)at * 2 + (began_before ? 0 : 1)) * a.dim + column;
-                if (VEC) { if (column < a.dim) store8<OF32>(part, sum); }
-                else
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) if (column + 32 * k < a.dim) part[32 * k] = sum[k];
-                if (!began_before && slab == 0 && lane == 0) a.long_runs[atomicAdd(a.n_long, 1u)] = at;
-            } else put_sums<B, VEC>(a, user, mine, column, sum);
-            first = false;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+            const uint32_t place = __shfl_sync(0xffffffffu, e0 + e < RUN ? one.y : two.y, (e0 + e) & 31);
+            if (e0 + e < total) x[e].load(rows + (int64_t)place * a.gt, a.dim - column);
         }
+    };
+    fetch(now, skip);
+    for (int e0 = skip; e0 < total; e0 += AT_ONCE) {
+        fetch(coming, e0 + AT_ONCE);
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const int i = e0 + e;
+            if (i >= total) break;
+            now[e].add(sum.x);
+            if (!(ends >> i & 1)) continue;
+            const uint32_t mine = __shfl_sync(0xffffffffu, i < RUN ? key : key2, i & 31);
+            put_run<B, TAKE>(a, at, user, mine, i < led ? 0 : i + 1 == total ? last_slot : -1, column, sum);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum.x[k] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) now[e] = coming[e];
     }
 }
 
-// The runs longer than a chunk, each by a thread block: its warps add a stretch of the chunks each, the stretches are added in order.
-template <class B, bool VEC>
+// The runs that were added by parts, each by a thread block: its warps add a stretch of the parts each, the stretches are added in order.
+template <class B>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const __grid_constant__ SumArgs a) {
     __shared__ float sh[JOIN_WARPS][SLAB];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slabs = (a.dim + SLAB - 1) / SLAB;
     let_next_start();
     wait_for_previous();
-    const int64_t items = (int64_t)*a.n_long * a.slabs;
+    const int64_t items = (int64_t)*a.n_long * slabs;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t at = a.long_runs[item / a.slabs];
-        const int slab = (int)(item % a.slabs);
+        const uint32_t at = a.long_runs[item / slabs];
+        const int column = (int)(item % slabs) * SLAB;
         const uint32_t user = at / a.chunks, chunk = at - user * a.chunks, n = a.n_valid[user];
-        const uint32_t* keys = a.key + (int64_t)user * a.pitch;
-        const uint32_t token = keys[chunk * RUN + RUN - 1];
-        uint32_t lo = (chunk + 1) * RUN, hi = n;          // the run ends before the first larger key
+        const uint2* sorted = a.sorted + (int64_t)user * a.pitch;
+        const uint32_t token = sorted[chunk * RUN + RUN - 1].x;
+        uint32_t lo = (chunk + 1) * RUN, hi = n;          // the run ends before the first larger key, among lo .. hi: 32 looks at once
         while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (keys[mid] == token) lo = mid + 1; else hi = mid;
+            const uint32_t step = (hi - lo + 31) / 32, i = lo + lane * step;
+            const int same = __popc(__ballot_sync(0xffffffffu, i < hi && sorted[i].x == token));
+            if (!same) break;
+            hi = hi - lo < same * step ? hi : lo + same * step;
+            lo += (same - 1) * step + 1;
         }
         const uint32_t parts = (lo - 1) / RUN - chunk + 1, each = (parts + JOIN_WARPS - 1) / JOIN_WARPS;
         const uint32_t p0 = warp * each < parts ? warp * each : parts, p1 = p0 + each < parts ? p0 + each : parts;
-        const int column = slab * SLAB + lane;
         float s[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] = 0.0f;
 #pragma unroll 4
         for (uint32_t p = p0; p < p1; ++p) {
-            const float* part = a.part + (((int64_t)at + p) * 2 + (p ? 0 : 1)) * a.dim + column;
+            const float* part = a.part + (((int64_t)at + p) * 2 + (p ? 0 : 1)) * a.dim + column + lane;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (column + 32 * k < a.dim) s[k] += part[32 * k];
+            for (int k = 0; k < 8; ++k) if (column + lane + 32 * k < a.dim) s[k] += part[32 * k];
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) sh[warp][lane + 32 * k] = s[k];
         __syncthreads();
-        if (warp == 0) {
-            float x[8];
-            const int c0 = VEC ? lane * 8 : lane, step = VEC ? 1 : 32;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] = sh[0][c0 + k * step];
-                for (int w = 1; w < JOIN_WARPS; ++w) x[k] += sh[w][c0 + k * step];
-            }
-            put_sums<B, VEC>(a, user, token, slab * SLAB + c0, x);
+        float x = 0.0f;                       // a column a thread
+        for (int w = 0; w < JOIN_WARPS; ++w) x += sh[w][threadIdx.x];
+        if (column + (int)threadIdx.x < a.dim) {
+            typename B::type* p = (typename B::type*)a.to.data + user * a.to.user_stride + (int64_t)token * a.dim + column + threadIdx.x;
+            x *= a.scale;
+            *p = B::put(a.to.accumulate ? B::get(*p) + x : x);
         }
         __syncthreads();
     }
@@ -387,7 +488,8 @@ struct co3_embed {
     uint32_t pitch, chunks;
     void* slab;
     OpsStatus* status;
-    uint32_t *key[2], *place[2], *n_valid, *n_long, *long_runs;
+    uint2* sorted[2];
+    uint32_t *n_valid, *n_long, *long_runs;
     float* part;
 };
 
@@ -413,18 +515,19 @@ extern "C" int co3_embed_create(co3_embed** out, int64_t vocab, int64_t dim, int
     if (rc == CO3_OK) {
         size_t at = 0;
         auto part = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-        const size_t words = 4 * (size_t)h->pitch * n_users, runs = (size_t)h->chunks * n_users;
-        const size_t o_status = part(sizeof(OpsStatus)), o_key = part(words), o_key2 = part(words), o_place = part(words), o_place2 = part(words);
+        const size_t pairs = 8 * (size_t)h->pitch * n_users, runs = (size_t)h->chunks * n_users;
+        const size_t o_status = part(sizeof(OpsStatus)), o_one = part(pairs), o_two = part(pairs);
         const size_t o_valid = part(4 * (size_t)n_users), o_count = part(4), o_long = part(4 * runs), o_part = part(runs * 2 * dim * 4);
         if (cudaMalloc(&h->slab, at) != cudaSuccess) { h->slab = nullptr; rc = CO3_ENOMEM; }
         else {
             char* base = (char*)h->slab;
             h->status = (OpsStatus*)(base + o_status);
-            h->key[0] = (uint32_t*)(base + o_key); h->key[1] = (uint32_t*)(base + o_key2);
-            h->place[0] = (uint32_t*)(base + o_place); h->place[1] = (uint32_t*)(base + o_place2);
+            h->sorted[0] = (uint2*)(base + o_one); h->sorted[1] = (uint2*)(base + o_two);
             h->n_valid = (uint32_t*)(base + o_valid); h->n_long = (uint32_t*)(base + o_count); h->long_runs = (uint32_t*)(base + o_long);
             h->part = (float*)(base + o_part);
-            if (cudaMemset(h->status, 0, sizeof(OpsStatus)) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) rc = CO3_ECUDA;
+            // the sort's counts in shared memory
+            if (cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SHARED) != cudaSuccess) rc = CO3_ECUDA;
+            else if (cudaMemset(h->status, 0, sizeof(OpsStatus)) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) rc = CO3_ECUDA;
         }
     }
     if (rc != CO3_OK) { (void)cudaGetLastError(); co3_embed_destroy(h); return rc; }
@@ -451,20 +554,23 @@ template <class A> int lookup_to(co3_embed* h, int type, bool vec, const LookupA
     if (type == CO3_BF16) return lookup_of<A, OBf16>(h, vec, a, grid, st);
     return lookup_of<A, OF16>(h, vec, a, grid, st);
 }
-template <class A, class B> int sums_of(co3_embed* h, bool vec, const SumArgs& a, cudaStream_t st) {
+template <class A, class B> int sums_of(co3_embed* h, int take, SumArgs a, cudaStream_t st) {
+    const int columns = take == WIDE ? COLUMNS<WIDE> : COLUMNS<PAIRS>;
+    a.slabs = (a.dim + columns - 1) / columns;
+    a.items = (int64_t)h->users * a.chunks * a.slabs;
+    if ((a.items + 7) / 8 > 0x7FFFFFFF) return CO3_ELIMIT;
     const dim3 grid((unsigned)((a.items + 7) / 8));
-    const int64_t runs = (int64_t)h->users * a.chunks * a.slabs, places = (int64_t)h->sms * 4;
-    const dim3 joins((unsigned)(runs < places ? runs : places));
-    int rc = vec ? launch_early(&h->launches, sum_kernel<A, B, true>, grid, 256, 0, 1, st, a)
-                 : launch_early(&h->launches, sum_kernel<A, B, false>, grid, 256, 0, 1, st, a);
-    if (rc != CO3_OK || a.chunks == 1) return rc;         // a run within one chunk needs no join
-    return vec ? launch_early(&h->launches, join_kernel<B, true>, joins, 32 * JOIN_WARPS, 0, 1, st, a)
-               : launch_early(&h->launches, join_kernel<B, false>, joins, 32 * JOIN_WARPS, 0, 1, st, a);
+    int rc = take == WIDE ? launch_early(&h->launches, sum_kernel<A, B, WIDE>, grid, 256, 0, 1, st, a)
+             : take == PAIRS ? launch_early(&h->launches, sum_kernel<A, B, PAIRS>, grid, 256, 0, 1, st, a)
+                             : launch_early(&h->launches, sum_kernel<A, B, SINGLES>, grid, 256, 0, 1, st, a);
+    if (rc != CO3_OK || a.chunks <= 2) return rc;         // a run that is added by parts lies in three chunks at least
+    const int64_t runs = (int64_t)h->users * a.chunks * ((a.dim + SLAB - 1) / SLAB), places = (int64_t)h->sms * 4;
+    return launch_early(&h->launches, join_kernel<B>, dim3((unsigned)(runs < places ? runs : places)), 32 * JOIN_WARPS, 0, 1, st, a);
 }
-template <class A> int sums_to(co3_embed* h, bool vec, const SumArgs& a, cudaStream_t st) {
-    if (a.to.type == CO3_F32) return sums_of<A, OF32>(h, vec, a, st);
-    if (a.to.type == CO3_BF16) return sums_of<A, OBf16>(h, vec, a, st);
-    return sums_of<A, OF16>(h, vec, a, st);
+template <class A> int sums_to(co3_embed* h, int take, const SumArgs& a, cudaStream_t st) {
+    if (a.to.type == CO3_F32) return sums_of<A, OF32>(h, take, a, st);
+    if (a.to.type == CO3_BF16) return sums_of<A, OBf16>(h, take, a, st);
+    return sums_of<A, OF16>(h, take, a, st);
 }
 
 }  // namespace
@@ -502,29 +608,34 @@ extern "C" int co3_embed_backward(co3_embed* h, const co3_array* dout, const co3
     memset(&s, 0, sizeof(s));
     s.tokens = tokens_of(tokens); s.vocab = h->vocab; s.n_tokens = (uint32_t)n_tokens; s.pitch = h->pitch; s.users = h->users;
     s.cluster = n_tokens <= SORT_ALONE ? 1 : SORT_CLUSTER;
-    s.passes = (bits + 7) / 8; s.digit_bits = (bits + s.passes - 1) / s.passes;
-    for (int i = 0; i < 2; ++i) { s.key[i] = h->key[i]; s.place[i] = h->place[i]; }
+    s.passes = (bits + SORT_BITS - 1) / SORT_BITS; s.digit_bits = (bits + s.passes - 1) / s.passes;
+    s.sorted[0] = h->sorted[0]; s.sorted[1] = h->sorted[1];
     s.n_valid = h->n_valid; s.n_long = h->n_long; s.status = h->status;
     int64_t fill = 0;
     if (!dtable->accumulate) {
         s.zero = (uint8_t*)dtable->data; s.zero_stride = dtable->user_stride * width; s.zero_bytes = h->vocab * h->dim * width;
-        const int64_t chunks = h->users * (s.zero_bytes / 65536 + 1);
-        fill = chunks < 2 * h->sms ? chunks : 2 * h->sms;
-        fill = (fill + s.cluster - 1) / s.cluster * s.cluster;
+        fill = (h->users * fill_chunks(s.zero_bytes) + s.cluster - 1) / s.cluster * s.cluster;
+        if (fill > 0x7FFF0000) return CO3_ELIMIT;
     }
-    int rc = launch_early(&h->launches, sort_kernel, dim3((unsigned)(h->users * s.cluster + fill)), SORT_THREADS, 0, s.cluster, st, s);
+    int rc = launch_early(&h->launches, sort_kernel, dim3((unsigned)(h->users * s.cluster + fill)), SORT_THREADS, SORT_SHARED, s.cluster, st, s);
     if (rc != CO3_OK || n_tokens == 0) return rc;
     SumArgs a;
     a.dout = dout->data; a.gu = dout->user_stride; a.gt = dout->token_stride;
-    a.key = h->key[s.passes & 1]; a.place = h->place[s.passes & 1]; a.n_valid = h->n_valid;
+    a.sorted = h->sorted[s.passes & 1]; a.n_valid = h->n_valid;
     a.pitch = h->pitch; a.chunks = (uint32_t)((n_tokens + RUN - 1) / RUN); a.n_long = h->n_long; a.long_runs = h->long_runs; a.part = h->part;
-    a.to = *dtable; a.dim = (int)h->dim; a.slabs = (int)((h->dim + SLAB - 1) / SLAB); a.items = (int64_t)h->users * a.chunks * a.slabs; a.scale = scale;
-    if ((a.items + 7) / 8 > 0x7FFFFFFF) return CO3_ELIMIT;
-    const bool vec = h->dim % 8 == 0 && rows_aligned(dout, h->users, n_tokens) && aligned_to(dtable->data, 16) &&
-                     (h->users == 1 || dtable->user_stride * width % 16 == 0);
-    if (dout->type == CO3_F32) return sums_to<OF32>(h, vec, a, st);
-    if (dout->type == CO3_BF16) return sums_to<OBf16>(h, vec, a, st);
-    return sums_to<OF16>(h, vec, a, st);
+    a.to = *dtable; a.dim = (int)h->dim; a.scale = scale;
+    // Eight columns a lane where both begin at whole 16 bytes and the warps are more than the device has places for; else two.
+    const int in = type_width(dout->type);
+    auto begins = [&](int bytes) {
+        return aligned_to(dout->data, bytes) && (n_tokens <= 1 || dout->token_stride * in % bytes == 0) && (h->users == 1 || dout->user_stride * in % bytes == 0);
+    };
+    int take = SINGLES;
+    if (h->dim % 2 == 0 && begins(2 * in)) take = PAIRS;
+    const int64_t warps = (int64_t)h->users * a.chunks * ((h->dim + COLUMNS<WIDE> - 1) / COLUMNS<WIDE>);
+    if (h->dim % 8 == 0 && begins(16) && aligned_to(dtable->data, 16) && (h->users == 1 || dtable->user_stride * width % 16 == 0) && warps >= (int64_t)h->sms * 16) take = WIDE;
+    if (dout->type == CO3_F32) return sums_to<OF32>(h, take, a, st);
+    if (dout->type == CO3_BF16) return sums_to<OBf16>(h, take, a, st);
+    return sums_to<OF16>(h, take, a, st);
 }
 
 extern "C" int co3_embed_status(co3_embed* h, uint32_t* flags, uint64_t* bad_tokens, int32_t clear) {

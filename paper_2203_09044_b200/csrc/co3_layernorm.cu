@@ -1,8 +1,9 @@
 // Layer norm forward and backward, with the reduction of the weight's and the bias' gradient per user (co3_layernorm_*).
 //
 // A row is held in the registers of TPR threads, E elements each, so that one read of it serves mean, variance and result: two
-// passes over registers, and the variance is that of differences.  Thread blocks stay and take row after row, with the weight in
-// registers; the next row's loads are in flight while a row is worked on.
+// passes over registers, and the variance is that of differences.  Thread blocks stay and take row after row.  What bounds the kernels is memory,
+// and what they need for it is bytes on their way: each thread copies its elements of the rows to come into shared memory of its own ahead
+// of time, which costs no registers and, since nobody else reads them, no barrier.
 #include "co3_ops.cuh"
 
 namespace {
@@ -28,195 +29,258 @@ struct LnBackward {
     co3_param_grad dweight, dbias;            // data null where not wanted
 };
 
-// Sum over the TPR threads of a row of K values each; `turn` counts the reductions of a thread block.
+// Sum over the TPR threads of a row of K values each; `turn` counts the reductions of these threads.
 template <int TPR, int K> __device__ __forceinline__ void row_sum(float (&x)[K], float (*sh)[32][K], int& turn) {
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = warp_sum_f32(x[k]);
     if (TPR == 32) return;
+    constexpr int W = TPR / 32;
+    const int warp = threadIdx.x >> 5, group = warp / W, first = group * W;
     float(*s)[K] = sh[turn & 1];              // two buffers: one barrier a reduction
     ++turn;
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
-        for (int k = 0; k < K; ++k) s[threadIdx.x >> 5][k] = x[k];
-    __syncthreads();
+        for (int k = 0; k < K; ++k) s[warp][k] = x[k];
+    asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "n"(TPR) : "memory");
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         float t = 0.0f;
-        if (TPR / 32 <= 8) {
+        if (W <= 8) {
 #pragma unroll
-            for (int w = 0; w < TPR / 32; ++w) t += s[w][k];
-        } else t = warp_sum_f32((threadIdx.x & 31) < TPR / 32 ? s[threadIdx.x & 31][k] : 0.0f);
+            for (int w = 0; w < W; ++w) t += s[first + w][k];
+        } else t = warp_sum_f32((threadIdx.x & 31) < W ? s[threadIdx.x & 31][k] : 0.0f);
         x[k] = t;
     }
 }
 
-// The elements that a thread holds of a row: E / V pieces of V neighbours, piece c at column (c TPR + t) V.  VEC: 16 bytes each,
-// else one element, for rows that begin anywhere or have an odd length.
-template <class T, bool VEC, int TPR, int E> struct Held {
-    static constexpr int V = VEC ? T::EACH : 1, N = E / V;
+// How rows are read: in whole 16 bytes; in words (f32 rows that begin anywhere, or of an odd length); element by element.
+enum Take { WHOLE, WORDS, SINGLES };
+
+// The elements that a thread holds of a row: E / V pieces of V neighbours, piece c at column (c TPR + t) V.  AHEAD: rows that are on
+// their way into shared memory while one is worked on (none element by element, where there is no such copy).
+template <class T, int TAKE, int TPR, int E> struct Held {
+    typedef typename T::type type;
+    static constexpr int V = TAKE == WHOLE ? T::EACH : 1, N = E / V, BYTES = V * sizeof(type);
+    static constexpr int THREADS = TPR >= 256 ? TPR : TPR == 32 && E >= 24 ? 128 : 256 / TPR * TPR, GROUPS = THREADS / TPR;
+    static constexpr int ROW = N * THREADS * BYTES;       // of a thread block, one row a group
+    static constexpr bool ASYNC = TAKE != SINGLES;
     static_assert(E % V == 0, "whole pieces");
     static __device__ __forceinline__ int column(int t, int c) { return (c * TPR + t) * V; }
-    typename std::conditional<VEC, uint4, typename T::type>::type raw[N];
-    __device__ __forceinline__ void load(const void* row, int t, int dim) {
+    // Begins to copy the thread's elements into its places of the slot, or reads them.
+    static __device__ __forceinline__ void send(uint8_t* slot, const type* row, int t, int dim) {
+        if constexpr (TAKE == SINGLES) return;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot) + threadIdx.x * BYTES;
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-            const int at = column(t, c);
-            if (at < dim) {
-                if constexpr (VEC) raw[c] = __ldcs((const uint4*)((const typename T::type*)row + at));
-                else raw[c] = ((const typename T::type*)row)[at];
-            } else {
-                if constexpr (VEC) raw[c] = make_uint4(0, 0, 0, 0);
-                else raw[c] = T::put(0.0f);
+        for (int c = 0; c < N; ++c)
+            if (column(t, c) < dim) {
+                if constexpr (TAKE == WHOLE) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + c * THREADS * BYTES), "l"(row + column(t, c)) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(to + c * THREADS * BYTES), "l"(row + column(t, c)) : "memory");
             }
-        }
     }
-    __device__ __forceinline__ void values(float* x) const {
+    // Pair j of the thread: elements 2j and 2j + 1, 0 beyond the row.
+    static __device__ __forceinline__ void take(const uint8_t* slot, const type* row, int t, int dim, Two* x) {
+        float f[E];
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            if constexpr (VEC) T::unpack(raw[c], x + c * V);
-            else x[c] = T::get(raw[c]);
+            const int at = column(t, c);
+            if constexpr (TAKE == WHOLE) {
+                const uint4 u = at < dim ? *(const uint4*)(slot + (c * THREADS + threadIdx.x) * BYTES) : make_uint4(0, 0, 0, 0);
+                T::unpack(u, f + c * V);
+            } else if constexpr (TAKE == WORDS) f[c] = at < dim ? *(const float*)(slot + (c * THREADS + threadIdx.x) * BYTES) : 0.0f;
+            else f[c] = at < dim ? T::get(row[at]) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) x[j] = Two(f[2 * j], f[2 * j + 1]);
+    }
+    static __device__ __forceinline__ void beyond(int t, int dim, float otherwise, Two* x) {
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) {
+            float a, b;
+            x[j].get(a, b);
+            const bool in_a = column(t, 2 * j / V) + 2 * j % V < dim, in_b = column(t, (2 * j + 1) / V) + (2 * j + 1) % V < dim;
+            x[j] = Two(in_a ? a : otherwise, in_b ? b : otherwise);
         }
     }
-    static __device__ __forceinline__ void store(void* row, int t, int dim, const float* x) {
+    static __device__ __forceinline__ void store(type* row, int t, int dim, const Two* x) {
+        float f[E];
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) x[j].get(f[2 * j], f[2 * j + 1]);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             const int at = column(t, c);
             if (at < dim) {
-                if constexpr (VEC) *(uint4*)((typename T::type*)row + at) = T::pack(x + c * V);
-                else ((typename T::type*)row)[at] = T::put(x[c]);
+                if constexpr (TAKE == WHOLE) *(uint4*)(row + at) = T::pack(f + c * V);
+                else row[at] = T::put(f[c]);
             }
         }
     }
     // per-column values in 32 bits
-    static __device__ __forceinline__ void param(const void* p, int type, float otherwise, int t, int dim, float* w) {
+    static __device__ __forceinline__ void param(const void* p, int type, float otherwise, int t, int dim, Two* w) {
+        float f[E];
 #pragma unroll
         for (int c = 0; c < N; ++c)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const int at = column(t, c) + k;
-                w[c * V + k] = at < dim ? (p ? load_as_f32(p, type, at) : otherwise) : 0.0f;
+                f[c * V + k] = at < dim ? (p ? load_as_f32(p, type, at) : otherwise) : 0.0f;
             }
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) w[j] = Two(f[2 * j], f[2 * j + 1]);
     }
 };
+// Sum of the products of pairs (of their sums, if `y` is null) in two chains.
+template <int P> __device__ __forceinline__ float sum_of(const Two* x, const Two* y) {
+    Two s[2] = {Two(0.0f, 0.0f), Two(0.0f, 0.0f)};
+#pragma unroll
+    for (int j = 0; j < P; ++j) s[j & 1] = y ? fma(x[j], y[j], s[j & 1]) : s[j & 1] + x[j];
+    return (s[0] + s[1]).sum();
+}
+__device__ __forceinline__ void sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
 
-template <int TPR> constexpr int LN_THREADS = TPR == 32 ? 256 : TPR;
+// Slots of shared memory for a thread block's rows of `arrays` arrays: those ahead and the one that is being read, in 192 KB at most.
+template <class H> __host__ __device__ constexpr int ln_slots(int arrays) {
+    const int most = sizeof(typename H::type) == 2 ? 4 : 3, fit = 192 * 1024 / (arrays * H::ROW);
+    return H::ASYNC ? (fit < 1 ? 1 : fit < most ? fit : most) : 1;
+}
 
-template <class T, bool VEC, int TPR, int E>
-__global__ void __launch_bounds__(LN_THREADS<TPR>) ln_forward_kernel(const __grid_constant__ LnForward a) {
-    typedef Held<T, VEC, TPR, E> H;
-    constexpr int GROUPS = LN_THREADS<TPR> / TPR;
+template <class T, int TAKE, int TPR, int E>
+__global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_forward_kernel(const __grid_constant__ LnForward a) {
+    typedef Held<T, TAKE, TPR, E> H;
+    typedef typename T::type type;
+    constexpr int SLOTS = ln_slots<H>(1);
+    extern __shared__ uint4 room[];
     __shared__ float sh[2][32][1];
     int turn = 0;
     const int t = threadIdx.x % TPR;
     let_next_start();
     wait_for_previous();
-    float w[E], b[E];
+    constexpr int P = E / 2;
+    Two w[P], b[P];
     H::param(a.weight, a.weight_type, 1.0f, t, a.dim, w);
     H::param(a.bias, a.weight_type, 0.0f, t, a.dim, b);
     auto row_of = [&](uint32_t r) {
         const uint32_t u = r / a.tokens;
-        return (const typename T::type*)a.x + u * a.xu + (r - u * a.tokens) * a.xt;
+        return (const type*)a.x + u * a.xu + (r - u * a.tokens) * a.xt;
     };
-    const uint32_t step = gridDim.x * GROUPS;
-    uint32_t r = blockIdx.x * GROUPS + threadIdx.x / TPR;
-    H next;
-    if (r < a.rows) next.load(row_of(r), t, a.dim);
-    for (; r < a.rows; r += step) {
-        float x[E];
-        next.values(x);
-        if (a.rows - r > step) next.load(row_of(r + step), t, a.dim);
-        float s[1] = {0.0f};
+    auto slot = [&](int i) { return (uint8_t*)room + i * H::ROW; };
+    const uint32_t step = gridDim.x * H::GROUPS;
+    uint32_t r = blockIdx.x * H::GROUPS + threadIdx.x / TPR;
+    uint64_t coming = r;
+    auto send = [&](int i) {
+        if (coming < a.rows) H::send(slot(i), row_of((uint32_t)coming), t, a.dim);
+        sent();
+        coming += step;
+    };
 #pragma unroll
-        for (int i = 0; i < E; ++i) s[0] += x[i];
+    for (int i = 0; i < SLOTS - 1; ++i) send(i);
+    for (int i = 0; r < a.rows; i = i + 1 == SLOTS ? 0 : i + 1) {
+        Two x[P];
+        if (SLOTS == 1) send(0);
+        arrived<SLOTS >= 2 ? SLOTS - 2 : 0>();
+        H::take(slot(i), row_of(r), t, a.dim, x);
+        if (SLOTS > 1) send(i ? i - 1 : SLOTS - 1);
+        float s[1] = {sum_of<P>(x, nullptr)};
         row_sum<TPR, 1>(s, sh, turn);
         const float mean = s[0] * a.inv_dim;
-        s[0] = 0.0f;
+        if (a.dim < TPR * E) H::beyond(t, a.dim, mean, x);            // their differences are 0
 #pragma unroll
-        for (int c = 0; c < H::N; ++c)
-#pragma unroll
-            for (int k = 0; k < H::V; ++k) {
-                const int i = c * H::V + k;
-                x[i] -= mean;
-                if (H::column(t, c) < a.dim) s[0] = fmaf(x[i], x[i], s[0]);
-            }
+        for (int j = 0; j < P; ++j) x[j] = x[j] + Two(-mean, -mean);
+        s[0] = sum_of<P>(x, x);
         row_sum<TPR, 1>(s, sh, turn);
         const float rstd = 1.0f / sqrtf(fmaf(s[0], a.inv_dim, a.eps));
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = fmaf(x[i] * rstd, w[i], b[i]);
+        for (int j = 0; j < P; ++j) x[j] = fma(x[j] * Two(rstd, rstd), w[j], b[j]);
         const uint32_t u = r / a.tokens, k = r - u * a.tokens;
-        H::store((typename T::type*)a.y + u * a.yu + k * a.yt, t, a.dim, x);
+        H::store((type*)a.y + u * a.yu + k * a.yt, t, a.dim, x);
         if (t == 0) { a.mean[r] = mean; a.rstd[r] = rstd; }
+        if (a.rows - r <= step) break;
+        r += step;
     }
 }
 
 // blockIdx.x: slice of the user blockIdx.y's rows.
-template <class T, bool VEC, int TPR, int E>
-__global__ void __launch_bounds__(LN_THREADS<TPR>) ln_backward_kernel(const __grid_constant__ LnBackward a) {
-    typedef Held<T, VEC, TPR, E> H;
-    constexpr int GROUPS = LN_THREADS<TPR> / TPR;
+template <class T, int TAKE, int TPR, int E>
+__global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_backward_kernel(const __grid_constant__ LnBackward a) {
+    typedef Held<T, TAKE, TPR, E> H;
+    typedef typename T::type type;
+    constexpr int SLOTS = ln_slots<H>(2);
+    extern __shared__ uint4 room[];
     __shared__ float sh[2][32][2];
     int turn = 0;
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const uint32_t user = blockIdx.y;
     let_next_start();
     wait_for_previous();
-    float w[E], dw[E], db[E];
+    constexpr int P = E / 2;
+    Two w[P], dw2[P], db2[P];
     H::param(a.weight, a.weight_type, 1.0f, t, a.dim, w);
 #pragma unroll
-    for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
-    const typename T::type* gy = (const typename T::type*)a.dy + user * a.gu;
-    const typename T::type* xs = (const typename T::type*)a.x + user * a.xu;
-    typename T::type* dx = (typename T::type*)a.dx + user * a.du;
+    for (int j = 0; j < P; ++j) dw2[j] = db2[j] = Two(0.0f, 0.0f);
+    const type* gy = (const type*)a.dy + user * a.gu;
+    const type* xs = (const type*)a.x + user * a.xu;
+    type* dx = (type*)a.dx + user * a.du;
     const float *means = a.mean + (int64_t)user * a.tokens, *rstds = a.rstd + (int64_t)user * a.tokens;
-    const uint32_t step = a.slices * GROUPS;
-    H ng, nx;
-    float nm = 0.0f, nr = 0.0f;
-    auto fetch = [&](uint32_t r) {
-        ng.load(gy + r * a.gt, t, a.dim);
-        nx.load(xs + r * a.xt, t, a.dim);
-        nm = means[r];
-        nr = rstds[r];
-    };
-    uint32_t r = blockIdx.x * GROUPS + group;
-    if (r < a.tokens) fetch(r);
-    for (; r < a.tokens; r += step) {
-        float g[E], x[E];
-        ng.values(g);
-        nx.values(x);
-        const float mean = nm, rstd = nr;
-        if (a.tokens - r > step) fetch(r + step);
-        float c[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            x[i] = (x[i] - mean) * rstd;
-            dw[i] = fmaf(g[i], x[i], dw[i]);
-            db[i] += g[i];
-            g[i] *= w[i];                     // 0 beyond the row
-            c[0] += g[i];
-            c[1] = fmaf(g[i], x[i], c[1]);
+    const uint32_t step = a.slices * H::GROUPS;
+    auto slot = [&](int i) { return (uint8_t*)room + i * 2 * H::ROW; };
+    uint32_t r = blockIdx.x * H::GROUPS + group;
+    uint64_t coming = r;
+    auto send = [&](int i) {
+        if (coming < a.tokens) {
+            H::send(slot(i), gy + coming * a.gt, t, a.dim);
+            H::send(slot(i) + H::ROW, xs + coming * a.xt, t, a.dim);
         }
-        row_sum<TPR, 2>(c, sh, turn);
-        if (a.dx) {
-            const float c1 = c[0] * a.inv_dim, c2 = c[1] * a.inv_dim;
+        sent();
+        coming += step;
+    };
 #pragma unroll
-            for (int i = 0; i < E; ++i) g[i] = (g[i] - fmaf(x[i], c2, c1)) * rstd;
+    for (int i = 0; i < SLOTS - 1; ++i) send(i);
+    float next_mean = r < a.tokens ? means[r] : 0.0f, next_rstd = r < a.tokens ? rstds[r] : 0.0f;
+    for (int i = 0; r < a.tokens; i = i + 1 == SLOTS ? 0 : i + 1) {
+        Two g[P], x[P];
+        if (SLOTS == 1) send(0);
+        arrived<SLOTS >= 2 ? SLOTS - 2 : 0>();
+        H::take(slot(i), gy + r * a.gt, t, a.dim, g);
+        H::take(slot(i) + H::ROW, xs + r * a.xt, t, a.dim, x);
+        if (SLOTS > 1) send(i ? i - 1 : SLOTS - 1);
+        const float mean = next_mean, rstd = next_rstd;
+        const bool more = a.tokens - r > step;
+        if (more) { next_mean = means[r + step]; next_rstd = rstds[r + step]; }
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            x[j] = (x[j] + Two(-mean, -mean)) * Two(rstd, rstd);
+            dw2[j] = fma(g[j], x[j], dw2[j]);
+            db2[j] = db2[j] + g[j];
+            g[j] = g[j] * w[j];               // 0 beyond the row
+        }
+        if (a.dx) {
+            float c[2] = {sum_of<P>(g, nullptr), sum_of<P>(g, x)};
+            row_sum<TPR, 2>(c, sh, turn);
+            const float c1 = -c[0] * a.inv_dim, c2 = -c[1] * a.inv_dim;
+#pragma unroll
+            for (int j = 0; j < P; ++j) g[j] = (g[j] + fma(x[j], Two(c2, c2), Two(c1, c1))) * Two(rstd, rstd);
             H::store(dx + r * a.dt, t, a.dim, g);
         }
+        if (!more) break;
+        r += step;
     }
     if (!a.dweight.data && !a.dbias.data) return;
-    if (GROUPS > 1) {                         // the warps' sums, in their order
-        __shared__ float sums[2][GROUPS > 1 ? 32 * E : 1];
-        for (int k = 0; k < GROUPS; ++k) {
+    float dw[E], db[E];
+#pragma unroll
+    for (int j = 0; j < P; ++j) { dw2[j].get(dw[2 * j], dw[2 * j + 1]); db2[j].get(db[2 * j], db[2 * j + 1]); }
+    if (H::GROUPS > 1) {                      // the groups' sums, in their order
+        __shared__ float sums[2][H::GROUPS > 1 ? TPR * E : 1];
+        for (int k = 0; k < H::GROUPS; ++k) {
             if (group == k)
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const int at = i * 32 + t;
+                    const int at = i * TPR + t;
                     sums[0][at] = dw[i] = k ? sums[0][at] + dw[i] : dw[i];
                     sums[1][at] = db[i] = k ? sums[1][at] + db[i] : db[i];
                 }
             __syncthreads();
         }
-        if (group != GROUPS - 1) return;
+        if (group != H::GROUPS - 1) return;
     }
     float* part = a.part + ((int64_t)user * a.slices + blockIdx.x) * 2 * a.dim;
 #pragma unroll
@@ -257,63 +321,92 @@ __global__ void __launch_bounds__(256) ln_join_kernel(const float* part, int sli
     if (to.data) store_as(to.data, to.type, user * to.user_stride + (column < dim ? column : column - dim), s, to.accumulate);
 }
 
-// How a row of `dim` elements is held: the least that holds it.  One warp up to 1024 elements, several above.
-struct LnShape { int tpr, e; };
-inline LnShape ln_shape(int64_t dim) {
-    if (dim <= 256) return {32, 8};
-    if (dim <= 512) return {32, 16};
-    if (dim <= 768) return {32, 24};
-    if (dim <= 1024) return {32, 32};
-    if (dim <= 2048) return {128, 16};
-    if (dim <= 4096) return {256, 16};
-    if (dim <= 8192) return {512, 16};
-    return {1024, 16};
-}
-// Thread blocks on an SM.
-inline int ln_per_sm(int tpr) { return tpr == 32 ? 2 : tpr == 128 ? 5 : tpr == 256 ? 3 : tpr == 512 ? 1 : 1; }
+// How a row of up to `dim` elements is held: threads, and elements of each.  Few threads have few of a reduction's steps for each element, and more
+// elements in flight each; many leave more registers to the backward pass' sums.  Times in us for 16 elements a thread and for 8, forward and
+// backward: 65536 x 768 bf16 (24 elements) 37 and 60, 63 and 107; 32768 x 2048 bf16 52 and 78, 82 and 103; f32 99 and 98, 140 and 169; 16384 x
+// 4096 f32 100 and 87, 141 and 132; 32768 x 1001 f32 word by word 57 and 58, 110 and 93.
+struct LnShape { int dim, tpr, e; };
+template <class T, int TAKE> constexpr LnShape LN_SHAPES[8] = {
+    {256, 32, 8}, {512, 32, 16}, {768, 32, 24}, {1024, 64, 16}, {2048, 128, 16}, {4096, 256, 16}, {8192, 512, 16}, {LN_MAX_DIM, 1024, 16}};
+template <> constexpr LnShape LN_SHAPES<OF32, WHOLE>[8] = {
+    {256, 32, 8}, {512, 32, 16}, {768, 32, 24}, {1024, 64, 16}, {2048, 128, 16}, {4096, 512, 8}, {8192, 512, 16}, {LN_MAX_DIM, 1024, 16}};
+template <> constexpr LnShape LN_SHAPES<OF32, WORDS>[8] = {
+    {256, 32, 8}, {512, 64, 8}, {768, 96, 8}, {1024, 128, 8}, {2048, 256, 8}, {4096, 512, 8}, {8192, 512, 16}, {LN_MAX_DIM, 1024, 16}};
 
 }  // namespace
 
 struct co3_layernorm {
     int64_t dim, launches;
     int users, device, sms;
+    int places[3][3][2];                      // thread blocks that the device holds at a time, by type, way of reading, and direction
     double eps;
     float* part;
 };
 
 namespace {
 
-int ln_slices(const co3_layernorm* h, int64_t tokens) {
-    const LnShape s = ln_shape(h->dim);
-    const int64_t groups = s.tpr == 32 ? 8 : 1, places = (int64_t)h->sms * ln_per_sm(s.tpr) / h->users, most = (tokens + 2 * groups - 1) / (2 * groups);
-    const int64_t n = places < most ? places : most;
-    return n < 1 ? 1 : (int)n;
+template <class H> int64_t ln_slices(const co3_layernorm* h, int64_t tokens, int places) {
+    const int64_t each = places / h->users, most = (tokens + 2 * H::GROUPS - 1) / (2 * H::GROUPS), n = each < most ? each : most;
+    return n < 1 ? 1 : n;
 }
 
-template <class T, bool VEC, int TPR, int E> int ln_forward_of(co3_layernorm* h, const LnForward& a, cudaStream_t st) {
-    const uint32_t groups = LN_THREADS<TPR> / TPR;
-    const int64_t need = ((int64_t)a.rows + groups - 1) / groups, places = (int64_t)h->sms * (2048 / LN_THREADS<TPR>);
-    return launch_early(&h->launches, ln_forward_kernel<T, VEC, TPR, E>, dim3((unsigned)(need < places ? need : places)), LN_THREADS<TPR>, 0, 1, st, a);
-}
-template <class T, bool VEC, int TPR, int E> int ln_backward_of(co3_layernorm* h, const LnBackward& a, cudaStream_t st) {
-    return launch_early(&h->launches, ln_backward_kernel<T, VEC, TPR, E>, dim3((unsigned)a.slices, (unsigned)h->users), LN_THREADS<TPR>, 0, 1, st, a);
-}
-template <class T, bool VEC, class A> int ln_launch_as(co3_layernorm* h, const A& a, cudaStream_t st) {
-    const LnShape s = ln_shape(h->dim);
-#define CO3_LN(tpr_, e_) \
-    if (s.tpr == tpr_ && s.e == e_) { \
-        if constexpr (std::is_same<A, LnForward>::value) return ln_forward_of<T, VEC, tpr_, e_>(h, a, st); \
-        else return ln_backward_of<T, VEC, tpr_, e_>(h, a, st); \
+// What is done with the kernels of a shape.
+struct LnPrepare {                            // asks for their shared memory, and for how many thread blocks there is room
+    co3_layernorm* h;
+    int64_t scratch;                          // numbers
+    template <class T, int TAKE, int TPR, int E> int run(int type) {
+        typedef Held<T, TAKE, TPR, E> H;
+        for (int back = 0; back < 2; ++back) {
+            const void* kernel = back ? (const void*)ln_backward_kernel<T, TAKE, TPR, E> : (const void*)ln_forward_kernel<T, TAKE, TPR, E>;
+            const int bytes = H::ASYNC ? ln_slots<H>(1 + back) * (1 + back) * H::ROW : 0;
+            int n = 0;
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess ||
+                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, H::THREADS, bytes) != cudaSuccess || n < 1) return CO3_ECUDA;
+            h->places[type][TAKE][back] = n * h->sms;
+            const int64_t slices = ln_slices<H>(h, OPS_MAX_ROWS, n * h->sms);
+            if (back && slices > 1 && h->users * slices * 2 * h->dim > scratch) scratch = h->users * slices * 2 * h->dim;
+        }
+        return CO3_OK;
     }
-    CO3_LN(32, 8) CO3_LN(32, 16) CO3_LN(32, 24) CO3_LN(32, 32) CO3_LN(128, 16) CO3_LN(256, 16) CO3_LN(512, 16) CO3_LN(1024, 16)
-#undef CO3_LN
-    return CO3_EINVAL;
+};
+struct LnRunForward {
+    co3_layernorm* h;
+    LnForward a;
+    cudaStream_t st;
+    template <class T, int TAKE, int TPR, int E> int run(int type) {
+        typedef Held<T, TAKE, TPR, E> H;
+        const int64_t need = ((int64_t)a.rows + H::GROUPS - 1) / H::GROUPS, places = h->places[type][TAKE][0];
+        return launch_early(&h->launches, ln_forward_kernel<T, TAKE, TPR, E>, dim3((unsigned)(need < places ? need : places)), H::THREADS,
+                            H::ASYNC ? ln_slots<H>(1) * H::ROW : 0, 1, st, a);
+    }
+};
+struct LnRunBackward {
+    co3_layernorm* h;
+    LnBackward a;
+    cudaStream_t st;
+    template <class T, int TAKE, int TPR, int E> int run(int type) {
+        typedef Held<T, TAKE, TPR, E> H;
+        a.slices = (int)ln_slices<H>(h, a.tokens, h->places[type][TAKE][1]);
+        const int rc = launch_early(&h->launches, ln_backward_kernel<T, TAKE, TPR, E>, dim3((unsigned)a.slices, (unsigned)h->users), H::THREADS,
+                                    H::ASYNC ? ln_slots<H>(2) * 2 * H::ROW : 0, 1, st, a);
+        if (rc != CO3_OK || a.slices == 1 || (!a.dweight.data && !a.dbias.data)) return rc;
+        return launch_early(&h->launches, ln_join_kernel, dim3((unsigned)((2 * h->dim + 31) / 32), (unsigned)h->users), 256, 0, 1, st, (const float*)h->part,
+                            a.slices, a.dim, a.dweight, a.dbias);
+    }
+};
+template <class T, int TAKE, int I, class W> int ln_with_shape(int64_t dim, int type, W& what) {
+    constexpr LnShape S = LN_SHAPES<T, TAKE>[I];
+    if (dim <= S.dim) return what.template run<T, TAKE, S.tpr, S.e>(type);
+    if constexpr (I < 7) return ln_with_shape<T, TAKE, I + 1>(dim, type, what);
+    else return CO3_EINVAL;
 }
-template <class A> int ln_launch(co3_layernorm* h, int type, bool vec, const A& a, cudaStream_t st) {
-    if (type == CO3_F32) return vec ? ln_launch_as<OF32, true>(h, a, st) : ln_launch_as<OF32, false>(h, a, st);
-    if (type == CO3_BF16) return vec ? ln_launch_as<OBf16, true>(h, a, st) : ln_launch_as<OBf16, false>(h, a, st);
-    return vec ? ln_launch_as<OF16, true>(h, a, st) : ln_launch_as<OF16, false>(h, a, st);
+template <class W> int ln_with(int64_t dim, int type, int take, W& what) {
+    if (type == CO3_F32) return take == WHOLE ? ln_with_shape<OF32, WHOLE, 0>(dim, type, what) : ln_with_shape<OF32, WORDS, 0>(dim, type, what);
+    if (type == CO3_BF16) return take == WHOLE ? ln_with_shape<OBf16, WHOLE, 0>(dim, type, what) : ln_with_shape<OBf16, SINGLES, 0>(dim, type, what);
+    return take == WHOLE ? ln_with_shape<OF16, WHOLE, 0>(dim, type, what) : ln_with_shape<OF16, SINGLES, 0>(dim, type, what);
 }
+// WHOLE, or what the type has for rows that begin anywhere.
+int ln_take(int type, bool whole) { return whole ? WHOLE : type == CO3_F32 ? WORDS : SINGLES; }
 
 }  // namespace
 
@@ -335,9 +428,11 @@ extern "C" int co3_layernorm_create(co3_layernorm** out, int64_t dim, int32_t n_
     int rc = CO3_OK;
     if (cudaGetDevice(&h->device) != cudaSuccess || cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess || h->sms < 1) rc = CO3_ECUDA;
     if (rc == CO3_OK) {
-        // of users whose rows go to more than one thread block
-        const int64_t slices = ln_slices(h, OPS_MAX_ROWS);
-        if (slices > 1 && cudaMalloc(&h->part, (size_t)(n_users * slices * 2 * dim * 4)) != cudaSuccess) { h->part = nullptr; rc = CO3_ENOMEM; }
+        LnPrepare p = {h, 0};
+        for (int type = CO3_F32; type <= CO3_F16 && rc == CO3_OK; ++type)
+            for (int whole = 0; whole < 2 && rc == CO3_OK; ++whole) rc = ln_with(dim, type, ln_take(type, whole != 0), p);
+        // sums of the thread blocks of users whose rows go to more than one
+        if (rc == CO3_OK && p.scratch && cudaMalloc(&h->part, (size_t)p.scratch * 4) != cudaSuccess) { h->part = nullptr; rc = CO3_ENOMEM; }
     }
     if (rc != CO3_OK) { (void)cudaGetLastError(); co3_layernorm_destroy(h); return rc; }
     *out = h;
@@ -357,8 +452,9 @@ extern "C" int co3_layernorm_forward(co3_layernorm* h, const co3_array* x, const
     a.xu = x->user_stride; a.xt = x->token_stride; a.yu = y->user_stride; a.yt = y->token_stride;
     a.tokens = (uint32_t)n_tokens; a.rows = (uint32_t)(n_tokens * h->users);
     a.dim = (int)h->dim; a.weight_type = weight_type; a.inv_dim = (float)(1.0 / (double)h->dim); a.eps = (float)h->eps;
-    const bool vec = h->dim * type_width(x->type) % 16 == 0 && rows_aligned(x, h->users, n_tokens) && rows_aligned(y, h->users, n_tokens);
-    return ln_launch(h, x->type, vec, a, (cudaStream_t)cuda_stream);
+    const bool whole = h->dim * type_width(x->type) % 16 == 0 && rows_aligned(x, h->users, n_tokens) && rows_aligned(y, h->users, n_tokens);
+    LnRunForward run = {h, a, (cudaStream_t)cuda_stream};
+    return ln_with(h->dim, x->type, ln_take(x->type, whole), run);
 }
 
 extern "C" int co3_layernorm_backward(co3_layernorm* h, const co3_array* dy, const co3_array* x, const void* weight, int32_t weight_type, const float* mean,
@@ -377,17 +473,14 @@ extern "C" int co3_layernorm_backward(co3_layernorm* h, const co3_array* dy, con
     a.dy = dy->data; a.x = x->data; a.weight = weight; a.dx = dx ? dx->data : nullptr; a.mean = mean; a.rstd = rstd;
     a.gu = dy->user_stride; a.gt = dy->token_stride; a.xu = x->user_stride; a.xt = x->token_stride;
     if (dx) { a.du = dx->user_stride; a.dt = dx->token_stride; }
-    a.tokens = (uint32_t)n_tokens; a.dim = (int)h->dim; a.weight_type = weight_type; a.slices = ln_slices(h, n_tokens);
+    a.tokens = (uint32_t)n_tokens; a.dim = (int)h->dim; a.weight_type = weight_type;
     a.inv_dim = (float)(1.0 / (double)h->dim); a.part = h->part;
     if (dweight) a.dweight = *dweight;
     if (dbias) a.dbias = *dbias;
-    const bool vec = h->dim * type_width(x->type) % 16 == 0 && rows_aligned(x, h->users, n_tokens) && rows_aligned(dy, h->users, n_tokens) &&
-                     (!dx || rows_aligned(dx, h->users, n_tokens));
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    const int rc = ln_launch(h, x->type, vec, a, st);
-    if (rc != CO3_OK || a.slices == 1 || (!dweight && !dbias)) return rc;
-    return launch_early(&h->launches, ln_join_kernel, dim3((unsigned)((2 * h->dim + 31) / 32), (unsigned)h->users), 256, 0, 1, st, (const float*)h->part,
-                        a.slices, a.dim, a.dweight, a.dbias);
+    const bool whole = h->dim * type_width(x->type) % 16 == 0 && rows_aligned(x, h->users, n_tokens) && rows_aligned(dy, h->users, n_tokens) &&
+                       (!dx || rows_aligned(dx, h->users, n_tokens));
+    LnRunBackward run = {h, a, (cudaStream_t)cuda_stream};
+    return ln_with(h->dim, x->type, ln_take(x->type, whole), run);
 }
 
 extern "C" int64_t co3_layernorm_launch_count(const co3_layernorm* h) { return h ? h->launches : 0; }
