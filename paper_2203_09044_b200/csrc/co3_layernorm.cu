@@ -14,7 +14,7 @@ struct LnForward {
     const void* x; const void* weight; const void* bias; void* y;
     float *mean, *rstd;
     int64_t xu, xt, yu, yt;                   // strides
-    uint32_t tokens, rows;
+    uint32_t tokens, users, step_users, step_tokens;      // of all groups together, from one row of a group to its next
     int dim, weight_type;
     float inv_dim, eps;
 };
@@ -29,27 +29,54 @@ struct LnBackward {
     co3_param_grad dweight, dbias;            // data null where not wanted
 };
 
-// Sum over the TPR threads of a row of K values each; `turn` counts the reductions of these threads.
-template <int TPR, int K> __device__ __forceinline__ void row_sum(float (&x)[K], float (*sh)[32][K], int& turn) {
+// Sum over the TPR threads of a row of one value each, or of two; `turn` counts the reductions of these threads, `sh` is theirs alone.
+__device__ __forceinline__ float over_warp(float x) { return warp_sum_f32(x); }
+__device__ __forceinline__ Two over_warp(Two x) {
+    float a, b;
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = warp_sum_f32(x[k]);
-    if (TPR == 32) return;
+    for (int o = 16; o; o >>= 1) {
+        x.get(a, b);
+        x = x + Two(__shfl_xor_sync(0xffffffffu, a, o), __shfl_xor_sync(0xffffffffu, b, o));
+    }
+    return x;
+}
+template <int TPR, class V> struct RowSum {
+    static constexpr int W = TPR / 32, GROUPS_MOST = TPR >= 256 ? 1 : 8 / W;
+    static constexpr int PITCH = (W * (int)sizeof(V) + 15) / 16 * 16 / (int)sizeof(V);        // a group's warps begin at 16 bytes
+    V sums[2][GROUPS_MOST * PITCH];           // two: one barrier a reduction
+};
+template <int TPR, class V> __device__ __forceinline__ V row_sum(V x, RowSum<TPR, V>& sh, int& turn) {
     constexpr int W = TPR / 32;
-    const int warp = threadIdx.x >> 5, group = warp / W, first = group * W;
-    float(*s)[K] = sh[turn & 1];              // two buffers: one barrier a reduction
-    ++turn;
-    if ((threadIdx.x & 31) == 0)
+    x = over_warp(x);
+    if constexpr (W == 1) return x;
+    else {
+        const int group = threadIdx.x / TPR, warp = threadIdx.x % TPR / 32, lane = threadIdx.x & 31;
+        V* const s = sh.sums[turn & 1] + group * RowSum<TPR, V>::PITCH;
+        ++turn;
+        if (lane == 0) s[warp] = x;
+        asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "n"(TPR) : "memory");
+        if constexpr (W > 8) {
+            V t = s[lane % W];
+            if (W < 32 && lane >= W) { if constexpr (sizeof(V) == 4) t = 0.0f; else t = Two(0.0f, 0.0f); }
+            return over_warp(t);
+        } else {                              // 16 bytes at a time
+            constexpr int EACH = 16 / sizeof(V);
+            union { uint4 u[(W + EACH - 1) / EACH]; unsigned long long pair[(W + EACH - 1) / EACH * 2]; float one[(W + EACH - 1) / EACH * 4]; } all;
 #pragma unroll
-        for (int k = 0; k < K; ++k) s[warp][k] = x[k];
-    asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "n"(TPR) : "memory");
+            for (int i = 0; i < (W + EACH - 1) / EACH; ++i) all.u[i] = ((const uint4*)s)[i];
+            if constexpr (sizeof(V) == 4) {
+                float t = all.one[0];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float t = 0.0f;
-        if (W <= 8) {
+                for (int w = 1; w < W; ++w) t += all.one[w];
+                return t;
+            } else {
+                Two t, o;
+                t.v = all.pair[0];
 #pragma unroll
-            for (int w = 0; w < W; ++w) t += s[first + w][k];
-        } else t = warp_sum_f32((threadIdx.x & 31) < W ? s[threadIdx.x & 31][k] : 0.0f);
-        x[k] = t;
+                for (int w = 1; w < W; ++w) { o.v = all.pair[w]; t = t + o; }
+                return t;
+            }
+        }
     }
 }
 
@@ -150,7 +177,7 @@ __global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_forward_ker
     typedef typename T::type type;
     constexpr int SLOTS = ln_slots<H>(1);
     extern __shared__ uint4 room[];
-    __shared__ float sh[2][32][1];
+    __shared__ __align__(16) RowSum<TPR, float> sh;
     int turn = 0;
     const int t = threadIdx.x % TPR;
     let_next_start();
@@ -159,43 +186,43 @@ __global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_forward_ker
     Two w[P], b[P];
     H::param(a.weight, a.weight_type, 1.0f, t, a.dim, w);
     H::param(a.bias, a.weight_type, 0.0f, t, a.dim, b);
-    auto row_of = [&](uint32_t r) {
-        const uint32_t u = r / a.tokens;
-        return (const type*)a.x + u * a.xu + (r - u * a.tokens) * a.xt;
-    };
     auto slot = [&](int i) { return (uint8_t*)room + i * H::ROW; };
-    const uint32_t step = gridDim.x * H::GROUPS;
-    uint32_t r = blockIdx.x * H::GROUPS + threadIdx.x / TPR;
-    uint64_t coming = r;
+    // rows of this group: the one that is worked on and the one that is sent for, as user and token, without a division for each
+    struct At { uint32_t user, token; };
+    auto next = [&](At& r) {
+        r.user += a.step_users;
+        r.token += a.step_tokens;
+        if (r.token >= a.tokens) { r.token -= a.tokens; ++r.user; }
+    };
+    const uint32_t first = blockIdx.x * H::GROUPS + threadIdx.x / TPR;
+    At at = {first / a.tokens, first % a.tokens}, coming = at;
+    auto row_of = [&](const At& r) { return (const type*)a.x + r.user * a.xu + r.token * a.xt; };
     auto send = [&](int i) {
-        if (coming < a.rows) H::send(slot(i), row_of((uint32_t)coming), t, a.dim);
+        if (coming.user < a.users) H::send(slot(i), row_of(coming), t, a.dim);
         sent();
-        coming += step;
+        next(coming);
     };
 #pragma unroll
     for (int i = 0; i < SLOTS - 1; ++i) send(i);
-    for (int i = 0; r < a.rows; i = i + 1 == SLOTS ? 0 : i + 1) {
+    for (int i = 0; at.user < a.users; i = i + 1 == SLOTS ? 0 : i + 1, next(at)) {
         Two x[P];
         if (SLOTS == 1) send(0);
         arrived<SLOTS >= 2 ? SLOTS - 2 : 0>();
-        H::take(slot(i), row_of(r), t, a.dim, x);
+        H::take(slot(i), row_of(at), t, a.dim, x);
         if (SLOTS > 1) send(i ? i - 1 : SLOTS - 1);
-        float s[1] = {sum_of<P>(x, nullptr)};
-        row_sum<TPR, 1>(s, sh, turn);
-        const float mean = s[0] * a.inv_dim;
+        const float mean = row_sum<TPR>(sum_of<P>(x, nullptr), sh, turn) * a.inv_dim;
         if (a.dim < TPR * E) H::beyond(t, a.dim, mean, x);            // their differences are 0
 #pragma unroll
         for (int j = 0; j < P; ++j) x[j] = x[j] + Two(-mean, -mean);
-        s[0] = sum_of<P>(x, x);
-        row_sum<TPR, 1>(s, sh, turn);
-        const float rstd = 1.0f / sqrtf(fmaf(s[0], a.inv_dim, a.eps));
+        const float rstd = rsqrtf(fmaf(row_sum<TPR>(sum_of<P>(x, x), sh, turn), a.inv_dim, a.eps));       // to two units in the last place
 #pragma unroll
         for (int j = 0; j < P; ++j) x[j] = fma(x[j] * Two(rstd, rstd), w[j], b[j]);
-        const uint32_t u = r / a.tokens, k = r - u * a.tokens;
-        H::store((type*)a.y + u * a.yu + k * a.yt, t, a.dim, x);
-        if (t == 0) { a.mean[r] = mean; a.rstd[r] = rstd; }
-        if (a.rows - r <= step) break;
-        r += step;
+        H::store((type*)a.y + at.user * a.yu + at.token * a.yt, t, a.dim, x);
+        if (t == 0) {
+            const int64_t r = (int64_t)at.user * a.tokens + at.token;
+            a.mean[r] = mean;
+            a.rstd[r] = rstd;
+        }
     }
 }
 
@@ -206,7 +233,7 @@ __global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_backward_ke
     typedef typename T::type type;
     constexpr int SLOTS = ln_slots<H>(2);
     extern __shared__ uint4 room[];
-    __shared__ float sh[2][32][2];
+    __shared__ __align__(16) RowSum<TPR, Two> sh;
     int turn = 0;
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const uint32_t user = blockIdx.y;
@@ -254,9 +281,8 @@ __global__ void __launch_bounds__(Held<T, TAKE, TPR, E>::THREADS) ln_backward_ke
             g[j] = g[j] * w[j];               // 0 beyond the row
         }
         if (a.dx) {
-            float c[2] = {sum_of<P>(g, nullptr), sum_of<P>(g, x)};
-            row_sum<TPR, 2>(c, sh, turn);
-            const float c1 = -c[0] * a.inv_dim, c2 = -c[1] * a.inv_dim;
+            float c1, c2;
+            (row_sum<TPR>(Two(sum_of<P>(g, nullptr), sum_of<P>(g, x)), sh, turn) * Two(-a.inv_dim, -a.inv_dim)).get(c1, c2);
 #pragma unroll
             for (int j = 0; j < P; ++j) g[j] = (g[j] + fma(x[j], Two(c2, c2), Two(c1, c1))) * Two(rstd, rstd);
             H::store(dx + r * a.dt, t, a.dim, g);
@@ -375,8 +401,11 @@ struct LnRunForward {
     cudaStream_t st;
     template <class T, int TAKE, int TPR, int E> int run(int type) {
         typedef Held<T, TAKE, TPR, E> H;
-        const int64_t need = ((int64_t)a.rows + H::GROUPS - 1) / H::GROUPS, places = h->places[type][TAKE][0];
-        return launch_early(&h->launches, ln_forward_kernel<T, TAKE, TPR, E>, dim3((unsigned)(need < places ? need : places)), H::THREADS,
+        const int64_t need = ((int64_t)a.tokens * a.users + H::GROUPS - 1) / H::GROUPS, places = h->places[type][TAKE][0];
+        const uint32_t grid = (uint32_t)(need < places ? need : places);
+        a.step_users = grid * H::GROUPS / a.tokens;
+        a.step_tokens = grid * H::GROUPS % a.tokens;
+        return launch_early(&h->launches, ln_forward_kernel<T, TAKE, TPR, E>, dim3(grid), H::THREADS,
                             H::ASYNC ? ln_slots<H>(1) * H::ROW : 0, 1, st, a);
     }
 };
@@ -450,7 +479,7 @@ extern "C" int co3_layernorm_forward(co3_layernorm* h, const co3_array* x, const
     LnForward a;
     a.x = x->data; a.weight = weight; a.bias = bias; a.y = y->data; a.mean = mean; a.rstd = rstd;
     a.xu = x->user_stride; a.xt = x->token_stride; a.yu = y->user_stride; a.yt = y->token_stride;
-    a.tokens = (uint32_t)n_tokens; a.rows = (uint32_t)(n_tokens * h->users);
+    a.tokens = (uint32_t)n_tokens; a.users = (uint32_t)h->users;
     a.dim = (int)h->dim; a.weight_type = weight_type; a.inv_dim = (float)(1.0 / (double)h->dim); a.eps = (float)h->eps;
     const bool whole = h->dim * type_width(x->type) % 16 == 0 && rows_aligned(x, h->users, n_tokens) && rows_aligned(y, h->users, n_tokens);
     LnRunForward run = {h, a, (cudaStream_t)cuda_stream};
