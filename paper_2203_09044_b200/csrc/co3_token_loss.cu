@@ -1,9 +1,9 @@
 // Losses of tokens over a large vocabulary, and their gradients, without the logits (co3_token_loss_*).
 //
 // All products run through one kernel on the tensor cores: pairs of thread blocks (two SMs) on tiles of 256 x 256, operands brought by TMA
-// into a ring of stages, accumulators in tensor memory, two of them, so that the products of the next tile run while eight warps of
+// into a ring of stages, accumulators in tensor memory, two of them, so that the products of the next tile run while sixteen warps of
 // each block work on the last one:
-//   STATS   z = H W^T                     -> per row and 128 columns: largest logit, sum of exponentials, weighted target logits
+//   STATS   z = H W^T                     -> per row and 64 columns: largest logit, sum of exponentials, weighted target logits
 //   DZ      z again, for a piece of the vocabulary -> dz, in 16 bits (and its remainder in 16 more, for 32-bit gradients of the weight)
 //   DHIDDEN dz W    over the piece        -> 32-bit sums
 //   DWEIGHT dz^T H  over a user's tokens  -> the user's gradient
@@ -20,14 +20,16 @@ constexpr int KB = 64;                        // depth of a stage: 128 bytes, on
 constexpr int STAGES = 5;
 constexpr int HALF_BYTES = 128 * KB * 2;      // one operand's part of a thread block and stage
 constexpr int STAGE_BYTES = 2 * HALF_BYTES;
-constexpr int FIRST_EPI = 2;                  // warps: loads, products, then eight for the tiles' ends
-constexpr int GEMM_THREADS = 320;
-constexpr int EPI_WARPS = 8;
-constexpr int OUT_BYTES = EPI_WARPS * 2 * 4096;          // two boxes of 32 x 128 bytes a warp, or 32 x 33 numbers
+constexpr int FIRST_EPI = 2;                  // warps: loads, products, then those for the tiles' ends
+// Each has 32 rows and 64 columns of a tile.  With half as many and 128 columns an end took 4000 (STATS) to 10000 cycles, nearly all of it
+// latency of instructions that wait for one another, against the 6144 that the products of a tile take at a depth of 768.
+constexpr int EPI_WARPS = 16;
+constexpr int GEMM_THREADS = 32 * (FIRST_EPI + EPI_WARPS);
+constexpr int OUT_BYTES = EPI_WARPS * 4096;   // a box of 32 rows of 128 bytes for each
 constexpr int GEMM_SHARED = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + 256;
 constexpr int ALIGN_ROWS = 64;                // a user's packed rows begin at a multiple of these
 constexpr int MAX_TOP = 128;
-constexpr int SPAN = 128;                     // columns of one set of statistics
+constexpr int SPAN = 64;                      // columns of a warp, and of one set of statistics
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 enum Mode { STATS, DZ, DHIDDEN, DWEIGHT };
@@ -48,7 +50,7 @@ struct Packed {                               // what the packing leaves, on the
 
 struct GemmArgs {
     CUtensorMap a, b, a_low;                  // a_low: the remainders of dz
-    CUtensorMap out, out_low;                 // what a tile's end stores: dz and its remainder, or dweight
+    CUtensorMap out, out_low;                 // what a tile's end stores: dz and its remainder, partial, or dweight
     Packed p;
     OpsStatus* status;
     int users, vocab, dim;
@@ -60,8 +62,7 @@ struct GemmArgs {
     float* dots;                              // [spans][rows]
     const int32_t* entry; const float* entry_q; const uint8_t* entry_first;      // [tokens][top], [tokens][top], [tokens][spans]
     int top, spans;
-    float* partial;                           // [splits][rows][dim]
-    int add;                                  // to what partial holds
+    int add;                                  // to what partial [splits][rows][dim] holds
     co3_param_grad dw;
     int dw_wide;                              // rows of dweight begin at multiples of 16 bytes and are written
 };
@@ -107,28 +108,30 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
-// 32 columns of the warp's 32 rows.  They are there after tmem_loaded or tmem_loaded_too, which name the same registers, so that nothing is
-// done with them before.
+// 32 (16) columns of the warp's 32 rows.  They are there after tmem_loaded or tmem_loaded_too, which name the same registers, so that
+// nothing is done with them before.
 __device__ __forceinline__ void tmem_load32(uint32_t at, float* x) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
                  : "r"(at));
 }
-__device__ __forceinline__ void tmem_loaded(float* x) {
+__device__ __forceinline__ void tmem_load16(uint32_t at, float* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_loaded32(float* x) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]) :: "memory");
 }
-__device__ __forceinline__ void tmem_loaded_too(float* x) {
+__device__ __forceinline__ void tmem_loaded16(float* x) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]) :: "memory");
+}
+__device__ __forceinline__ void tmem_loaded32_too(float* x) {
     asm volatile("" : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31]) :: "memory");
 }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ float exp2_in_order(float x) {          // not moved ahead of earlier stores: registers
-    float y;
-    asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -176,8 +179,8 @@ template <int MODE> __device__ __forceinline__ bool tile_at(const GemmArgs& a, i
     return true;
 }
 
-// ---- the tiles' ends: warp `part` of four has 32 rows, `half` says which 128 of the 256 columns; a lane has a row -------------------
-// The entries of a row that lie in its 128 columns, in order.
+// ---- the tiles' ends: warp `part` of four has 32 rows, `quarter` says which 64 of the 256 columns; a lane has a row -----------------------
+// The entries of a row that lie in its 64 columns, in order.
 template <bool ONE> struct Entries {
     const int32_t* entry; const float* q;
     int left, next;
@@ -210,7 +213,7 @@ template <bool ONE> struct Entries {
     }
 };
 
-// The entries among columns C .. C + 31 of the 128.  Written so that no index into the array is left, which would put it into local memory
+// The entries among columns C .. C + 31 of the 64.  Written so that no index into the array is left, which would put it into local memory
 // (the kernel of the statistics then took 1.5 times as long).
 __device__ __forceinline__ void take_if(int at, int k, float x, float& z) {
     asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\tselp.f32 %0, %3, %0, p;\n\t}" : "+f"(z) : "r"(at), "r"(k), "f"(x));
@@ -235,77 +238,97 @@ template <int C, bool ONE> __device__ __forceinline__ void subtract_entries(floa
     }
 }
 
-template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int half, Entries<ONE>& e) {
-    const int first = w.n + half * SPAN;      // the piece is the whole vocabulary
+template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int quarter, Entries<ONE>& e) {
+    const int first = w.n + quarter * SPAN;   // the piece is the whole vocabulary
     if (first >= a.vocab) return;
     float dot = 0.0f;
-    take_entries<0>(x, first, e, dot); take_entries<32>(x, first, e, dot); take_entries<64>(x, first, e, dot); take_entries<96>(x, first, e, dot);
+    take_entries<0>(x, first, e, dot);
+    take_entries<32>(x, first, e, dot);
     if (first + SPAN > a.vocab)
 #pragma unroll
         for (int k = 0; k < SPAN; ++k) if (first + k >= a.vocab) x[k] = -INFINITY;
-    float m[4] = {x[0], x[1], x[2], x[3]}, s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
     for (int k = 4; k < SPAN; ++k) m[k & 3] = fmaxf(m[k & 3], x[k]);
     const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a.scale;
-    const float from = top == -INFINITY ? 0.0f : top;     // nothing but -infinity: its exponentials are 0
+    const float from = top == -INFINITY ? 0.0f : -top;    // nothing but -infinity: its exponentials are 0
+    const Two scale(a.scale, a.scale), shift(from, from);
+    Two s[2] = {Two(0.0f, 0.0f), Two(0.0f, 0.0f)};
 #pragma unroll
-    for (int k = 0; k < SPAN; ++k) s[k & 3] += exp2_fast(fmaf(x[k], a.scale, -from));
+    for (int k = 0; k < SPAN; k += 2) {
+        float y, z;
+        fma(Two(x[k], x[k + 1]), scale, shift).get(y, z);
+        s[k / 2 & 1] = s[k / 2 & 1] + Two(exp2_fast(y), exp2_fast(z));
+    }
     if (row < rows) {
         const int64_t at = (int64_t)(first / SPAN) * a.rows + row;
-        a.stats[at] = make_float2(top, (s[0] + s[1]) + (s[2] + s[3]));
+        a.stats[at] = make_float2(top, (s[0] + s[1]).sum());
         a.dots[at] = dot;
     }
 }
 
-// Stores of a warp go by way of shared memory: 32 rows of 128 bytes in two buffers, in the order of the 128-byte swizzle, from where
-// TMA takes them.  (Stored from registers, 16 bytes a lane and a row each, dz of 3456 x 25136 in two numbers took 305 us.)
+// Stores of a warp go by way of shared memory: 32 rows of 128 bytes in the order of the 128-byte swizzle, from where TMA takes them.
+// (Stored from registers, 16 bytes a lane and a row each, dz of 3456 x 25136 in two numbers took 305 us, against 130.)
 struct OutBox {
-    uint32_t at;                              // the warp's two buffers
-    int turn;
-    // Waits until the buffer's last box has been read.
-    __device__ __forceinline__ uint32_t begin() {
-        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    uint32_t at;
+    // Waits until the last box has been read.
+    __device__ __forceinline__ void begin() const {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
-        return at + (turn++ & 1) * 4096;
     }
-    static __device__ __forceinline__ void put(uint32_t box, int piece, uint4 u) {            // 16 bytes of the lane's row
+    __device__ __forceinline__ void put(int piece, uint4 u) const {           // 16 bytes of the lane's row
         const uint32_t lane = threadIdx.x & 31;
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(box + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + lane * 128 + ((piece ^ (lane & 7)) << 4)), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
     }
-    static __device__ __forceinline__ void send(uint32_t box, const CUtensorMap* map, int x, int y, int z, bool flat) {
+    __device__ __forceinline__ void send2(const CUtensorMap* map, int x, int y) const {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0)
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;" :: "l"(map), "r"(x), "r"(y), "r"(at) : "memory");
+    }
+    __device__ __forceinline__ void send3(const CUtensorMap* map, int x, int y, int z, bool add) const {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if ((threadIdx.x & 31) == 0) {
-            if (flat) asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" :: "l"(map), "r"(x), "r"(y), "r"(box) : "memory");
-            else asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(box) : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            if (add)
+                asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n\tcp.async.bulk.commit_group;" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(at) : "memory");
+            else
+                asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];\n\tcp.async.bulk.commit_group;" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(at) : "memory");
         }
     }
-    static __device__ __forceinline__ void finish() {
+    __device__ __forceinline__ void finish() const {
         if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 };
 
-// Columns I .. I + 63 of the 128.
-template <int I, class T, bool ONE, bool LOW>
-__device__ __forceinline__ void dz_half(const GemmArgs& a, float (&x)[SPAN], int first, int column, int row0, float lse, float c, Entries<ONE>& e, OutBox& out) {
+template <class T, bool ONE, bool LOW>
+__device__ __forceinline__ void end_dz(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int row0, int quarter, Entries<ONE>& e, const OutBox& out) {
+    const int column = w.n + quarter * SPAN, first = a.v0 + column;
+    const bool here = row < rows;
+    const float lse = here ? -a.p.row_lse[row] : 0.0f, c = here ? a.p.row_c[row] : 0.0f;
+    const Two scale(a.scale, a.scale), shift(lse, lse), factor(c, c);
 #pragma unroll
-    for (int k = I; k < I + 64; ++k) x[k] = exp2_in_order(fmaf(x[k], a.scale, -lse));
-    subtract_entries<I>(x, first, e);
-    subtract_entries<I + 32>(x, first, e);
+    for (int k = 0; k < SPAN; k += 2) {
+        float y, z;
+        fma(Two(x[k], x[k + 1]), scale, shift).get(y, z);
+        x[k] = exp2_fast(y);
+        x[k + 1] = exp2_fast(z);
+    }
+    subtract_entries<0>(x, first, e);
+    subtract_entries<32>(x, first, e);
     if (c == 0.0f)                            // rows between users, and tokens without weight: 0 whatever the logits are
 #pragma unroll
-        for (int k = I; k < I + 64; ++k) x[k] = 0.0f;
+        for (int k = 0; k < SPAN; ++k) x[k] = 0.0f;
     if (first + SPAN > a.vocab)
 #pragma unroll
-        for (int k = I; k < I + 64; ++k) if (first + k >= a.vocab) x[k] = 0.0f;
-    const uint32_t box = out.begin();
+        for (int k = 0; k < SPAN; ++k) if (first + k >= a.vocab) x[k] = 0.0f;
+    out.begin();
 #pragma unroll
-    for (int k = I; k < I + 64; k += 8) {
+    for (int k = 0; k < SPAN; k += 8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[k + j] *= c;
+        for (int j = k; j < k + 8; j += 2) (Two(x[j], x[j + 1]) * factor).get(x[j], x[j + 1]);
         const uint4 u = T::pack(x + k);
-        OutBox::put(box, (k - I) / 8, u);
+        out.put(k / 8, u);
         if (LOW) {
             float y[8];
             T::unpack(u, y);
@@ -313,78 +336,108 @@ __device__ __forceinline__ void dz_half(const GemmArgs& a, float (&x)[SPAN], int
             for (int j = 0; j < 8; ++j) x[k + j] -= y[j];
         }
     }
-    OutBox::send(box, &a.out, column + I, row0, 0, true);
+    out.send2(&a.out, column, row0);
     if (LOW) {
-        const uint32_t low = out.begin();
+        out.begin();
 #pragma unroll
-        for (int k = I; k < I + 64; k += 8) OutBox::put(low, (k - I) / 8, T::pack(x + k));
-        OutBox::send(low, &a.out_low, column + I, row0, 0, true);
+        for (int k = 0; k < SPAN; k += 8) out.put(k / 8, T::pack(x + k));
+        out.send2(&a.out_low, column, row0);
     }
 }
 
-template <class T, bool ONE, bool LOW>
-__device__ __forceinline__ void end_dz(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int row0, int half, Entries<ONE>& e, OutBox& out) {
-    const int column = w.n + half * SPAN, first = a.v0 + column;
-    const bool here = row < rows;
-    const float lse = here ? a.p.row_lse[row] : 0.0f, c = here ? a.p.row_c[row] : 0.0f;
-    dz_half<0, T, ONE, LOW>(a, x, first, column, row0, lse, c, e, out);
-    dz_half<64, T, ONE, LOW>(a, x, first, column, row0, lse, c, e, out);
+// Each sum is written or added to once: no order of additions is left open.  (Stored from registers, a row a lane, a tile's end took 20000 to
+// 50000 cycles.)
+__device__ __forceinline__ void end_dhidden(const GemmArgs& a, const TileWork& w, int rows, const float (&x)[SPAN], int row0, int quarter, const OutBox& out) {
+    const int first = w.n + quarter * SPAN;
+    if (row0 >= rows) return;                 // for the whole warp; rows behind the last one are nobody's
+#pragma unroll
+    for (int c = 0; c < SPAN; c += 32) {
+        if (first + c >= a.dim) break;
+        out.begin();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) out.put(k, OF32::pack(x + c + 4 * k));
+        out.send3(&a.out, first + c, row0, w.split, a.add);
+    }
 }
 
-__device__ __forceinline__ void end_dhidden(const GemmArgs& a, const TileWork& w, int rows, const float (&x)[SPAN], int64_t row, int half) {
-    const int first = w.n + half * SPAN;
-    if (row >= rows) return;
-    float* to = a.partial + ((int64_t)w.split * a.rows + row) * a.dim + first;
+// dweight where its rows begin anywhere, or are added to: 32 rows of 64 columns turned round in shared memory, so that a store is one piece of
+// a row, two elements of 16 bits a lane.  D: the type of dweight.
+template <class D>
+__device__ __forceinline__ void put_rows(const GemmArgs& a, typename D::type* base, int rows, int columns, const float (&x)[SPAN], const OutBox& out) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t* const box = (const uint32_t*)__cvta_shared_to_generic(out.at);
+    // word `lane` of row r: the 16-byte pieces of a row lie where OutBox::put has them
+    auto word = [&](int r) { return box[r * 32 + (((lane >> 2) ^ (r & 7)) << 2 | (lane & 3))]; };
+    const int64_t pitch = a.dim;
+    if constexpr (sizeof(typename D::type) == 4) {
 #pragma unroll
-    for (int k = 0; k < SPAN; k += 4) {
-        if (first + k >= a.dim) break;        // dim is a multiple of 8
-        float4 s = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-        float4* p = (float4*)(to + k);
-        if (a.add) { const float4 o = *p; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
-        *p = s;
+        for (int c = 0; c < SPAN; c += 32) {
+            if (c >= columns) break;
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) out.put(k, D::pack(x + c + 4 * k));
+            __syncwarp();
+            if (c + lane >= columns) continue;
+            float* p = (float*)base + c + lane;
+            if (a.dw.accumulate)
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r, p += pitch) *p += __uint_as_float(word(r));
+            else
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r, p += pitch) *p = __uint_as_float(word(r));
+        }
+    } else {
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) out.put(k, D::pack(x + 8 * k));
+        __syncwarp();
+        const int pairs = columns < SPAN ? columns / 2 : SPAN / 2;            // columns are even
+        typename D::type* p = base + 2 * lane;
+        if (a.dw.accumulate) {
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r, p += pitch) {
+                float f, g;
+                D::unpack2(word(r), f, g);
+                if (lane < pairs) { p[0] = D::put(D::get(p[0]) + f); p[1] = D::put(D::get(p[1]) + g); }
+            }
+        } else if (((uintptr_t)base & 2) == 0) {          // rows have an even number of elements: all begin at 4 bytes, or none does
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r, p += pitch)
+                if (lane < pairs) *(uint32_t*)p = word(r);
+        } else {                              // a whole word is a pair's first element and the one before it, which the lane before has
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r, p += pitch) {
+                const uint32_t mine = word(r), before = __shfl_up_sync(0xffffffffu, mine, 1);
+                if (lane >= pairs) continue;
+                if (lane) *(uint32_t*)(p - 1) = before >> 16 | mine << 16;
+                else *(uint16_t*)p = (uint16_t)mine;
+                if (lane == pairs - 1) ((uint16_t*)p)[1] = (uint16_t)(mine >> 16);
+            }
+        }
     }
 }
 
 // D: the type of dweight.
 template <class D>
-__device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w, float (&x)[SPAN], int row0, int half, float (*turn)[33], OutBox& out) {
-    const int lane = threadIdx.x & 31, first = w.n + half * SPAN, v = a.v0 + row0;
-    if (v >= a.vocab) return;
+__device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w, float (&x)[SPAN], int row0, int quarter, const OutBox& out) {
+    const int first = w.n + quarter * SPAN, v = a.v0 + row0;
+    if (v >= a.vocab || first >= a.dim) return;
     const float down = 1.0f / a.p.up[w.user];
+    const Two by(down, down);
 #pragma unroll
-    for (int k = 0; k < SPAN; ++k) x[k] *= down;
-    if (a.dw_wide) {
-        constexpr int BOX = 128 / sizeof(typename D::type);
-#pragma unroll
-        for (int c = 0; c < SPAN; c += BOX) {
-            if (first + c >= a.dim) break;
-            const uint32_t box = out.begin();
-#pragma unroll
-            for (int k = 0; k < 8; ++k) OutBox::put(box, k, D::pack(x + c + k * D::EACH));
-            OutBox::send(box, &a.out, first + c, v, w.user, false);
-        }
+    for (int k = 0; k < SPAN; k += 2) (Two(x[k], x[k + 1]) * by).get(x[k], x[k + 1]);
+    if (!a.dw_wide) {
+        put_rows<D>(a, (typename D::type*)a.dw.data + w.user * a.dw.user_stride + (int64_t)v * a.dim + first, a.vocab - v < 32 ? a.vocab - v : 32, a.dim - first, x, out);
         return;
     }
-    typename D::type* base = (typename D::type*)a.dw.data + w.user * a.dw.user_stride + (int64_t)v * a.dim;
-    const int count = a.vocab - v < 32 ? a.vocab - v : 32;
+    constexpr int BOX = 128 / sizeof(typename D::type);
 #pragma unroll
-    for (int c = 0; c < SPAN; c += 32) {
-        const int column = first + c;
-        if (column >= a.dim) break;
-        // turned round in shared memory, so that a store is one piece of a row
+    for (int c = 0; c < SPAN; c += BOX) {
+        if (first + c >= a.dim) break;
+        out.begin();
 #pragma unroll
-        for (int k = 0; k < 32; ++k) turn[lane][k] = x[c + k];
-        __syncwarp();
-        if (column + lane < a.dim) {
-            typename D::type* p = base + column + lane;
-            if (a.dw.accumulate)
-#pragma unroll 8
-                for (int r = 0; r < count; ++r, p += a.dim) *p = D::put(D::get(*p) + turn[r][lane]);
-            else
-#pragma unroll 8
-                for (int r = 0; r < count; ++r, p += a.dim) *p = D::put(turn[r][lane]);
-        }
-        __syncwarp();
+        for (int k = 0; k < 8; ++k) out.put(k, D::pack(x + c + k * D::EACH));
+        out.send3(&a.out, first + c, v, w.user, false);
     }
 }
 
@@ -499,17 +552,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
             fine &= bar_wait(drained, 0);
         }
     } else {
-        const int part = warp & 3, half = (warp - FIRST_EPI) >> 2;         // a warp reads the quarter of the lanes that its number gives
+        const int part = warp & 3, quarter = (warp - FIRST_EPI) >> 2;         // a warp reads the fourth of the lanes that its number gives
         uint32_t turn_no = 0;
         const uint32_t far_free = at_rank(free_, 0);
-        uint8_t* const mine = stages + STAGES * STAGE_BYTES + (warp - FIRST_EPI) * 8192;
-        OutBox out = {shared_at(mine), 0};
+        const OutBox out = {shared_at(stages + STAGES * STAGE_BYTES + (warp - FIRST_EPI) * 4096)};
         for (int64_t i = pair; fine && tile_at<MODE>(a, rows, i, w); i += pairs) {
             const int in_tile = (int)rank * 128 + part * 32;
             const int64_t row = (int64_t)w.m + in_tile + lane;
             Entries<ONE> e;                   // looked for while the products run
             if constexpr (MODE == STATS || MODE == DZ) {
-                const int first = a.v0 + w.n + half * SPAN;
+                const int first = a.v0 + w.n + quarter * SPAN;
                 e.begin(a, row < rows && first < a.vocab, row, first);
             }
             float x[SPAN];
@@ -519,21 +571,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
                 if (!(fine = bar_wait(done + 8 * buffer, turn_no >> 1 & 1))) break;
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t at = tmem + buffer * TILE + half * SPAN + ((uint32_t)part << 21);        // lane 32 part
+                const uint32_t at = tmem + buffer * TILE + quarter * SPAN + ((uint32_t)part << 21);     // lane 32 part
                 if (k == w.k0) {
-#pragma unroll
-                    for (int c = 0; c < SPAN; c += 32) tmem_load32(at + c, x + c);
-                    tmem_loaded(x);
-#pragma unroll
-                    for (int c = 32; c < SPAN; c += 32) tmem_loaded_too(x + c);
+                    tmem_load32(at, x);
+                    tmem_load32(at + 32, x + 32);
+                    tmem_loaded32(x);
+                    tmem_loaded32_too(x + 32);
                 } else
 #pragma unroll
-                    for (int c = 0; c < SPAN; c += 32) {
-                        float y[32];
-                        tmem_load32(at + c, y);
-                        tmem_loaded(y);
+                    for (int c = 0; c < SPAN; c += 16) {
+                        float y[16];
+                        tmem_load16(at + c, y);
+                        tmem_loaded16(y);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) x[c + j] += y[j];
+                        for (int j = 0; j < 16; ++j) x[c + j] += y[j];
                     }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -545,13 +596,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
             if (w.k0 >= w.k1)                 // no depth (a user without a token that counts): the sums are 0
 #pragma unroll
                 for (int j = 0; j < SPAN; ++j) x[j] = 0.0f;
-            if constexpr (MODE == STATS) end_stats<ONE>(a, w, rows, x, row, half, e);
-            if constexpr (MODE == DZ) end_dz<T, ONE, LOW>(a, w, rows, x, row, w.m + in_tile, half, e, out);
-            if constexpr (MODE == DHIDDEN) end_dhidden(a, w, rows, x, row, half);
-            if constexpr (MODE == DWEIGHT) end_dweight<D>(a, w, x, w.m + in_tile, half, (float(*)[33])mine, out);
+            if constexpr (MODE == STATS) end_stats<ONE>(a, w, rows, x, row, quarter, e);
+            if constexpr (MODE == DZ) end_dz<T, ONE, LOW>(a, w, rows, x, row, w.m + in_tile, quarter, e, out);
+            if constexpr (MODE == DHIDDEN) end_dhidden(a, w, rows, x, w.m + in_tile, quarter, out);
+            if constexpr (MODE == DWEIGHT) end_dweight<D>(a, w, x, w.m + in_tile, quarter, out);
             __syncwarp();
         }
-        if (MODE == DZ || MODE == DWEIGHT) OutBox::finish();
+        if (MODE != STATS) out.finish();
     }
     if (!fine) atomicOr(&a.status->flags, CO3_FLAG_TIMEOUT);
     __syncwarp();
@@ -573,7 +624,7 @@ struct Targets {
 };
 __device__ __forceinline__ int64_t index_at(const Targets& k, int64_t at) { return k.wide ? ((const int64_t*)k.data)[at] : (int64_t)((const int32_t*)k.data)[at]; }
 
-// A warp per token: its entries in the order of their numbers, their shares q, sum q log q, and for each 128 columns how many lie before.
+// A warp per token: its entries in the order of their numbers, their shares q, sum q log q, and for each 64 columns how many lie before.
 struct EntryArgs {
     Targets k;
     int64_t n_all;
@@ -898,7 +949,7 @@ struct co3_token_loss {
     int users, type, grad_type, max_top, device, pairs, spans, max_splits;
     int64_t piece;                            // columns of dz that are held at a time
     EncodeTiled encode;
-    CUtensorMap map_hidden, map_dz, map_low, map_dz_out, map_low_out;
+    CUtensorMap map_hidden, map_dz, map_low, map_dz_out, map_low_out, map_partial;
     void* slab;
     OpsStatus* status;
     Packed p;
@@ -920,14 +971,14 @@ bool make_map(const co3_token_loss* h, CUtensorMap* map, const void* data, int64
     return h->encode(map, map_type(h->type), 2, (void*)data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// dweight in boxes of 128 bytes and 32 rows.
-bool make_grad_map(const co3_token_loss* h, CUtensorMap* map, const co3_param_grad* g) {
-    const int width = type_width(g->type);
-    const cuuint64_t dims[3] = {(cuuint64_t)h->dim, (cuuint64_t)h->vocab, (cuuint64_t)h->users};
-    const cuuint64_t strides[2] = {(cuuint64_t)(h->dim * width), (cuuint64_t)((h->users > 1 ? g->user_stride : h->dim * h->vocab) * width)};
+// dweight in boxes of 128 bytes and 32 rows; partial likewise.
+bool make_out_map(const co3_token_loss* h, CUtensorMap* map, void* data, int type, int64_t rows, int64_t pieces, int64_t piece_stride) {
+    const int width = type_width(type);
+    const cuuint64_t dims[3] = {(cuuint64_t)h->dim, (cuuint64_t)rows, (cuuint64_t)pieces};
+    const cuuint64_t strides[2] = {(cuuint64_t)(h->dim * width), (cuuint64_t)(piece_stride * width)};
     const cuuint32_t box[3] = {(cuuint32_t)(128 / width), 32, 1}, one[3] = {1, 1, 1};
     return strides[1] < (cuuint64_t)1 << 40 &&
-           h->encode(map, map_type(g->type), 3, g->data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           h->encode(map, map_type(type), 3, data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1008,7 +1059,7 @@ int begin_call(co3_token_loss* h, const co3_array* hidden, const void* weight, i
     if (!make_map(h, &a.b, weight, h->dim, h->vocab, weight_stride)) return CO3_EINVAL;
     a.p = h->p; a.status = h->status; a.users = h->users; a.vocab = (int)h->vocab; a.dim = (int)h->dim; a.splits = 1; a.terms = 1; a.rows = h->rows;
     a.scale = LOG2E / temperature; a.stats = h->stats; a.dots = h->dots; a.entry = h->entry; a.entry_q = h->q; a.entry_first = h->first; a.top = k.top;
-    a.spans = h->spans; a.partial = h->partial;
+    a.spans = h->spans;
     return CO3_OK;
 }
 
@@ -1046,7 +1097,7 @@ template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* 
     if (dweight) {
         const int width = type_width(dweight->type);
         wide = !dweight->accumulate && aligned_to(dweight->data, 16) && h->dim * width % 16 == 0 && (h->users == 1 || dweight->user_stride * width % 16 == 0) &&
-               make_grad_map(h, &map_dw, dweight);
+               make_out_map(h, &map_dw, dweight->data, dweight->type, h->vocab, h->users, h->users > 1 ? dweight->user_stride : h->dim * h->vocab);
     }
     if (dhidden) splits = splits_of(h, mt * nt, up_to(h->piece < h->vocab ? h->piece : h->vocab, KB) / KB);
     for (int64_t v0 = 0; v0 < h->vocab && rc == CO3_OK; v0 += h->piece) {
@@ -1060,7 +1111,7 @@ template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* 
         rc = gemm(h, dz, mt * ct, a, st);
         if (rc == CO3_OK && dhidden) {
             GemmArgs b = a;
-            b.a = h->map_dz; b.splits = splits; b.add = v0 > 0;
+            b.a = h->map_dz; b.out = h->map_partial; b.splits = splits; b.add = v0 > 0;
             rc = gemm(h, gemm_kernel<DHIDDEN, T, T, true, false>, mt * nt * splits, b, st);
         }
         if (rc == CO3_OK && dweight) {
@@ -1146,7 +1197,7 @@ extern "C" int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_
             h->entry = (int32_t*)(base + o_e); h->q = (float*)(base + o_q); h->constant = (float*)(base + o_k); h->first = (uint8_t*)(base + o_f); h->mass = (uint8_t*)(base + o_m);
             if (cudaMemset(h->status, 0, sizeof(OpsStatus)) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess ||
                 !make_map(h, &h->map_hidden, h->hidden, h->dim, h->rows, h->dim) || !make_map(h, &h->map_dz, h->dz, h->piece, h->rows, h->piece) ||
-                !make_map(h, &h->map_dz_out, h->dz, h->piece, h->rows, h->piece, 32) ||
+                !make_out_map(h, &h->map_partial, h->partial, CO3_F32, h->rows, h->max_splits, h->rows * h->dim) || !make_map(h, &h->map_dz_out, h->dz, h->piece, h->rows, h->piece, 32) ||
                 (h->grad_type == CO3_F32 && (!make_map(h, &h->map_low, h->low, h->piece, h->rows, h->piece) || !make_map(h, &h->map_low_out, h->low, h->piece, h->rows, h->piece, 32)))) rc = CO3_ECUDA;
         }
     }
