@@ -3,7 +3,7 @@
 // All products run through one kernel on the tensor cores: pairs of thread blocks (two SMs) on tiles of 256 x 256, operands brought by TMA
 // into a ring of stages, accumulators in tensor memory, two of them, so that the products of the next tile run while sixteen warps of
 // each block work on the last one:
-//   STATS   z = H W^T                     -> per row and 64 columns: largest logit, sum of exponentials, weighted target logits
+//   STATS   z = H W^T                     -> per row and 256 columns: largest logit, sum of exponentials, weighted target logits
 //   DZ      z again, for a piece of the vocabulary -> dz, in 16 bits (and its remainder in 16 more, for 32-bit gradients of the weight)
 //   DHIDDEN dz W    over the piece        -> 32-bit sums
 //   DWEIGHT dz^T H  over a user's tokens  -> the user's gradient
@@ -29,7 +29,7 @@ constexpr int OUT_BYTES = EPI_WARPS * 4096;   // a box of 32 rows of 128 bytes f
 constexpr int GEMM_SHARED = 1024 + STAGES * STAGE_BYTES + OUT_BYTES + 256;
 constexpr int ALIGN_ROWS = 64;                // a user's packed rows begin at a multiple of these
 constexpr int MAX_TOP = 128;
-constexpr int SPAN = 64;                      // columns of a warp, and of one set of statistics
+constexpr int SPAN = 64;                      // columns of a warp
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 enum Mode { STATS, DZ, DHIDDEN, DWEIGHT };
@@ -58,10 +58,10 @@ struct GemmArgs {
     int splits, terms;
     int64_t rows;                             // pitch of arrays [..][rows]
     float scale;                              // log2(e) / temperature
-    float2* stats;                            // [spans][rows] largest, sum
-    float* dots;                              // [spans][rows]
-    const int32_t* entry; const float* entry_q; const uint8_t* entry_first;      // [tokens][top], [tokens][top], [tokens][spans]
-    int top, spans;
+    float2* stats;                            // [tiles][rows] largest, sum
+    float* dots;                              // [tiles][rows]
+    const int32_t* entry; const float* entry_q; const uint8_t* entry_first;      // [tokens][top], [tokens][top], [tokens][tiles]
+    int top, tiles;                           // tiles of the vocabulary
     int add;                                  // to what partial [splits][rows][dim] holds
     co3_param_grad dw;
     int dw_wide;                              // rows of dweight begin at multiples of 16 bytes and are written
@@ -196,11 +196,12 @@ template <bool ONE> struct Entries {
         } else {
             const int64_t token = a.p.row_token[row];
             if (token < 0) return;
-            const int skip = a.entry_first[token * a.spans + first_column / SPAN];
+            const int skip = a.entry_first[token * a.tiles + first_column / TILE];
             left = a.top - skip;
             entry = a.entry + token * a.top + skip;
             q = a.entry_q + token * a.top + skip;
             fetch();
+            while (next < first_column) advance();        // those of the tile's columns before
         }
     }
     __device__ __forceinline__ void fetch() {
@@ -238,9 +239,12 @@ template <int C, bool ONE> __device__ __forceinline__ void subtract_entries(floa
     }
 }
 
-template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int quarter, Entries<ONE>& e) {
-    const int first = w.n + quarter * SPAN;   // the piece is the whole vocabulary
-    if (first >= a.vocab) return;
+// `sets`: of the four warps that have the same rows, [4 quarters][32 rows] of (largest, sum, weighted logits); there are two for tiles in turn,
+// and each warp waits until all have given theirs.
+template <bool ONE>
+__device__ __forceinline__ bool end_stats(const GemmArgs& a, const TileWork& w, int rows, float (&x)[SPAN], int64_t row, int quarter, Entries<ONE>& e, float* sets, uint32_t joined,
+                                          uint32_t parity) {
+    const int first = w.n + quarter * SPAN, lane = threadIdx.x & 31;      // the piece is the whole vocabulary
     float dot = 0.0f;
     take_entries<0>(x, first, e, dot);
     take_entries<32>(x, first, e, dot);
@@ -260,11 +264,23 @@ template <bool ONE> __device__ __forceinline__ void end_stats(const GemmArgs& a,
         fma(Two(x[k], x[k + 1]), scale, shift).get(y, z);
         s[k / 2 & 1] = s[k / 2 & 1] + Two(exp2_fast(y), exp2_fast(z));
     }
-    if (row < rows) {
-        const int64_t at = (int64_t)(first / SPAN) * a.rows + row;
-        a.stats[at] = make_float2(top, (s[0] + s[1]).sum());
-        a.dots[at] = dot;
-    }
+    float* const mine = sets + quarter * 96 + lane;
+    mine[0] = top; mine[32] = (s[0] + s[1]).sum(); mine[64] = dot;
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(joined) : "memory");
+    if (!bar_wait(joined, parity)) return false;
+    if (quarter || row >= rows) return true;
+    float t[4], all = top;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) { t[i] = sets[i * 96 + lane]; all = fmaxf(all, t[i]); }
+    const float base = all == -INFINITY ? 0.0f : all;
+    float sum = mine[32] * exp2_fast(top - base);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) { sum += sets[i * 96 + 32 + lane] * exp2_fast(t[i] - base); dot += sets[i * 96 + 64 + lane]; }
+    const int64_t at = (int64_t)(w.n / TILE) * a.rows + row;
+    a.stats[at] = make_float2(all, sum);
+    a.dots[at] = dot;
+    return true;
 }
 
 // Stores of a warp go by way of shared memory: 32 rows of 128 bytes in the order of the 128-byte swizzle, from where TMA takes them.
@@ -453,8 +469,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
     extern __shared__ uint8_t raw[];
     uint8_t* const stages = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     uint64_t* const bars = (uint64_t*)(stages + STAGES * STAGE_BYTES + OUT_BYTES);
-    const uint32_t full = shared_at(bars), empty = full + 8 * STAGES, done = empty + 8 * STAGES, free_ = done + 16, drained = free_ + 16;
-    volatile uint32_t* const tmem_at = (volatile uint32_t*)(bars + 2 * STAGES + 5);
+    const uint32_t full = shared_at(bars), empty = full + 8 * STAGES, done = empty + 8 * STAGES, free_ = done + 16, drained = free_ + 16, joined = drained + 8;
+    volatile uint32_t* const tmem_at = (volatile uint32_t*)(bars + 2 * STAGES + 9);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -462,6 +478,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
         for (int i = 0; i < STAGES; ++i) { bar_init(full + 8 * i, 1); bar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(done + 8 * i, 1); bar_init(free_ + 8 * i, 2 * EPI_WARPS); }
         bar_init(drained, 1);
+        for (int i = 0; i < 4; ++i) bar_init(joined + 8 * i, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -556,6 +573,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
         uint32_t turn_no = 0;
         const uint32_t far_free = at_rank(free_, 0);
         const OutBox out = {shared_at(stages + STAGES * STAGE_BYTES + (warp - FIRST_EPI) * 4096)};
+        float* const sets = (float*)(stages + STAGES * STAGE_BYTES) + part * 768;
+        uint32_t set = 0;
         for (int64_t i = pair; fine && tile_at<MODE>(a, rows, i, w); i += pairs) {
             const int in_tile = (int)rank * 128 + part * 32;
             const int64_t row = (int64_t)w.m + in_tile + lane;
@@ -596,7 +615,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
             if (w.k0 >= w.k1)                 // no depth (a user without a token that counts): the sums are 0
 #pragma unroll
                 for (int j = 0; j < SPAN; ++j) x[j] = 0.0f;
-            if constexpr (MODE == STATS) end_stats<ONE>(a, w, rows, x, row, quarter, e);
+            if constexpr (MODE == STATS) {
+                if (!(fine = end_stats<ONE>(a, w, rows, x, row, quarter, e, sets + (set & 1) * 384, joined + 8 * part, set & 1))) break;
+                ++set;
+            }
             if constexpr (MODE == DZ) end_dz<T, ONE, LOW>(a, w, rows, x, row, w.m + in_tile, quarter, e, out);
             if constexpr (MODE == DHIDDEN) end_dhidden(a, w, rows, x, w.m + in_tile, quarter, out);
             if constexpr (MODE == DWEIGHT) end_dweight<D>(a, w, x, w.m + in_tile, quarter, out);
@@ -624,12 +646,12 @@ struct Targets {
 };
 __device__ __forceinline__ int64_t index_at(const Targets& k, int64_t at) { return k.wide ? ((const int64_t*)k.data)[at] : (int64_t)((const int32_t*)k.data)[at]; }
 
-// A warp per token: its entries in the order of their numbers, their shares q, sum q log q, and for each 64 columns how many lie before.
+// A warp per token: its entries in the order of their numbers, their shares q, sum q log q, and for each tile of the vocabulary how many lie before it.
 struct EntryArgs {
     Targets k;
     int64_t n_all;
     uint32_t tokens;
-    int vocab, spans;
+    int vocab, tiles;
     float inv_t;
     int32_t* entry; float* q; float* constant; uint8_t* first; uint8_t* mass;
     OpsStatus* status;
@@ -696,18 +718,19 @@ __global__ void __launch_bounds__(256) entry_kernel(const __grid_constant__ Entr
         a.mass[n] = kept > 0;
     }
     __syncwarp();
-    for (int s = lane; s < a.spans; s += 32) {
+    for (int s = lane; s < a.tiles; s += 32) {
         int lo = 0, hi = (int)top;
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if ((int64_t)sh_sorted[warp][mid] < (int64_t)s * SPAN) lo = mid + 1; else hi = mid;
+            if ((int64_t)sh_sorted[warp][mid] < (int64_t)s * TILE) lo = mid + 1; else hi = mid;
         }
-        a.first[n * a.spans + s] = (uint8_t)lo;
+        a.first[n * a.tiles + s] = (uint8_t)lo;
     }
 }
 
 // One thread block: counts the tokens with a target, and gives each its packed row.
 constexpr int SEG = 256;                      // tokens that a warp counts
+constexpr int SEGS_NEAR = 2048, USERS_NEAR = 1024;
 struct PackArgs {
     Targets k;
     const uint8_t* mass;                      // null: one entry a token
@@ -728,12 +751,17 @@ __device__ __forceinline__ bool has_target(const PackArgs& a, uint32_t user, uin
     return v >= 0 && v < a.vocab;
 }
 __global__ void __launch_bounds__(1024) pack_kernel(const __grid_constant__ PackArgs a) {
-    __shared__ int warp_sums[32];
+    __shared__ int warp_sums[32], near_count[SEGS_NEAR], near_offset[USERS_NEAR + 1];
+    __shared__ float near_most[SEGS_NEAR];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t below = (1u << lane) - 1u;
     let_next_start();
     wait_for_previous();
     const int64_t all = (int64_t)a.users * a.segs;
+    // where the counts of a step are kept for the next: near if there is room
+    int32_t* const seg_count = all <= SEGS_NEAR ? near_count : a.seg_count;
+    float* const seg_most = all <= SEGS_NEAR ? near_most : a.seg_most;
+    int32_t* const offset = a.users <= USERS_NEAR ? near_offset : a.p.offset;
     for (int64_t g = warp; g < all; g += 32) {
         const uint32_t user = (uint32_t)(g / a.segs), t0 = (uint32_t)(g - (int64_t)user * a.segs) * SEG;
         int n = 0;
@@ -747,7 +775,7 @@ __global__ void __launch_bounds__(1024) pack_kernel(const __grid_constant__ Pack
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        if (lane == 0) { a.seg_count[g] = n; a.seg_most[g] = most; }
+        if (lane == 0) { seg_count[g] = n; seg_most[g] = most; }
     }
     __syncthreads();
     for (int user = warp; user < a.users; user += 32) {
@@ -756,19 +784,19 @@ __global__ void __launch_bounds__(1024) pack_kernel(const __grid_constant__ Pack
         for (uint32_t s0 = 0; s0 < a.segs; s0 += 32) {
             const uint32_t s = s0 + lane;
             const int64_t g = (int64_t)user * a.segs + s;
-            const int c = s < a.segs ? a.seg_count[g] : 0;
-            if (s < a.segs) most = fmaxf(most, a.seg_most[g]);
+            const int c = s < a.segs ? seg_count[g] : 0;
+            if (s < a.segs) most = fmaxf(most, seg_most[g]);
             int up = c;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += v; }
-            if (s < a.segs) a.seg_count[g] = sum + up - c;            // tokens with a target before the segment
+            if (s < a.segs) seg_count[g] = sum + up - c;            // tokens with a target before the segment
             sum += __shfl_sync(0xffffffffu, up, 31);
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         if (lane == 0) {
             a.p.count[user] = sum;
-            a.p.offset[user + 1] = (sum + ALIGN_ROWS - 1) / ALIGN_ROWS * ALIGN_ROWS;
+            offset[user + 1] = (sum + ALIGN_ROWS - 1) / ALIGN_ROWS * ALIGN_ROWS;
             float up = 1.0f;
             if (a.half) {                     // the largest factor to 2^13 .. 2^14: dz is at most that
                 most = a.dloss ? most * fabsf(a.scale) : fabsf(a.scale) / (float)(sum > 0 ? sum : 1);
@@ -786,22 +814,22 @@ __global__ void __launch_bounds__(1024) pack_kernel(const __grid_constant__ Pack
     int carry = 0;
     for (int u0 = 0; u0 < a.users; u0 += 1024) {          // running sum over the users
         const int user = u0 + (int)threadIdx.x;
-        int up = user < a.users ? a.p.offset[user + 1] : 0;
+        int up = user < a.users ? offset[user + 1] : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, up, o); if (lane >= o) up += v; }
         if (lane == 31) warp_sums[warp] = up;
         __syncthreads();
         int before = 0, total = 0;
         for (int w = 0; w < 32; ++w) { before += w < warp ? warp_sums[w] : 0; total += warp_sums[w]; }
-        if (user < a.users) a.p.offset[user + 1] = carry + before + up;
+        if (user < a.users) offset[user + 1] = carry + before + up;
         carry += total;
         __syncthreads();
     }
-    if (threadIdx.x == 0) a.p.offset[0] = 0;
+    if (threadIdx.x == 0) offset[0] = 0;
     __syncthreads();
     for (int64_t g = warp; g < all; g += 32) {
         const uint32_t user = (uint32_t)(g / a.segs), t0 = (uint32_t)(g - (int64_t)user * a.segs) * SEG;
-        int row = a.p.offset[user] + a.seg_count[g];
+        int row = offset[user] + seg_count[g];
 #pragma unroll
         for (int i = 0; i < SEG / 32; ++i) {
             const uint32_t t = t0 + i * 32 + lane;
@@ -814,8 +842,9 @@ __global__ void __launch_bounds__(1024) pack_kernel(const __grid_constant__ Pack
             row += __popc(mask);
         }
     }
+    for (int i = threadIdx.x; offset != a.p.offset && i <= a.users; i += 1024) a.p.offset[i] = offset[i];
     for (int user = warp; user < a.users; user += 32)     // the zero rows behind a user's
-        for (int r = a.p.offset[user] + a.p.count[user] + lane; r < a.p.offset[user + 1]; r += 32) a.p.row_token[r] = -1;
+        for (int r = offset[user] + a.p.count[user] + lane; r < offset[user + 1]; r += 32) a.p.row_token[r] = -1;
 }
 
 // A warp per packed row: the hidden state, and what the tiles' ends need of the token.
@@ -854,45 +883,63 @@ template <bool VEC> __global__ void __launch_bounds__(256) gather_kernel(const _
     a.p.row_c[row] = n < 0 ? 0.0f : (a.dloss ? a.dloss[n] * a.scale : a.scale / (float)a.p.count[user]) * a.p.up[user];
 }
 
-// Statistics of the spans to loss and lse: 32 tokens, eight stretches of the spans, joined in order.
+// Statistics of the tiles to loss and lse: 32 tokens, 32 warps with a stretch of the tiles each, joined in order.
+constexpr int LOSS_WARPS = 32;
 struct LossArgs {
     const float2* stats;
     const float *dots, *constant;
     int64_t rows, n_all;
-    int spans;
+    int tiles;
     float inv_t;
     Packed p;
     float *loss, *lse;
 };
-__global__ void __launch_bounds__(256) loss_kernel(const __grid_constant__ LossArgs a) {
-    __shared__ float sh[8][32][3];
+__global__ void __launch_bounds__(32 * LOSS_WARPS) loss_kernel(const __grid_constant__ LossArgs a) {
+    __shared__ float sh[LOSS_WARPS][3][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n = (int64_t)blockIdx.x * 32 + lane;
     let_next_start();
     wait_for_previous();
     const int row = n < a.n_all ? a.p.token_row[n] : -1;
     float m = -INFINITY, s = 0.0f, dot = 0.0f;
-    auto join = [&](float m2, float s2, float d2) {
-        const float big = fmaxf(m, m2), from = big == -INFINITY ? 0.0f : big;
-        s = s * exp2_fast(m - from) + s2 * exp2_fast(m2 - from);
-        m = big;
-        dot += d2;
-    };
     if (row >= 0) {
-        const int each = (a.spans + 7) / 8, end = (warp + 1) * each < a.spans ? (warp + 1) * each : a.spans;
-#pragma unroll 4
-        for (int i = warp * each; i < end; ++i) {
-            const float2 x = a.stats[i * a.rows + row];
-            join(x.x, x.y, a.dots[i * a.rows + row]);
+        const int each = (a.tiles + LOSS_WARPS - 1) / LOSS_WARPS, end = (warp + 1) * each < a.tiles ? (warp + 1) * each : a.tiles;
+        for (int i0 = warp * each; i0 < end; i0 += 8) {       // eight loads on their way
+            float2 x[8];
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool here = i0 + i < end;
+                x[i] = here ? a.stats[(i0 + i) * a.rows + row] : make_float2(-INFINITY, 0.0f);
+                d[i] = here ? a.dots[(i0 + i) * a.rows + row] : 0.0f;
+            }
+            float big = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) big = fmaxf(big, x[i].x);
+            const float from = big == -INFINITY ? 0.0f : big;
+            s *= exp2_fast(m - from);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { s += x[i].y * exp2_fast(x[i].x - from); dot += d[i]; }
+            m = big;
         }
     }
-    sh[warp][lane][0] = m; sh[warp][lane][1] = s; sh[warp][lane][2] = dot;
+    sh[warp][0][lane] = m; sh[warp][1][lane] = s; sh[warp][2][lane] = dot;
     __syncthreads();
-    if (warp || n >= a.n_all) return;
-    for (int w = 1; w < 8; ++w) join(sh[w][lane][0], sh[w][lane][1], sh[w][lane][2]);
-    const float lse = row < 0 ? 0.0f : (m + log2f(s)) * LN2;
-    a.lse[n] = lse;
-    a.loss[n] = row < 0 ? 0.0f : (lse - dot * a.inv_t) + (a.constant ? a.constant[n] : 0.0f);
+    // a token a warp: its 32 stretches over the lanes
+    const int64_t mine = (int64_t)blockIdx.x * 32 + warp;
+    if (mine >= a.n_all) return;
+    m = sh[lane][0][warp]; s = sh[lane][1][warp]; dot = sh[lane][2][warp];
+    float big = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    const float from = big == -INFINITY ? 0.0f : big;
+    s = warp_sum_f32(s * exp2_fast(m - from));
+    dot = warp_sum_f32(dot);
+    if (lane) return;
+    const bool none = a.p.token_row[mine] < 0;
+    const float lse = none ? 0.0f : (big + log2f(s)) * LN2;
+    a.lse[mine] = lse;
+    a.loss[mine] = none ? 0.0f : (lse - dot * a.inv_t) + (a.constant ? a.constant[mine] : 0.0f);
 }
 
 // The splits' sums to dhidden, a warp to 256 columns of a token.
@@ -946,7 +993,7 @@ typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, v
 
 struct co3_token_loss {
     int64_t vocab, dim, max_tokens, rows, launches;       // rows: all packed ones there can be, to whole tiles
-    int users, type, grad_type, max_top, device, pairs, spans, max_splits;
+    int users, type, grad_type, max_top, device, pairs, tiles, max_splits;
     int64_t piece;                            // columns of dz that are held at a time
     EncodeTiled encode;
     CUtensorMap map_hidden, map_dz, map_low, map_dz_out, map_low_out, map_partial;
@@ -1035,7 +1082,7 @@ int begin_call(co3_token_loss* h, const co3_array* hidden, const void* weight, i
     int rc = CO3_OK;
     if (teacher) {
         EntryArgs e;
-        e.k = k; e.n_all = n_all; e.tokens = (uint32_t)n_tokens; e.vocab = (int)h->vocab; e.spans = h->spans; e.inv_t = 1.0f / temperature;
+        e.k = k; e.n_all = n_all; e.tokens = (uint32_t)n_tokens; e.vocab = (int)h->vocab; e.tiles = h->tiles; e.inv_t = 1.0f / temperature;
         e.entry = h->entry; e.q = h->q; e.constant = h->constant; e.first = h->first; e.mass = h->mass; e.status = h->status;
         rc = launch_early(&h->launches, entry_kernel, dim3(blocks_for(n_all, 8)), 256, 0, 1, st, e);
         if (rc != CO3_OK) return rc;
@@ -1059,7 +1106,7 @@ int begin_call(co3_token_loss* h, const co3_array* hidden, const void* weight, i
     if (!make_map(h, &a.b, weight, h->dim, h->vocab, weight_stride)) return CO3_EINVAL;
     a.p = h->p; a.status = h->status; a.users = h->users; a.vocab = (int)h->vocab; a.dim = (int)h->dim; a.splits = 1; a.terms = 1; a.rows = h->rows;
     a.scale = LOG2E / temperature; a.stats = h->stats; a.dots = h->dots; a.entry = h->entry; a.entry_q = h->q; a.entry_first = h->first; a.top = k.top;
-    a.spans = h->spans;
+    a.tiles = h->tiles;
     return CO3_OK;
 }
 
@@ -1084,9 +1131,9 @@ template <class T> int forward_of(co3_token_loss* h, Call& c, float temperature,
     int rc = gemm(h, c.one ? gemm_kernel<STATS, T, T, true, false> : gemm_kernel<STATS, T, T, false, false>, tiles, a, st);
     if (rc != CO3_OK) return rc;
     LossArgs l;
-    l.stats = h->stats; l.dots = h->dots; l.constant = c.one ? nullptr : h->constant; l.rows = h->rows; l.n_all = c.n_all; l.spans = h->spans;
+    l.stats = h->stats; l.dots = h->dots; l.constant = c.one ? nullptr : h->constant; l.rows = h->rows; l.n_all = c.n_all; l.tiles = h->tiles;
     l.inv_t = 1.0f / temperature; l.p = h->p; l.loss = loss; l.lse = lse;
-    return launch_early(&h->launches, loss_kernel, dim3((unsigned)((c.n_all + 31) / 32)), 256, 0, 1, st, l);
+    return launch_early(&h->launches, loss_kernel, dim3((unsigned)((c.n_all + 31) / 32)), 32 * LOSS_WARPS, 0, 1, st, l);
 }
 
 template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* dhidden, const co3_param_grad* dweight, int64_t n_tokens, cudaStream_t st) {
@@ -1151,7 +1198,7 @@ extern "C" int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_
     memset((void*)h, 0, sizeof(*h));
     h->vocab = cfg->vocab; h->dim = cfg->dim; h->max_tokens = cfg->max_tokens; h->users = cfg->n_users;
     h->type = cfg->type; h->grad_type = cfg->grad_type; h->max_top = cfg->max_top;
-    h->spans = (int)((h->vocab + SPAN - 1) / SPAN);
+    h->tiles = (int)((h->vocab + TILE - 1) / TILE);
     h->rows = up_to(up_to(h->max_tokens, ALIGN_ROWS) * h->users, TILE);
     if (h->rows == 0) h->rows = TILE;
     // dz of a piece of the vocabulary: 256 MB, at least 2048 columns.  Pieces of one size.
@@ -1180,10 +1227,10 @@ extern "C" int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_
         const size_t o_status = part(sizeof(OpsStatus)), o_off = part(4 * (size_t)(h->users + 1)), o_cnt = part(4 * (size_t)h->users), o_up = part(4 * (size_t)h->users);
         const size_t o_rt = part(4 * rows), o_tr = part(4 * tokens), o_c = part(4 * rows), o_lse = part(4 * rows), o_tgt = part(4 * rows);
         const size_t o_sc = part(4 * segs), o_sm = part(4 * segs);
-        const size_t o_h = part(rows * h->dim * 2), o_stats = part(8 * rows * h->spans), o_dots = part(4 * rows * h->spans);
+        const size_t o_h = part(rows * h->dim * 2), o_stats = part(8 * rows * h->tiles), o_dots = part(4 * rows * h->tiles);
         const size_t o_dz = part(rows * h->piece * 2), o_low = part(h->grad_type == CO3_F32 ? rows * h->piece * 2 : 0);
         const size_t o_part = part(4 * rows * h->dim * h->max_splits);
-        const size_t o_e = part(4 * tokens * top), o_q = part(4 * tokens * top), o_k = part(4 * tokens), o_f = part(tokens * h->spans), o_m = part(tokens);
+        const size_t o_e = part(4 * tokens * top), o_q = part(4 * tokens * top), o_k = part(4 * tokens), o_f = part(h->max_top > 1 ? tokens * h->tiles : tokens), o_m = part(tokens);
         if (cudaMalloc(&h->slab, at) != cudaSuccess) { h->slab = nullptr; rc = CO3_ENOMEM; }
         else {
             char* base = (char*)h->slab;
