@@ -1068,7 +1068,7 @@ class Embedding(_Operator):
 
     _kind = "embed"
 
-    def __init__(self, vocab, dim, n_users=1, tokens=0):
+    def __init__(self, vocab, dim, n_users=1, *, tokens):
         self.vocab, self.dim = int(vocab), int(dim)
         self._create(lambda h: lib().co3_embed_create(h, self.vocab, self.dim, int(n_users), int(tokens)), n_users)
 
@@ -1177,7 +1177,7 @@ class TokenLoss(_Operator):
 
     _kind = "token_loss"
 
-    def __init__(self, vocab, dim, n_users=1, tokens=0, dtype=None, grad_dtype=None, top=1):
+    def __init__(self, vocab, dim, n_users=1, *, tokens, dtype=None, grad_dtype=None, top=1):
         import torch
         self.vocab, self.dim, self.dtype, self.grad_dtype = int(vocab), int(dim), dtype or torch.bfloat16, grad_dtype or torch.float32
         cfg = TokenLossConfig(self.vocab, self.dim, int(tokens), int(n_users), _type_code(self.dtype), _type_code(self.grad_dtype), int(top))

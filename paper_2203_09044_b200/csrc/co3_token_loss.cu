@@ -409,7 +409,7 @@ __device__ __forceinline__ void put_rows(const GemmArgs& a, typename D::type* ba
         __syncwarp();
         const int pairs = columns < SPAN ? columns / 2 : SPAN / 2;            // columns are even
         typename D::type* p = base + 2 * lane;
-        if (a.dw.accumulate) {
+        if (a.dw.accumulate) {                // two roundings: of this call's sum, and of what it makes with the one before
 #pragma unroll 4
             for (int r = 0; r < rows; ++r, p += pitch) {
                 float f, g;
@@ -458,11 +458,13 @@ __device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------------------
-// Stages of depth that an accumulator takes: the tensor cores cut a sum's last bits off at each 16 of depth (0.2 .. 0.7 units in the
-// last place of 32 bits, always towards zero), so sums over more are added up in registers, rounded to nearest (z over 4096: 4.5e-6 of it in one
-// sum).  dhidden is rounded to 16 bits in the end.
-template <int MODE> constexpr int CHUNK = MODE == DHIDDEN ? 1 << 20 : 16;
+// Stages of depth that an accumulator takes.  The tensor cores cut a sum's last bits off at each 16 of depth (0.2 .. 0.7 units in the last
+// place of 32 bits, always towards zero), so where results have 32 bits, sums over more than 1024 are added up in registers, rounded to nearest (z
+// over 4096: 4.5e-6 of it off in one sum, 1.1e-6 in four).  Reading an accumulator out holds the products up for about 2300 cycles, against the
+// 8192 that they take over 1024, so what is rounded to 16 bits in the end is one sum.
+template <int MODE, class D> constexpr int CHUNK = MODE == STATS || (MODE != DHIDDEN && sizeof(typename D::type) == 4) ? 16 : 1 << 20;
 
+// D: the type of dweight.  LOW: dz in two numbers.
 template <int MODE, class T, class D, bool ONE, bool LOW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs a) {
     constexpr bool A_ALONG = MODE != DWEIGHT, B_ALONG = MODE == STATS || MODE == DZ;       // whether the depth runs along the matrix' rows
@@ -545,7 +547,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
                     const uint32_t buffer = turn_no & 1, to = tmem + buffer * TILE;
                     if (!(fine = bar_wait(free_ + 8 * buffer, (turn_no >> 1 & 1) ^ 1))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const int k2 = w.k1 - k < CHUNK<MODE> ? w.k1 : k + CHUNK<MODE>;
+                    const int k2 = w.k1 - k < CHUNK<MODE, D> ? w.k1 : k + CHUNK<MODE, D>;
                     for (bool add = false; k < k2; ++k) {
                         if (!(fine = bar_wait(full + 8 * s, phase))) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -609,7 +611,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
                 __syncwarp();
                 if (lane == 0) bar_arrive_cluster(far_free + 8 * buffer);
                 ++turn_no;
-                k = w.k1 - k < CHUNK<MODE> ? w.k1 : k + CHUNK<MODE>;
+                k = w.k1 - k < CHUNK<MODE, D> ? w.k1 : k + CHUNK<MODE, D>;
             } while (k < w.k1);
             if (!fine) break;
             if (w.k0 >= w.k1)                 // no depth (a user without a token that counts): the sums are 0
@@ -1035,7 +1037,8 @@ template <class K> bool big_shared(K kernel) {
 template <class T> bool all_big() {
     return big_shared(gemm_kernel<STATS, T, T, true, false>) && big_shared(gemm_kernel<STATS, T, T, false, false>) &&
            big_shared(gemm_kernel<DZ, T, T, true, false>) && big_shared(gemm_kernel<DZ, T, T, false, false>) &&
-           big_shared(gemm_kernel<DZ, T, T, true, true>) && big_shared(gemm_kernel<DZ, T, T, false, true>) &&
+           big_shared(gemm_kernel<DZ, T, OF32, true, false>) && big_shared(gemm_kernel<DZ, T, OF32, false, false>) &&
+           big_shared(gemm_kernel<DZ, T, OF32, true, true>) && big_shared(gemm_kernel<DZ, T, OF32, false, true>) &&
            big_shared(gemm_kernel<DHIDDEN, T, T, true, false>) && big_shared(gemm_kernel<DWEIGHT, T, T, true, false>) &&
            big_shared(gemm_kernel<DWEIGHT, T, OF32, true, false>);
 }
@@ -1153,8 +1156,10 @@ template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* 
         a.v0 = (int)v0;
         a.columns = (int)(h->vocab - v0 < h->piece ? h->vocab - v0 : h->piece);
         const int64_t ct = up_to(a.columns, TILE) / TILE;
-        void (*dz)(GemmArgs) = c.one ? (low ? gemm_kernel<DZ, T, T, true, true> : gemm_kernel<DZ, T, T, true, false>)
-                                     : (low ? gemm_kernel<DZ, T, T, false, true> : gemm_kernel<DZ, T, T, false, false>);
+        // dz is summed alike with and without dweight: so dhidden has the same bits
+        void (*dz)(GemmArgs) = low                       ? (c.one ? gemm_kernel<DZ, T, OF32, true, true> : gemm_kernel<DZ, T, OF32, false, true>)
+                               : h->grad_type == CO3_F32 ? (c.one ? gemm_kernel<DZ, T, OF32, true, false> : gemm_kernel<DZ, T, OF32, false, false>)
+                                                         : (c.one ? gemm_kernel<DZ, T, T, true, false> : gemm_kernel<DZ, T, T, false, false>);
         rc = gemm(h, dz, mt * ct, a, st);
         if (rc == CO3_OK && dhidden) {
             GemmArgs b = a;
@@ -1230,7 +1235,7 @@ extern "C" int co3_token_loss_create(co3_token_loss** out, const co3_token_loss_
         const size_t o_h = part(rows * h->dim * 2), o_stats = part(8 * rows * h->tiles), o_dots = part(4 * rows * h->tiles);
         const size_t o_dz = part(rows * h->piece * 2), o_low = part(h->grad_type == CO3_F32 ? rows * h->piece * 2 : 0);
         const size_t o_part = part(4 * rows * h->dim * h->max_splits);
-        const size_t o_e = part(4 * tokens * top), o_q = part(4 * tokens * top), o_k = part(4 * tokens), o_f = part(h->max_top > 1 ? tokens * h->tiles : tokens), o_m = part(tokens);
+        const size_t o_e = part(4 * tokens * top), o_q = part(4 * tokens * top), o_k = part(4 * tokens), o_f = part(tokens * h->tiles), o_m = part(tokens);
         if (cudaMalloc(&h->slab, at) != cudaSuccess) { h->slab = nullptr; rc = CO3_ENOMEM; }
         else {
             char* base = (char*)h->slab;
@@ -1274,6 +1279,7 @@ extern "C" int co3_token_loss_backward(co3_token_loss* h, const co3_array* hidde
     if (n_tokens && (!lse || !aligned_to(lse, 4) || !aligned_to(dloss, 4))) return CO3_EINVAL;
     if (!(fabsf(scale) < INFINITY)) return CO3_EINVAL;
     if (n_tokens == 0) dhidden = nullptr;
+    if (dhidden && n_tokens * h->users * ((h->dim + 255) / 256) > (int64_t)8 * 0x7FFFFFFF) return CO3_ELIMIT;      // thread blocks of a launch
     if (!dhidden && !dweight) return CO3_OK;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     Call c;

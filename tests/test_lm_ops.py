@@ -739,10 +739,11 @@ def refused(call, *errors):
 
 
 def test_refusals():
-    for make in (lambda: b.Embedding(0, 8), lambda: b.Embedding(8, 0), lambda: b.Embedding(8, 8, n_users=0), lambda: b.Embedding(8, 8, tokens=-1), lambda: b.Embedding(1 << 31, 8),
+    for make in (lambda: b.Embedding(0, 8, tokens=1), lambda: b.Embedding(8, 0, tokens=1), lambda: b.Embedding(8, 8, n_users=0, tokens=1), lambda: b.Embedding(8, 8, tokens=-1),
+                 lambda: b.Embedding(1 << 31, 8, tokens=1),
                  lambda: b.LayerNorm(0), lambda: b.LayerNorm(16385), lambda: b.LayerNorm(8, eps=-1.0), lambda: b.LayerNorm(8, eps=NAN), lambda: b.LayerNorm(8, n_users=0),
-                 lambda: b.TokenLoss(0, 8), lambda: b.TokenLoss(8, 12), lambda: b.TokenLoss(8, 8, top=129), lambda: b.TokenLoss(8, 8, top=0), lambda: b.TokenLoss(8, 8, dtype=F32),
-                 lambda: b.TokenLoss(8, 8, dtype=BF16, grad_dtype=F16), lambda: b.TokenLoss(8, 8, n_users=0)):
+                 lambda: b.TokenLoss(0, 8, tokens=1), lambda: b.TokenLoss(8, 12, tokens=1), lambda: b.TokenLoss(8, 8, tokens=1, top=129), lambda: b.TokenLoss(8, 8, tokens=1, top=0),
+                 lambda: b.TokenLoss(8, 8, tokens=1, dtype=F32), lambda: b.TokenLoss(8, 8, tokens=1, dtype=BF16, grad_dtype=F16), lambda: b.TokenLoss(8, 8, n_users=0, tokens=1)):
         refused(make, b.Co3Error)
     cuda = dict(device="cuda")
     e = b.Embedding(10, 8, n_users=2, tokens=4)
