@@ -17,7 +17,7 @@ namespace {
 
 constexpr int TILE = 256;                     // rows and columns of a pair's tile
 constexpr int KB = 64;                        // depth of a stage: 128 bytes, one swizzle span
-constexpr int STAGES = 5;
+constexpr int STAGES = 5;                     // six take as long: what the products wait for is the way from L2 to the SMs
 constexpr int HALF_BYTES = 128 * KB * 2;      // one operand's part of a thread block and stage
 constexpr int STAGE_BYTES = 2 * HALF_BYTES;
 constexpr int FIRST_EPI = 2;                  // warps: loads, products, then those for the tiles' ends
@@ -77,14 +77,16 @@ __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile
 __device__ __forceinline__ void bar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t far) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(far) : "memory");
+// Orders what this thread block does, no more: what the other side waits for is that tensor memory has been read, which the tcgen05 fences
+// order.  (With a release for the whole cluster a warp waited here for its stores to memory, 2000 cycles a tile and more.)
+__device__ __forceinline__ void bar_arrive_far(uint32_t far) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(far) : "memory");
 }
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     unsigned long long since = 0;
     for (uint32_t i = 1;; ++i) {
         uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
         if (done) return true;
         if (i % 256 == 0) {
@@ -459,10 +461,10 @@ __device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w
 
 // ---- the kernel ------------------------------------------------------------------------------------------------------------
 // Stages of depth that an accumulator takes.  The tensor cores cut a sum's last bits off at each 16 of depth (0.2 .. 0.7 units in the last
-// place of 32 bits, always towards zero), so where results have 32 bits, sums over more than 1024 are added up in registers, rounded to nearest (z
-// over 4096: 4.5e-6 of it off in one sum, 1.1e-6 in four).  Reading an accumulator out holds the products up for about 2300 cycles, against the
-// 8192 that they take over 1024, so what is rounded to 16 bits in the end is one sum.
-template <int MODE, class D> constexpr int CHUNK = MODE == STATS || (MODE != DHIDDEN && sizeof(typename D::type) == 4) ? 16 : 1 << 20;
+// place of 32 bits, always towards zero), so where results have 32 bits, sums over more than 1024 are added up in
+// registers, rounded to nearest: z over 4096 4.5e-6 of it off in one sum, 1.1e-6 in four.  Four cost 42 thousand cycles a tile, one 37, so what
+// is rounded to 16 bits in the end is one sum.
+template <int MODE, class D> constexpr int CHUNK = MODE == STATS ? 16 : MODE == DHIDDEN || sizeof(typename D::type) == 2 ? 1 << 20 : 16;
 
 // D: the type of dweight.  LOW: dz in two numbers.
 template <int MODE, class T, class D, bool ONE, bool LOW>
@@ -609,7 +611,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gem
                     }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(far_free + 8 * buffer);
+                if (lane == 0) bar_arrive_far(far_free + 8 * buffer);
                 ++turn_no;
                 k = w.k1 - k < CHUNK<MODE, D> ? w.k1 : k + CHUNK<MODE, D>;
             } while (k < w.k1);
@@ -1050,12 +1052,14 @@ int gemm(co3_token_loss* h, void (*kernel)(GemmArgs), int64_t tiles, const GemmA
     return launch_early(&h->launches, kernel, dim3((unsigned)(2 * (pairs < 1 ? 1 : pairs))), GEMM_THREADS, GEMM_SHARED, 1, st, a);
 }
 
-// How many parts the depth of dhidden is cut into: as many as let the last round of tiles fill the device best, for few rows.
-int splits_of(const co3_token_loss* h, int64_t tiles, int64_t depth) {
+// How many parts the depth of dhidden (in stages) is cut into.  For few tiles more of them fill the device, or its last round; each costs its
+// sums' way to memory and back.
+int splits_of(const co3_token_loss* h, int64_t tiles, int64_t rows, int64_t depth) {
     int best = 1;
     double least = 1e30;
-    for (int s = 1; s <= h->max_splits && depth / s >= 8; ++s) {
-        const double t = (double)((tiles * s + h->pairs - 1) / h->pairs) / s * (1.0 + 0.01 * s);
+    for (int s = 1; s <= h->max_splits && (s == 1 || depth / s >= 8); ++s) {
+        const double stage = 0.35e-6, rate = 5e12;        // 512 cycles; bytes a second
+        const double t = (double)((tiles * s + h->pairs - 1) / h->pairs) * (double)((depth + s - 1) / s) * stage + (double)s * (double)rows * (double)h->dim * 8.0 / rate;
         if (t < least) { least = t; best = s; }
     }
     return best;
@@ -1149,7 +1153,7 @@ template <class T> int backward_of(co3_token_loss* h, Call& c, const co3_array* 
         wide = !dweight->accumulate && aligned_to(dweight->data, 16) && h->dim * width % 16 == 0 && (h->users == 1 || dweight->user_stride * width % 16 == 0) &&
                make_out_map(h, &map_dw, dweight->data, dweight->type, h->vocab, h->users, h->users > 1 ? dweight->user_stride : h->dim * h->vocab);
     }
-    if (dhidden) splits = splits_of(h, mt * nt, up_to(h->piece < h->vocab ? h->piece : h->vocab, KB) / KB);
+    if (dhidden) splits = splits_of(h, mt * nt, c.rows, up_to(h->piece < h->vocab ? h->piece : h->vocab, KB) / KB);
     for (int64_t v0 = 0; v0 < h->vocab && rc == CO3_OK; v0 += h->piece) {
         GemmArgs a = c.g;
         a.out = h->map_dz_out; a.out_low = h->map_low_out;
