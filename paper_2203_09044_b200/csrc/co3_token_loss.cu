@@ -423,13 +423,17 @@ __device__ __forceinline__ void put_rows(const GemmArgs& a, typename D::type* ba
             for (int r = 0; r < rows; ++r, p += pitch)
                 if (lane < pairs) *(uint32_t*)p = word(r);
         } else {                              // a whole word is a pair's first element and the one before it, which the lane before has
+            const bool whole = lane > 0 && lane < pairs;
 #pragma unroll 8
             for (int r = 0; r < rows; ++r, p += pitch) {
                 const uint32_t mine = word(r), before = __shfl_up_sync(0xffffffffu, mine, 1);
-                if (lane >= pairs) continue;
-                if (lane) *(uint32_t*)(p - 1) = before >> 16 | mine << 16;
-                else *(uint16_t*)p = (uint16_t)mine;
-                if (lane == pairs - 1) ((uint16_t*)p)[1] = (uint16_t)(mine >> 16);
+                if (whole) *(uint32_t*)(p - 1) = before >> 16 | mine << 16;
+            }
+            if (lane < rows) {                // the first and the last element of a row, by the lane that has it
+                typename D::type* const q = base + lane * pitch;
+                const int last = pairs - 1;
+                q[0] = D::put(x[0]);
+                ((uint16_t*)q)[2 * last + 1] = (uint16_t)(box[lane * 32 + (((last >> 2) ^ (lane & 7)) << 2 | (last & 3))] >> 16);
             }
         }
     }
