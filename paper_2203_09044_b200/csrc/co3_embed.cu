@@ -295,10 +295,10 @@ struct SumArgs {
     float scale;
 };
 
-// How a warp takes a row: WIDE eight neighbouring columns a lane, 16 bytes of 16-bit numbers; PAIRS two neighbouring ones, for few rows, and
+// How a warp takes a row: WIDE eight neighbouring columns a lane, 16 bytes of 16-bit numbers; QUADS and PAIRS four and two, for few rows, and
 // for gradients that begin anywhere; SINGLES every 32nd, two of them, for rows that begin anywhere.
-enum Take { WIDE, PAIRS, SINGLES };
-template <int TAKE> constexpr int PER_LANE = TAKE == WIDE ? 8 : 2;
+enum Take { WIDE, QUADS, PAIRS, SINGLES };
+template <int TAKE> constexpr int PER_LANE = TAKE == WIDE ? 8 : TAKE == QUADS ? 4 : 2;
 template <int TAKE> constexpr int COLUMNS = 32 * PER_LANE<TAKE>;
 
 __device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {      // two sums in one instruction
@@ -307,52 +307,51 @@ __device__ __forceinline__ void add_pair(float& a, float& b, float x, float y) {
 
 template <class A, int TAKE> struct RowPart {
     typedef typename A::type type;
-    uint4 wide[TAKE == WIDE ? 8 / A::EACH : 1];
-    alignas(2 * sizeof(type)) type two[2];
+    static constexpr int N = PER_LANE<TAKE>, BYTES = N * sizeof(type);
+    alignas(BYTES < 16 ? BYTES : 16) type x[N];
     __device__ __forceinline__ void load(const type* p, int columns) {        // columns: that are left from the lane's first
-        if (TAKE == WIDE) {
-            if (columns > 0)
+        if (TAKE == SINGLES) {
+            if (columns > 0) x[0] = p[0];
+            if (columns > 32) x[1] = p[32];
+        } else if (columns > 0) {
+            if (BYTES == 4) *(uint32_t*)x = __ldcs((const uint32_t*)p);
+            else if (BYTES == 8) *(uint2*)x = __ldcs((const uint2*)p);
+            else
 #pragma unroll
-                for (int i = 0; i < 8 / A::EACH; ++i) wide[i] = __ldcs((const uint4*)p + i);
-        } else if (TAKE == PAIRS) {
-            if (columns > 0) {
-                if (sizeof(type) == 2) *(uint32_t*)two = __ldcs((const uint32_t*)p);
-                else *(uint2*)two = __ldcs((const uint2*)p);
-            }
-        } else {
-            if (columns > 0) two[0] = p[0];
-            if (columns > 32) two[1] = p[32];
+                for (int i = 0; i < BYTES / 16; ++i) ((uint4*)x)[i] = __ldcs((const uint4*)p + i);
         }
     }
     __device__ __forceinline__ void add(float* s) const {
-        if (TAKE == WIDE) {
-            float x[8];
+        float f[N];
+        if constexpr (sizeof(type) == 4) {
 #pragma unroll
-            for (int i = 0; i < 8 / A::EACH; ++i) A::unpack(wide[i], x + i * A::EACH);
+            for (int k = 0; k < N; ++k) f[k] = A::get(x[k]);
+        } else {
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) add_pair(s[k], s[k + 1], x[k], x[k + 1]);
-        } else { s[0] += A::get(two[0]); s[1] += A::get(two[1]); }
+            for (int k = 0; k < N; k += 2) A::unpack2(*(const uint32_t*)(x + k), f[k], f[k + 1]);
+        }
+#pragma unroll
+        for (int k = 0; k < N; k += 2) add_pair(s[k], s[k + 1], f[k], f[k + 1]);
     }
 };
 
-struct Sum8 { float x[8]; };
+template <int N> struct Sums { float x[N]; };
 
-// A run's sum: to the gradient, or (slot >= 0) to its part's place.  Not inlined: the loop over rows has eight of these.
+// A run's sum to its token's row, from the lane's first column on, of which `left` are left; `part`: to its part's place instead.  Not inlined:
+// the loop over rows has four of these.
 template <class B, int TAKE>
-__device__ __noinline__ void put_run(const SumArgs& a, uint32_t at, uint32_t user, uint32_t token, int slot, int column, Sum8 s) {
+__device__ __noinline__ void put_run(typename B::type* p, float* part, int left, float scale, int accumulate, Sums<PER_LANE<TAKE>> s) {
     constexpr int N = PER_LANE<TAKE>, STEP = TAKE == SINGLES ? 32 : 1;
-    if (slot >= 0) {
-        float* p = a.part + ((int64_t)at * 2 + slot) * a.dim + column;
+    if (left <= 0) return;
+    if (part) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) if (column + STEP * k < a.dim) p[STEP * k] = s.x[k];
+        for (int k = 0; k < N; ++k) if (STEP * k < left) part[STEP * k] = s.x[k];
         return;
     }
-    typename B::type* p = (typename B::type*)a.to.data + user * a.to.user_stride + (int64_t)token * a.dim + column;
 #pragma unroll
-    for (int k = 0; k < N; ++k) s.x[k] *= a.scale;
-    if (TAKE == WIDE) {                       // the gradient's rows begin at multiples of 16 bytes
-        if (column >= a.dim) return;
-        if (a.to.accumulate) {
+    for (int k = 0; k < N; ++k) s.x[k] *= scale;
+    if constexpr (TAKE == WIDE) {             // the gradient's rows begin at multiples of 16 bytes
+        if (accumulate) {
             float o[8];
             load8<B>(p, o);
 #pragma unroll
@@ -362,7 +361,7 @@ __device__ __noinline__ void put_run(const SumArgs& a, uint32_t at, uint32_t use
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (column + STEP * k < a.dim) p[STEP * k] = B::put(a.to.accumulate ? B::get(p[STEP * k]) + s.x[k] : s.x[k]);
+            if (TAKE != SINGLES || STEP * k < left) p[STEP * k] = B::put(accumulate ? B::get(p[STEP * k]) + s.x[k] : s.x[k]);
     }
 }
 
@@ -403,9 +402,10 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     const uint64_t ends = (uint64_t)__ballot_sync(0xffffffffu, key2 != after2) << 32 | __ballot_sync(0xffffffffu, key != (lane == 31 ? next : after)) | 1ull << (total - 1);
     const int column = slab * COLUMNS<TAKE> + (TAKE == SINGLES ? lane : lane * PER_LANE<TAKE>);
     const typename A::type* rows = (const typename A::type*)a.dout + user * a.gu + column;
-    Sum8 sum;
+    typename B::type* const to = (typename B::type*)a.to.data + user * a.to.user_stride + column;
+    Sums<PER_LANE<TAKE>> sum;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum.x[k] = 0.0f;
+    for (int k = 0; k < PER_LANE<TAKE>; ++k) sum.x[k] = 0.0f;
     RowPart<A, TAKE> now[AT_ONCE], coming[AT_ONCE];
     auto fetch = [&](RowPart<A, TAKE>(&x)[AT_ONCE], int e0) {
 #pragma unroll
@@ -424,9 +424,10 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
             now[e].add(sum.x);
             if (!(ends >> i & 1)) continue;
             const uint32_t mine = __shfl_sync(0xffffffffu, i < RUN ? key : key2, i & 31);
-            put_run<B, TAKE>(a, at, user, mine, i < led ? 0 : i + 1 == total ? last_slot : -1, column, sum);
+            const int slot = i < led ? 0 : i + 1 == total ? last_slot : -1;
+            put_run<B, TAKE>(to + (int64_t)mine * a.dim, slot < 0 ? nullptr : a.part + ((int64_t)at * 2 + slot) * a.dim + column, a.dim - column, a.scale, a.to.accumulate, sum);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum.x[k] = 0.0f;
+            for (int k = 0; k < PER_LANE<TAKE>; ++k) sum.x[k] = 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) now[e] = coming[e];
@@ -555,12 +556,13 @@ template <class A> int lookup_to(co3_embed* h, int type, bool vec, const LookupA
     return lookup_of<A, OF16>(h, vec, a, grid, st);
 }
 template <class A, class B> int sums_of(co3_embed* h, int take, SumArgs a, cudaStream_t st) {
-    const int columns = take == WIDE ? COLUMNS<WIDE> : COLUMNS<PAIRS>;
+    const int columns = take == WIDE ? COLUMNS<WIDE> : take == QUADS ? COLUMNS<QUADS> : COLUMNS<PAIRS>;
     a.slabs = (a.dim + columns - 1) / columns;
     a.items = (int64_t)h->users * a.chunks * a.slabs;
     if ((a.items + 7) / 8 > 0x7FFFFFFF) return CO3_ELIMIT;
     const dim3 grid((unsigned)((a.items + 7) / 8));
     int rc = take == WIDE ? launch_early(&h->launches, sum_kernel<A, B, WIDE>, grid, 256, 0, 1, st, a)
+             : take == QUADS ? launch_early(&h->launches, sum_kernel<A, B, QUADS>, grid, 256, 0, 1, st, a)
              : take == PAIRS ? launch_early(&h->launches, sum_kernel<A, B, PAIRS>, grid, 256, 0, 1, st, a)
                              : launch_early(&h->launches, sum_kernel<A, B, SINGLES>, grid, 256, 0, 1, st, a);
     if (rc != CO3_OK || a.chunks <= 2) return rc;         // a run that is added by parts lies in three chunks at least
@@ -624,15 +626,17 @@ extern "C" int co3_embed_backward(co3_embed* h, const co3_array* dout, const co3
     a.sorted = h->sorted[s.passes & 1]; a.n_valid = h->n_valid;
     a.pitch = h->pitch; a.chunks = (uint32_t)((n_tokens + RUN - 1) / RUN); a.n_long = h->n_long; a.long_runs = h->long_runs; a.part = h->part;
     a.to = *dtable; a.dim = (int)h->dim; a.scale = scale;
-    // Eight columns a lane where both begin at whole 16 bytes and the warps are more than the device has places for; else two.
+    // As many columns a lane as the arrays' beginnings allow and as leave more warps than half of what the device has places for.
     const int in = type_width(dout->type);
     auto begins = [&](int bytes) {
+        bytes = bytes < 16 ? bytes : 16;
         return aligned_to(dout->data, bytes) && (n_tokens <= 1 || dout->token_stride * in % bytes == 0) && (h->users == 1 || dout->user_stride * in % bytes == 0);
     };
+    auto warps = [&](int columns) { return (int64_t)h->users * a.chunks * ((h->dim + columns - 1) / columns) >= (int64_t)h->sms * 16; };
     int take = SINGLES;
     if (h->dim % 2 == 0 && begins(2 * in)) take = PAIRS;
-    const int64_t warps = (int64_t)h->users * a.chunks * ((h->dim + COLUMNS<WIDE> - 1) / COLUMNS<WIDE>);
-    if (h->dim % 8 == 0 && begins(16) && aligned_to(dtable->data, 16) && (h->users == 1 || dtable->user_stride * width % 16 == 0) && warps >= (int64_t)h->sms * 16) take = WIDE;
+    if (h->dim % 4 == 0 && begins(4 * in) && warps(COLUMNS<QUADS>)) take = QUADS;
+    if (h->dim % 8 == 0 && begins(16) && aligned_to(dtable->data, 16) && (h->users == 1 || dtable->user_stride * width % 16 == 0) && warps(COLUMNS<WIDE>)) take = WIDE;
     if (dout->type == CO3_F32) return sums_to<OF32>(h, take, a, st);
     if (dout->type == CO3_BF16) return sums_to<OBf16>(h, take, a, st);
     return sums_to<OF16>(h, take, a, st);
