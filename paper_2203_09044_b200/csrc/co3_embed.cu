@@ -50,6 +50,8 @@ template <class T> __device__ __forceinline__ void store8(typename T::type* p, c
     if (T::EACH == 4) ((uint4*)p)[1] = T::pack(x + 4);
 }
 
+// A warp per 1024 columns of a row, all loads on their way before the first store.  Bound by memory: 65536 rows of 4096 bf16 142 us, 7.5 TB/s,
+// some of the rows from L2; 512 rows of 768 2.2 us.
 template <class A, class B, bool VEC>
 __global__ void __launch_bounds__(256) lookup_kernel(const __grid_constant__ LookupArgs a) {
     const int lane = threadIdx.x & 31;
@@ -155,6 +157,9 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits) {
     return same;
 }
 
+// Stable sort by radix, nine bits a pass at most: a warp ranks its keys by ballots and counts them, the counts of all warps and blocks are
+// summed by digit, and each key's place is known.  Bound by the steps that wait for one another: 62 tokens 9 us, 2000 of 8 users 12,
+// 65536 36, all of it behind the zeros where there are any (524 MB: 75 us).
 __global__ void __launch_bounds__(SORT_THREADS, 2) sort_kernel(const __grid_constant__ SortArgs a) {
     extern __shared__ uint32_t hist[];        // [SORT_WARPS][bins]
     __shared__ uint32_t totals[SORT_BINS + 1], base[SORT_BINS], warp_sums[SORT_BINS / 32];
@@ -365,6 +370,8 @@ __device__ __noinline__ void put_run(typename B::type* p, float* part, int left,
     }
 }
 
+// Reads each row of dout once, 512 bytes of it at a time, and writes a token's row once.  65536 rows of 2048 bf16 to 39217: 94 us, 4.4 TB/s, issue slots 62 %
+// used at 24 warps an SM; 12500 of 768 to as many of 32 bits at an odd element: 33 us, most of it while the zeros before it still go to memory.
 template <class A, class B, int TAKE>
 __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs a) {
     constexpr int AT_ONCE = 4;                // rows whose loads are in flight while as many are added (64k tokens: 4 take 204 us, 8 in more registers 210)

@@ -470,6 +470,9 @@ __device__ __forceinline__ void end_dweight(const GemmArgs& a, const TileWork& w
 // is rounded to 16 bits in the end is one sum.
 template <int MODE, class D> constexpr int CHUNK = MODE == STATS ? 16 : MODE == DHIDDEN || sizeof(typename D::type) == 2 ? 1 << 20 : 16;
 
+// What bounds it.  4096 tokens x 16384 x 4096, each of the four products 350 us, 1.57 PFLOP/s, the tensor cores at work 85 % of the time; 8192 x 131072 x 4096
+// over seconds at the power limit (1.25 GHz): 27.3 ms for 35 TFLOP of four products, 1.29 PFLOP/s against the 1.38 of a library's plain product.  There the
+// products wait for operands on their way from L2 (64 KB a pair in 512 cycles).  At a depth of 768 a tile's end takes as long as its products.
 // D: the type of dweight.  LOW: dz in two numbers.
 template <int MODE, class T, class D, bool ONE, bool LOW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs a) {
