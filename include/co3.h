@@ -490,8 +490,8 @@ int64_t co3_adamw_launch_count(const co3_adamw* h);
  * embedding lookup, layer norm, and losses over a large vocabulary.  A batch is [n_users][n_tokens]; every user has weight gradients
  * of its own, written into that user's row of a gradient array.
  *
- * Each handle belongs to the device that was current when it was made and owns its scratch (one allocation); later calls allocate
- * nothing, only enqueue kernels and may be captured into a graph and replayed.  Calls on one handle share its scratch: they are issued on
+ * Each handle belongs to the device that was current when it was made (not during a capture) and owns its scratch (one allocation); later
+ * calls allocate nothing, only enqueue kernels and may be captured into a graph and replayed.  Calls on one handle share its scratch: they are issued on
  * one stream, or ordered by the caller, graphs that were captured from the same handle among them.  Each call needs the handle's device to
  * be current.  Outputs must not share memory with anything else of the call.  Sums have a fixed order: the same inputs in the same layout
  * give the same bits.
@@ -569,7 +569,8 @@ int64_t co3_layernorm_launch_count(const co3_layernorm* h);
  * second product.  Products are summed in 32 bits.  Exponentials below 2^-126 count as 0.  f16: dz is scaled by a power of two per user, so that none is lost below 2^-24.
  * weight: device, vocab rows, weight_stride elements apart; its address and the stride are multiples of 16 bytes, dim is a multiple of 8.
  * loss, lse, dloss: device f32 [n_users][n_tokens].  lse is what the forward call gave for the same inputs.  dhidden, dweight: NULL where
- * not wanted.  top from 1 to max_top, which is at most 128. */
+ * not wanted.  top from 1 to max_top, which is at most 128.  co3_token_loss_status also reports CO3_FLAG_TIMEOUT: a wait between warps or
+ * thread blocks was given up after four seconds (should never happen), and the call's results are not to be used. */
 typedef struct co3_token_loss co3_token_loss;
 typedef struct {
     int64_t vocab, dim, max_tokens;

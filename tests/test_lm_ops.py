@@ -515,6 +515,26 @@ def test_a_vocabulary_in_several_pieces():
                      c, dhidden[None], d[None], kind)
 
 
+@pytest.mark.parametrize("at", [0, 3])
+def test_a_weight_that_passes_32_bits(at):
+    """4.6e9 elements.  Of a weight of zeros all logits are 0: dz is 1 / vocab, less 1 at the target, and dhidden is 0."""
+    vocab, dim = 70_001, 65_536
+    t = b.TokenLoss(vocab, dim, tokens=2, dtype=BF16, grad_dtype=BF16)
+    weight = torch.zeros((vocab, dim), dtype=BF16, device="cuda")
+    hidden = torch.ones((2, dim), dtype=BF16, device="cuda")
+    k = torch.tensor([vocab - 1, -1], device="cuda")
+    loss, lse = t.loss(hidden, weight, k)
+    assert abs(loss[0].item() - math.log(vocab)) <= 1e-5 and loss[1].item() == 0
+    memory = torch.full((vocab * dim + 8,), 7.0, dtype=BF16, device="cuda")
+    d = memory[at:at + vocab * dim]
+    dhidden = t.loss_grad(hidden, weight, k, lse, dweight=d)
+    assert not dhidden.any()
+    p, d = 1.0 / vocab, d.view(vocab, dim)
+    for rows, want in ((d[:9], p), (d[65_530:65_540], p), (d[vocab - 9:vocab - 1], p), (d[vocab - 1:], p - 1.0)):
+        assert ((rows.double() - want).abs() <= abs(want) * (2 * u(BF16) + 1e-5)).all()
+    assert bool((memory[:at] == 7).all()) and bool((memory[at + vocab * dim:] == 7).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_logits_far_apart(dtype):
     """Logits of hundreds: exponentials of differences only, losses of 0 and of hundreds."""
