@@ -342,10 +342,10 @@ template <class A, int TAKE> struct RowPart {
 
 template <int N> struct Sums { float x[N]; };
 
-// A run's sum to its token's row, from the lane's first column on, of which `left` are left; `part`: to its part's place instead.  Not inlined:
-// the loop over rows has four of these.
+// A run's sum to its token's row, from the lane's first column on, of which `left` are left; `part`: to its part's place instead.  (As a call, with
+// its arguments moved to where calls have them, 65536 rows took 192 us with sort and zeros instead of 182.)
 template <class B, int TAKE>
-__device__ __noinline__ void put_run(typename B::type* p, float* part, int left, float scale, int accumulate, Sums<PER_LANE<TAKE>> s) {
+__device__ __forceinline__ void put_run(typename B::type* p, float* part, int left, float scale, int accumulate, Sums<PER_LANE<TAKE>> s) {
     constexpr int N = PER_LANE<TAKE>, STEP = TAKE == SINGLES ? 32 : 1;
     if (left <= 0) return;
     if (part) {
@@ -370,11 +370,13 @@ __device__ __noinline__ void put_run(typename B::type* p, float* part, int left,
     }
 }
 
-// Reads each row of dout once, 512 bytes of it at a time, and writes a token's row once.  65536 rows of 2048 bf16 to 39217: 94 us, 4.4 TB/s, issue slots 62 %
-// used at 24 warps an SM; 12500 of 768 to as many of 32 bits at an odd element: 33 us, most of it while the zeros before it still go to memory.
+// Reads each row of dout once, 512 bytes of it at a time, and writes a token's row once.  65536 rows of 2048 bf16 to 39217: 82 us, 5.2 TB/s; 12500
+// of 768 to as many of 32 bits at an odd element: 22 us, while the zeros before it still go to memory.
 template <class A, class B, int TAKE>
 __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs a) {
-    constexpr int AT_ONCE = 4;                // rows whose loads are in flight while as many are added (64k tokens: 4 take 204 us, 8 in more registers 210)
+    // Rows whose loads are in flight while as many are added: with 16 bytes a lane four (65536 rows of 2048 bf16 182 us with sort and zeros, eight 196), with less
+    // eight (8 users' 2000 of 768 133, four 136).
+    constexpr int AT_ONCE = RowPart<A, TAKE>::BYTES >= 16 ? 4 : 8;
     constexpr uint32_t NONE = 0xFFFFFFFFu;
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
