@@ -480,6 +480,32 @@ def test_distillation(shape, top, tau, dtype, teacher):
     assert untouched() and t.status() == (0, 0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("users,tokens", [(1, 8192), (1, 8193), (32, 256), (33, 249), (256, 32), (256, 1), (257, 3), (300, 40), (2100, 5)])
+def test_losses_of_many_tokens_and_users(users, tokens, dtype):
+    """Both sides of the limits of 8192 tokens and 256 users, above which the tokens with a target are packed in another way; beyond 1024 users that one keeps its counts elsewhere."""
+    g = gen(users + tokens)
+    vocab, dim = 24, 8
+    t = b.TokenLoss(vocab, dim, n_users=users, tokens=tokens, dtype=dtype, grad_dtype=F32, top=3)
+    hidden, weight = normal(g, users, tokens, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype)
+    k = some_targets(g, users, tokens, vocab)
+    there = k >= 0
+    loss, lse = t.loss(hidden, weight, k)
+    c = torch.rand((users, tokens), generator=g, device="cuda")
+    d = torch.empty((users, vocab, dim), device="cuda")
+    dhidden = t.loss_grad(hidden, weight, k, lse, c, dweight=d)
+    check_losses(t, hidden, weight, there, k.clamp(min=0)[..., None], torch.ones((users, tokens, 1), dtype=torch.float64, device="cuda"), 1.0, loss, lse, c, dhidden, d)
+    # no token's loss depends on the others, nor on the user it is of
+    alone = b.TokenLoss(vocab, dim, tokens=tokens, dtype=dtype, top=3)
+    index = torch.stack([k, torch.randint(-2, vocab, k.shape, generator=g, device="cuda"), (k + 1).clamp(min=-1, max=vocab - 1)], -1)
+    logits = normal(g, users, tokens, 3)
+    soft = t.distill(hidden, weight, index, logits, 2.0)
+    for i in {0, users // 2, users - 1}:
+        assert all(torch.equal(x[i], y) for x, y in zip((loss, lse), alone.loss(hidden[i], weight, k[i])))
+        assert all(torch.equal(x[i], y) for x, y in zip(soft, alone.distill(hidden[i], weight, index[i], logits[i], 2.0)))
+    assert t.status() == (0, 0) and alone.status() == (0, 0)
+
+
 def test_the_gradient_formula_of_distillation_against_differences():
     g = gen(2)
     n, vocab, dim, tau = 3, 7, 8, 1.7

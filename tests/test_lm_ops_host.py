@@ -208,14 +208,16 @@ def test_loss_launches_and_scratch(fake, users, n, vocab, dim, top, type_, grad_
     with Made(fake, "token_loss", C.byref(config(vocab, dim, n, users, type_, grad_type, top))) as h:
         base, size = fake.fake_allocated(), fake.fake_allocated_bytes()
         x, t = array(type_, n * dim, dim), tokens(n)
-        assert len(h("forward", x, A, dim, t, None, 1.0, n, A, A, None)) == 4
+        first = 1 if users * n <= 8192 and users <= 256 else 2                  # launches that pack the tokens with a target
+        assert len(h("forward", x, A, dim, t, None, 1.0, n, A, A, None)) == 2 + first
         for stride in (vocab * dim, vocab * dim + 1):
             seen = h("backward", x, A, dim, t, None, 1.0, n, A, A, 1.0, x, grad(grad_type, stride), None)
-            assert (len(seen) - 3) % 3 == 0 and len(seen) >= 6
-            assert len(h("backward", x, A, dim, t, None, 1.0, n, A, None, 1.0, x, None, None)) == 3 + 2 * (len(seen) - 3) // 3
+            other = 1 + first
+            assert (len(seen) - other) % 3 == 0 and len(seen) >= other + 3
+            assert len(h("backward", x, A, dim, t, None, 1.0, n, A, None, 1.0, x, None, None)) == other + 2 * (len(seen) - other) // 3
         kt, lg = tokens(n, top), array(b.F32, n * top, top)
         seen = h("forward", x, A, dim, kt, lg, 2.0, n, A, A, None)
-        assert len(seen) == 5
+        assert len(seen) == 3 + first
         e = Entry.from_buffer_copy(bytes(seen[0].arg))
         assert e.n_all == users * n and e.tiles == (vocab + 255) // 256 and e.top == top
         # each array ends before the next begins, and the last with the allocation
