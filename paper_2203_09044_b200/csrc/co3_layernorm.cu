@@ -473,7 +473,7 @@ extern "C" int co3_layernorm_create(co3_layernorm** out, int64_t dim, int32_t n_
 
 extern "C" int co3_layernorm_forward(co3_layernorm* h, const co3_array* x, const void* weight, const void* bias, int32_t weight_type, int64_t n_tokens,
                                      const co3_array* y, float* mean, float* rstd, void* cuda_stream) {
-    if (!h || n_tokens < 0 || n_tokens * h->users > OPS_MAX_ROWS) return CO3_EINVAL;
+    if (!h || n_tokens < 0 || n_tokens > OPS_MAX_ROWS / h->users) return CO3_EINVAL;
     if (!array_fine(x, h->users, n_tokens, h->dim, false) || !array_fine(y, h->users, n_tokens, h->dim, true) || x->type != y->type) return CO3_EINVAL;
     if ((weight || bias) && (!type_known(weight_type) || !aligned_to(weight, type_width(weight_type)) || !aligned_to(bias, type_width(weight_type)))) return CO3_EINVAL;
     if (!device_is(h->device)) return CO3_EINVAL;
@@ -492,7 +492,7 @@ extern "C" int co3_layernorm_forward(co3_layernorm* h, const co3_array* x, const
 extern "C" int co3_layernorm_backward(co3_layernorm* h, const co3_array* dy, const co3_array* x, const void* weight, int32_t weight_type, const float* mean,
                                       const float* rstd, int64_t n_tokens, const co3_array* dx, const co3_param_grad* dweight,
                                       const co3_param_grad* dbias, void* cuda_stream) {
-    if (!h || n_tokens < 0 || n_tokens * h->users > OPS_MAX_ROWS) return CO3_EINVAL;
+    if (!h || n_tokens < 0 || n_tokens > OPS_MAX_ROWS / h->users) return CO3_EINVAL;
     if (!array_fine(x, h->users, n_tokens, h->dim, false) || !array_fine(dy, h->users, n_tokens, h->dim, false) || x->type != dy->type) return CO3_EINVAL;
     if (dx && (!array_fine(dx, h->users, n_tokens, h->dim, true) || dx->type != x->type)) return CO3_EINVAL;
     if (weight && (!type_known(weight_type) || !aligned_to(weight, type_width(weight_type)))) return CO3_EINVAL;

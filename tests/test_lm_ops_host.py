@@ -184,6 +184,15 @@ def test_layer_norm_calls_that_are_refused(fake):
     Made(fake, "layernorm", 16, 2, 1e-5, expect=b.ENOMEM)
 
 
+def test_layer_norm_of_more_rows_than_a_product_of_64_bits_holds(fake):
+    """n_tokens times 4 users is 4, or 0, in 64 bits."""
+    x = array(b.F32, 16, 16)
+    with Made(fake, "layernorm", 16, 4, 1e-5) as h:
+        for n in ((1 << 62) + 1, 1 << 62):
+            h("backward", x, x, A, b.F32, A, A, n, x, grad(b.F32, 16), None, None, expect=b.EINVAL)
+            h("forward", x, A, A, b.F32, n, x, A, A, None, expect=b.EINVAL)
+
+
 # ---- losses -------------------------------------------------------------------------------------------------------------------
 def config(vocab=1000, dim=64, n=100, users=2, type_=b.BF16, grad_type=b.F32, top=1):
     return b.TokenLossConfig(vocab, dim, n, users, type_, grad_type, top)
