@@ -550,8 +550,7 @@ namespace {
 bool embed_tokens_fine(const co3_embed* h, const co3_tokens* k, int64_t n) {
     if (!k || (k->type != CO3_I32 && k->type != CO3_I64) || k->top != 1) return false;
     if (n == 0) return true;
-    const int64_t most = (int64_t)1 << 46;
-    return k->data && aligned_to(k->data, k->type == CO3_I32 ? 4 : 8) && k->user_stride >= 0 && k->token_stride >= 0 && k->user_stride <= most && k->token_stride <= most;
+    return k->data && aligned_to(k->data, k->type == CO3_I32 ? 4 : 8) && stride_fine(h->users, k->user_stride) && stride_fine(n, k->token_stride);
 }
 Tokens tokens_of(const co3_tokens* k) { return Tokens{k->data, k->user_stride, k->token_stride, k->type == CO3_I64}; }
 

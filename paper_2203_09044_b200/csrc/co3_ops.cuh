@@ -107,13 +107,17 @@ inline int type_width(int type) { return type == CO3_F32 ? 4 : 2; }
 inline bool type_known(int type) { return type == CO3_F32 || type == CO3_BF16 || type == CO3_F16; }
 inline bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
+// Whether `count` things `stride` elements apart lie within reach: no sum of such distances passes 64 bits, in bytes neither.
+inline bool stride_fine(int64_t count, int64_t stride) {
+    const int64_t most = (int64_t)1 << 46;
+    return stride >= 0 && stride <= (count > 2 ? most / (count - 1) : most);
+}
 // Whether an array [users][tokens][dim] that a call is given can be addressed, and, if `out`, whether no two of its elements share a place.
 inline bool array_fine(const co3_array* a, int64_t users, int64_t tokens, int64_t dim, bool out) {
     if (!a || !type_known(a->type)) return false;
-    if (users * tokens * dim == 0) return true;
+    if (users == 0 || tokens == 0 || dim == 0) return true;
     if (!a->data || !aligned_to(a->data, type_width(a->type))) return false;
-    const int64_t most = (int64_t)1 << 46;
-    if (a->user_stride < 0 || a->token_stride < 0 || a->user_stride > most || a->token_stride > most) return false;
+    if (!stride_fine(users, a->user_stride) || !stride_fine(tokens, a->token_stride)) return false;
     if (out && tokens > 1 && a->token_stride < dim) return false;
     if (out && users > 1 && a->user_stride < (tokens - 1) * a->token_stride + dim &&
         !(tokens > 1 && a->user_stride >= dim && a->token_stride >= (users - 1) * a->user_stride + dim)) return false;      // or tokens outermost
@@ -122,8 +126,8 @@ inline bool array_fine(const co3_array* a, int64_t users, int64_t tokens, int64_
 // ... and of a gradient of a weight: [users][n], each user's part in one piece.
 inline bool grad_fine(const co3_param_grad* g, int64_t users, int64_t n) {
     if (!g || !type_known(g->type)) return false;
-    if (users * n == 0) return true;
-    return g->data && aligned_to(g->data, type_width(g->type)) && (users == 1 || (g->user_stride >= n && g->user_stride <= (int64_t)1 << 46));
+    if (users == 0 || n == 0) return true;
+    return g->data && aligned_to(g->data, type_width(g->type)) && (users == 1 || (g->user_stride >= n && stride_fine(users, g->user_stride)));
 }
 // Whether every row of the array begins on a multiple of 16 bytes.
 inline bool rows_aligned(const co3_array* a, int64_t users, int64_t tokens) {

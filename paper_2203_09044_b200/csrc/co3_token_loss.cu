@@ -1224,9 +1224,8 @@ bool call_fine(const co3_token_loss* h, const co3_array* hidden, const void* wei
     if (!weight || !aligned_to(weight, 16) || weight_stride < h->dim || weight_stride % 8 || weight_stride > (int64_t)1 << 38) return false;
     if (!targets || (targets->type != CO3_I32 && targets->type != CO3_I64) || targets->top < 1) return false;
     if (teacher ? targets->top > h->max_top || !array_fine(teacher, h->users, n_tokens, targets->top, false) : targets->top != 1) return false;
-    const int64_t most = (int64_t)1 << 46;
     if (n_tokens && (!targets->data || !aligned_to(targets->data, targets->type == CO3_I32 ? 4 : 8))) return false;
-    if (targets->user_stride < 0 || targets->token_stride < 0 || targets->user_stride > most || targets->token_stride > most) return false;
+    if (!stride_fine(h->users, targets->user_stride) || !stride_fine(n_tokens, targets->token_stride)) return false;
     // its reciprocal, and that times log2(e), are normal numbers
     return temperature >= 1e-30f && temperature <= 1e30f && (teacher || temperature == 1.0f);
 }

@@ -193,6 +193,40 @@ def test_layer_norm_of_more_rows_than_a_product_of_64_bits_holds(fake):
             h("forward", x, A, A, b.F32, n, x, A, A, None, expect=b.EINVAL)
 
 
+@pytest.mark.parametrize("what", ["x", "y", "dy", "dx", "dweight", "hidden", "targets", "teacher", "dhidden"])
+def test_strides_whose_last_element_has_no_address(fake, what):
+    """Strides of up to 2^46 elements were taken whatever their number: 2^18 of 2^45 wrap to a negative number of 64 bits, under which an array
+    whose users all lie in one place looked like one whose users lie apart."""
+    n, far = (1 << 18) + 1, 1 << 45
+    with Made(fake, "layernorm", 16, 2, 1e-5) as h:
+        x, wide = array(b.F32, 16 * n, 16), array(b.F32, 0, far)
+        pick = lambda name, good=x: wide if name == what else good                                             # noqa: E731
+        refused = b.EINVAL if what in ("x", "y", "dy", "dx") else b.OK
+        if what in ("x", "y") or refused == b.OK:
+            h("forward", pick("x"), A, A, b.F32, n, pick("y"), A, A, None, expect=refused)
+        if what != "y":
+            h("backward", pick("dy"), pick("x"), A, b.F32, A, A, n, pick("dx"), None, None, None, expect=refused)
+    with Made(fake, "layernorm", 16, 65535, 1e-5) as h:
+        x, far = array(b.F32, 16, 16), (1 << 46) // 65534 + 1
+        h("backward", x, x, A, b.F32, A, A, 1, x, grad(b.F32, far if what == "dweight" else 16), None, None, expect=b.EINVAL if what == "dweight" else b.OK)
+    with Made(fake, "token_loss", C.byref(config(n=3, users=2, top=2))) as h:
+        far = (1 << 45) + 8
+        x, t, lg = array(b.BF16, 3 * 64, 64), tokens(3, 2), array(b.F32, 6, 2)
+        bad = {"hidden": array(b.BF16, 64, far), "targets": b.Tokens(A, b.I64, 2, 2, far), "teacher": array(b.F32, 2, far), "dhidden": array(b.BF16, 64, far)}
+        args = {"hidden": x, "targets": t, "teacher": lg, "dhidden": x} | ({what: bad[what]} if what in bad else {})
+        refused = b.EINVAL if what in bad else b.OK
+        h("backward", args["hidden"], A, 64, args["targets"], args["teacher"], 2.0, 3, A, A, 1.0, args["dhidden"], grad(b.F32, 64000), None, expect=refused)
+    with Made(fake, "embed", 100, 16, 2, 3) as e:
+        x, t = array(b.F32, 48, 16), b.Tokens(A, b.I64, 1, 1, far) if what == "targets" else tokens(3)
+        e("forward", t, 3, A, b.F32, 1.0, x, None, expect=b.EINVAL if what == "targets" else b.OK)
+        e("backward", x, t, 3, 1.0, grad(b.F32, 1600), None, expect=b.EINVAL if what == "targets" else b.OK)
+
+
+def test_a_gradient_of_2_to_64_elements(fake):
+    with Made(fake, "token_loss", C.byref(config(vocab=1 << 30, dim=1 << 20, n=0, users=1 << 14))) as h:
+        h("backward", array(b.BF16, data=None), A, 1 << 20, tokens(0, data=None), None, 1.0, 0, None, None, 1.0, None, grad(b.F32, data=None), None, expect=b.EINVAL)
+
+
 # ---- losses -------------------------------------------------------------------------------------------------------------------
 def config(vocab=1000, dim=64, n=100, users=2, type_=b.BF16, grad_type=b.F32, top=1):
     return b.TokenLossConfig(vocab, dim, n, users, type_, grad_type, top)
