@@ -569,8 +569,9 @@ int64_t co3_layernorm_launch_count(const co3_layernorm* h);
  * second product.  Products are summed in 32 bits.  Exponentials below 2^-126 count as 0.  f16: dz is scaled by a power of two per user, so that none is lost below 2^-24.
  * weight: device, vocab rows, weight_stride elements apart; its address and the stride are multiples of 16 bytes, dim is a multiple of 8.
  * loss, lse, dloss: device f32 [n_users][n_tokens].  lse is what the forward call gave for the same inputs.  dhidden, dweight: NULL where
- * not wanted.  top from 1 to max_top, which is at most 128.  co3_token_loss_status also reports CO3_FLAG_TIMEOUT: a wait between warps or
- * thread blocks was given up after four seconds (should never happen), and the call's results are not to be used. */
+ * not wanted.  top from 1 to max_top, which is at most 128.  tau from 1e-30 to 1e30 (1 for cross entropy), scale / tau finite.
+ * co3_token_loss_status also reports CO3_FLAG_TIMEOUT: a wait between warps or thread blocks was given up after four seconds (should never
+ * happen), and the call's results are not to be used. */
 typedef struct co3_token_loss co3_token_loss;
 typedef struct {
     int64_t vocab, dim, max_tokens;

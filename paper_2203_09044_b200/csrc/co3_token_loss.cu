@@ -1380,7 +1380,7 @@ extern "C" int co3_token_loss_backward(co3_token_loss* h, const co3_array* hidde
     if (dhidden && (!array_fine(dhidden, h->users, n_tokens, h->dim, true) || dhidden->type != h->type)) return CO3_EINVAL;
     if (dweight && (!grad_fine(dweight, h->users, h->vocab * h->dim) || dweight->type != h->grad_type)) return CO3_EINVAL;
     if (n_tokens && (!lse || !aligned_to(lse, 4) || !aligned_to(dloss, 4))) return CO3_EINVAL;
-    if (!(fabsf(scale) < INFINITY)) return CO3_EINVAL;
+    if (!(fabsf(scale / temperature) < INFINITY)) return CO3_EINVAL;
     if (n_tokens == 0) dhidden = nullptr;
     if (dhidden && n_tokens * h->users * ((h->dim + 255) / 256) > (int64_t)8 * 0x7FFFFFFF) return CO3_ELIMIT;      // thread blocks of a launch
     if (!dhidden && !dweight) return CO3_OK;

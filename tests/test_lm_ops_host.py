@@ -298,6 +298,15 @@ def test_loss_calls_that_are_refused(fake):
     Made(fake, "token_loss", C.byref(config()), expect=b.ENOMEM)
 
 
+def test_a_scale_that_the_temperature_makes_infinite(fake):
+    """c / tau of every token would be infinite or not a number, although scale and temperature are numbers that are taken."""
+    with Made(fake, "token_loss", C.byref(config(top=3))) as h:
+        x, g = array(b.BF16, 6400, 64), grad(b.F32, 64000)
+        back = lambda tau, scale, rc: h("backward", x, A, 64, tokens(100, 3), array(b.F32, 300, 3), tau, 100, A, A, scale, x, g, None, expect=rc)     # noqa: E731
+        for tau, scale, rc in ((1e-30, 1e9, b.EINVAL), (0.5, -3e38, b.EINVAL), (1e-30, 1e8, b.OK), (0.5, 1e38, b.OK), (1e30, -3e38, b.OK), (2.0, 0.0, b.OK)):
+            back(tau, scale, rc)
+
+
 def test_null_handles(fake):
     x, t, g = array(), tokens(1), grad()
     assert fake.co3_embed_forward(None, t, 1, A, 0, 1.0, x, None) == b.EINVAL and fake.co3_embed_backward(None, x, t, 1, 1.0, g, None) == b.EINVAL
