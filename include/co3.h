@@ -561,7 +561,7 @@ int64_t co3_layernorm_launch_count(const co3_layernorm* h);
  *                  q = softmax(teacher / tau) over the entries,   lse = log sum_v exp(z_v / tau),   loss = sum_k q_k (log q_k - z_k / tau + lse)
  *                  An entry below zero is left out; one that stands twice counts twice.
  * A token without a target (or with no entry whose teacher logit is above -infinity) has loss 0, lse 0 and no gradient, whatever its
- * hidden state holds.
+ * hidden state holds.  Neither has a token whose dloss is 0 any gradient.
  *   backward: c = dloss[u][t] scale (dloss NULL: scale over the number of the user's tokens that have a target, the gradient of their mean)
  *   dz_v = c / tau (exp(z_v / tau - lse) - q_v);   dhidden = dz weight;   dweight[u] = sum over the user's tokens of dz_v hidden
  * hidden, weight and dhidden have the handle's type (bf16 or f16: what the tensor cores take).  dz is rounded to that type before the two

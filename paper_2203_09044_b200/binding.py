@@ -1194,8 +1194,8 @@ class TokenLoss(_Operator):
     def loss_grad(self, hidden, weight, targets, lse, dloss=None, scale=1.0, dhidden=None, dweight=None, accumulate=False, want_dhidden=True,
                   stream=None):
         """dhidden (None if not wanted); the users' gradients of the weight go into dweight where given ([users, vocab * dim], see
-        Embedding.backward).  lse: what loss() gave.  dloss: gradient of each token's loss; None: of the mean over each user's tokens
-        that have a target."""
+        Embedding.backward).  lse: what loss() gave.  dloss: gradient of each token's loss, 0 where none is wanted, whatever the token
+        holds; None: of the mean over each user's tokens that have a target."""
         return self._backward(hidden, weight, targets, None, 1.0, lse, dloss, scale, dhidden, dweight, accumulate, want_dhidden, stream)
 
     def distill(self, hidden, weight, index, logits, temperature=1.0, loss=None, lse=None, stream=None):

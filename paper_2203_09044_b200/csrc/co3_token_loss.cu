@@ -7,8 +7,8 @@
 //   DZ      z again, for a piece of the vocabulary -> dz, in 16 bits (and its remainder in 16 more, for 32-bit gradients of the weight)
 //   DHIDDEN dz W    over the piece        -> 32-bit sums
 //   DWEIGHT dz^T H  over a user's tokens  -> the user's gradient
-// Before them the tokens that have a target are packed side by side, users at multiples of 64 rows with zero rows between, so that
-// tokens that are none cost nothing and no other user's rows reach a sum.
+// Before them the tokens that have a target (and, for a gradient, a dloss other than 0) are packed side by side, users at multiples of 64 rows
+// with zero rows between, so that the others cost nothing and no other user's rows reach a sum.
 #include <cuda.h>
 
 #include "co3_ops.cuh"
@@ -334,7 +334,7 @@ __device__ __forceinline__ void end_dz(const GemmArgs& a, const TileWork& w, int
     }
     subtract_entries<0>(x, first, e);
     subtract_entries<32>(x, first, e);
-    if (c == 0.0f)                            // rows between users, and tokens without weight: 0 whatever the logits are
+    if (c == 0.0f)                            // rows between users, and factors of 0: 0 whatever the logits are
 #pragma unroll
         for (int k = 0; k < SPAN; ++k) x[k] = 0.0f;
     if (first + SPAN > a.vocab)
@@ -755,11 +755,15 @@ struct PackArgs {
     Packed p;
     OpsStatus* status;
 };
+// Whether the token counts: it has a target, and a gradient is wanted of it.  (A dz of 0 alone would not do: what is not a number in its hidden
+// state would reach its user's weight gradient.)
 __device__ __forceinline__ bool has_target(const PackArgs& a, uint32_t user, uint32_t t, bool count) {
-    if (a.mass) return a.mass[(int64_t)user * a.tokens + t] != 0;
+    const int64_t n = (int64_t)user * a.tokens + t;
+    const bool wanted = !a.dloss || a.dloss[n] != 0.0f;
+    if (a.mass) return wanted && a.mass[n] != 0;
     const int64_t v = index_at(a.k, user * a.k.user_stride + t * a.k.token_stride);
     if (count && v >= a.vocab) { atomicAdd(&a.status->bad_tokens, 1ull); atomicOr(&a.status->flags, CO3_FLAG_TOKEN); }
-    return v >= 0 && v < a.vocab;
+    return wanted && v >= 0 && v < a.vocab;
 }
 // f16: the power of two that brings the user's largest factor to 2^13 .. 2^14: dz is at most that.
 __device__ __forceinline__ float scale_of(const PackArgs& a, float most, int count) {

@@ -623,6 +623,31 @@ def test_not_a_number_where_it_counts():
     assert d[0].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype,kind", [(BF16, F32), (BF16, BF16), (F16, F32)])
+@pytest.mark.parametrize("users,tokens", [(2, 90), (257, 5)])         # both ways of packing
+def test_tokens_whose_gradient_is_not_wanted(users, tokens, dtype, kind):
+    """A token with dloss 0 has no gradient, whatever it holds: the same bits as if it had no target."""
+    g = gen(users)
+    vocab, dim, top = 300, 72, 3
+    t = b.TokenLoss(vocab, dim, n_users=users, tokens=tokens, dtype=dtype, grad_dtype=kind, top=top)
+    hidden, weight = normal(g, users, tokens, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype) * 0.2
+    k = torch.randint(0, vocab, (users, tokens), generator=g, device="cuda")
+    out = torch.rand((users, tokens), generator=g, device="cuda") < 0.3
+    out[1], out[0, 0] = True, True                        # a user of whose tokens none counts
+    hidden = torch.where(out[..., None], torch.tensor([NAN, math.inf], dtype=dtype, device="cuda")[k % 2][..., None], hidden)
+    c = torch.where(out, torch.tensor([0.0, -0.0], device="cuda")[k % 2], 0.1 + torch.rand((users, tokens), generator=g, device="cuda"))
+    index, logits = torch.stack([k, (k + 1) % vocab, (k + 7) % vocab], -1), normal(g, users, tokens, top)
+    d, e = torch.empty((users, vocab * dim), dtype=kind, device="cuda"), torch.empty((users, vocab * dim), dtype=kind, device="cuda")
+    _, lse = t.loss(hidden, weight, k)
+    got, want = t.loss_grad(hidden, weight, k, lse, c, dweight=d), t.loss_grad(hidden, weight, k.masked_fill(out, -1), lse, c, dweight=e)
+    assert torch.equal(got, want) and not got[out].any() and torch.equal(d, e) and d.isfinite().all() and not d[1].any() and d[0].any()
+    _, lse = t.distill(hidden, weight, index, logits, 2.0)
+    got = t.distill_grad(hidden, weight, index, logits, lse, c, 2.0, dweight=d)
+    want = t.distill_grad(hidden, weight, index.masked_fill(out[..., None], -1), logits, lse, c, 2.0, dweight=e)
+    assert torch.equal(got, want) and not got[out].any() and torch.equal(d, e) and d.isfinite().all() and not d[1].any() and d[0].any()
+    assert t.status() == (0, 0)
+
+
 def test_losses_of_no_tokens():
     t = b.TokenLoss(40, 64, n_users=2, tokens=5, grad_dtype=F32)
     weight, none = torch.ones((40, 64), dtype=BF16, device="cuda"), torch.empty((2, 0, 64), dtype=BF16, device="cuda")
