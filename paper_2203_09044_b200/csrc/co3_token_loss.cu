@@ -686,7 +686,7 @@ __global__ void __launch_bounds__(256) entry_kernel(const __grid_constant__ Entr
             const int64_t v = index_at(a.k, user * a.k.user_stride + t * a.k.token_stride + j);
             if (v >= a.vocab) { atomicAdd(&a.status->bad_tokens, 1ull); atomicOr(&a.status->flags, CO3_FLAG_TOKEN); }
             else if (v >= 0) {
-                z[i] = load_as_f32(a.k.teacher, a.k.teacher_type, user * a.k.teacher_user + t * a.k.teacher_token + j) * a.inv_t;
+                z[i] = load_as_f32(a.k.teacher, a.k.teacher_type, user * a.k.teacher_user + t * a.k.teacher_token + j);
                 if (z[i] != -INFINITY) index[i] = (int32_t)v;        // one without mass is none
             }
             sh_index[warp][j] = index[i];
@@ -697,8 +697,9 @@ __global__ void __launch_bounds__(256) entry_kernel(const __grid_constant__ Entr
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     float e[4], sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        e[i] = index[i] != 0x7FFFFFFF ? expf(z[i] - most) : 0.0f;
+    for (int i = 0; i < 4; ++i) {             // over the temperature only what is left of the largest: a logit itself may pass 32 bits there
+        z[i] = (z[i] - most) * a.inv_t;
+        e[i] = index[i] != 0x7FFFFFFF ? expf(z[i]) : 0.0f;
         sum += e[i];
     }
     sum = warp_sum_f32(sum);
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(256) entry_kernel(const __grid_constant__ Entr
             rank += x < index[i] || (x == index[i] && o < j);
         }
         const float q = here ? e[i] / sum : 0.0f;
-        if (here && q != 0.0f) about = fmaf(q, z[i] - most - log_sum, about);
+        if (here && q != 0.0f) about = fmaf(q, z[i] - log_sum, about);
         a.entry[n * top + rank] = index[i];
         a.q[n * top + rank] = q;
         sh_sorted[warp][rank] = index[i];

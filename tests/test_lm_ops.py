@@ -506,6 +506,27 @@ def test_losses_of_many_tokens_and_users(users, tokens, dtype):
     assert t.status() == (0, 0) and alone.status() == (0, 0)
 
 
+@pytest.mark.parametrize("teacher", [F32, BF16, F16])
+@pytest.mark.parametrize("tau", [0.25, 1.0])
+def test_teacher_logits_at_their_type_s_ends(teacher, tau):
+    """Masked with the type's lowest value, or as large as it goes: over the temperature they pass 32 bits, their differences from the largest tell the shares."""
+    low, high, inf = torch.finfo(teacher).min, torch.finfo(teacher).max, math.inf
+    logits = torch.tensor([[low, low, low], [high, high, 0.0], [low, 1.0, 0.0], [high, low, high], [low, low, -inf], [-inf, low, 0.0], [-inf, -inf, -inf], [-inf, low, -inf]],
+                          dtype=teacher, device="cuda")[None]
+    g = gen(7)
+    vocab, dim, n = 40, 64, logits.shape[1]
+    t = b.TokenLoss(vocab, dim, tokens=n, dtype=BF16, top=3)
+    hidden, weight = normal(g, 1, n, dim, dtype=BF16), normal(g, vocab, dim, dtype=BF16) * 0.25
+    index = torch.tensor([[5, 0, 39]], device="cuda").expand(1, n, 3).contiguous()
+    q = shares(logits, index, tau)
+    there = q.sum(-1) > 0
+    assert there.tolist() == [[True] * 6 + [False, True]]
+    loss, lse = t.distill(hidden, weight, index, logits, tau)
+    c, d = torch.ones((1, n), device="cuda"), torch.empty((1, vocab, dim), device="cuda")
+    dhidden = t.distill_grad(hidden, weight, index, logits, lse, c, tau, dweight=d[0])
+    check_losses(t, hidden, weight, there, index, q, tau, loss, lse, c, dhidden, d)
+
+
 def test_the_gradient_formula_of_distillation_against_differences():
     g = gen(2)
     n, vocab, dim, tau = 3, 7, 8, 1.7
