@@ -404,6 +404,24 @@ __device__ __forceinline__ void put_rows(const GemmArgs& a, typename D::type* ba
 #pragma unroll 8
                 for (int r = 0; r < rows; ++r, p += pitch) *p = __uint_as_float(word(r));
         }
+    } else if (a.dw.accumulate) {             // added in 32 bits, rounded once: two elements a lane, two rows at a time (as quick as with sums of 16 bits)
+        const int half = lane >> 4, pair = lane & 15;
+#pragma unroll
+        for (int c = 0; c < SPAN; c += 32) {
+            if (c >= columns) break;
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) out.put(k, OF32::pack(x + c + 4 * k));
+            __syncwarp();
+            if (c + 2 * pair >= columns) continue;        // columns are even
+            typename D::type* p = base + half * pitch + c + 2 * pair;
+#pragma unroll 8
+            for (int r = half; r < rows; r += 2, p += 2 * pitch) {
+                const float2 f = *(const float2*)(box + r * 32 + (((pair >> 1) ^ (r & 7)) << 2 | (pair & 1) << 1));
+                p[0] = D::put(D::get(p[0]) + f.x);
+                p[1] = D::put(D::get(p[1]) + f.y);
+            }
+        }
     } else {
         __syncwarp();
 #pragma unroll
@@ -411,14 +429,7 @@ __device__ __forceinline__ void put_rows(const GemmArgs& a, typename D::type* ba
         __syncwarp();
         const int pairs = columns < SPAN ? columns / 2 : SPAN / 2;            // columns are even
         typename D::type* p = base + 2 * lane;
-        if (a.dw.accumulate) {                // two roundings: of this call's sum, and of what it makes with the one before
-#pragma unroll 4
-            for (int r = 0; r < rows; ++r, p += pitch) {
-                float f, g;
-                D::unpack2(word(r), f, g);
-                if (lane < pairs) { p[0] = D::put(D::get(p[0]) + f); p[1] = D::put(D::get(p[1]) + g); }
-            }
-        } else if (((uintptr_t)base & 2) == 0) {          // rows have an even number of elements: all begin at 4 bytes, or none does
+        if (((uintptr_t)base & 2) == 0) {     // rows have an even number of elements: all begin at 4 bytes, or none does
 #pragma unroll 8
             for (int r = 0; r < rows; ++r, p += pitch)
                 if (lane < pairs) *(uint32_t*)p = word(r);

@@ -612,6 +612,26 @@ def test_small_and_large_gradients_in_half_precision(size):
     check_losses(t, hidden, weight, k >= 0, k.clamp(min=0)[..., None], torch.ones((users, tokens, 1), dtype=torch.float64, device="cuda"), 1.0, loss, lse, c, dhidden, d)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("at,dim", [(0, 72), (1, 136), (2, 8)])
+def test_a_weight_gradient_in_16_bits_that_is_added_to_is_rounded_once(dtype, at, dim):
+    """A weight of zeros: dz is 1/64, or -63/64 at the target, exactly in 16 bits, and sums of whole hidden states up to 255 and of whole numbers up to
+    2000 have 20 bits at most.  So nothing is rounded but what is stored."""
+    g = gen(at)
+    users, tokens, vocab = 2, 60, 64
+    t = b.TokenLoss(vocab, dim, n_users=users, tokens=tokens, dtype=dtype, grad_dtype=dtype)
+    hidden = torch.randint(-255, 256, (users, tokens, dim), generator=g, device="cuda").to(dtype)
+    weight = torch.zeros((vocab, dim), dtype=dtype, device="cuda")
+    k = torch.randint(0, vocab, (users, tokens), generator=g, device="cuda")
+    _, lse = t.loss(hidden, weight, k)
+    rows, part, untouched = rows_for(users, vocab * dim, at, dtype)
+    part.copy_(torch.randint(-2000, 2001, part.shape, generator=g, device="cuda"))
+    dz = 1 / 64 - torch.nn.functional.one_hot(k, vocab).double()
+    want = part.double() + (dz.transpose(1, 2) @ hidden.double()).reshape(users, -1)
+    t.loss_grad(hidden, weight, k, lse, torch.ones((users, tokens), device="cuda"), dweight=part, accumulate=True)
+    assert torch.equal(part, want.float().to(dtype)) and untouched()
+
+
 def test_targets_that_the_vocabulary_does_not_have():
     g = gen(6)
     t = b.TokenLoss(100, 64, tokens=6, top=2)
