@@ -110,7 +110,7 @@ def token_batch(successors, n_users, tokens, gen):
     for t in range(tokens):
         at.append(successors[at[-1], pick[:, t]])
     sequence = torch.stack(at, 1)
-    length = torch.randint(tokens // 2, tokens + 1, (n_users, 1), generator=gen, device="cuda")
+    length = torch.randint(max(1, tokens // 2), tokens + 1, (n_users, 1), generator=gen, device="cuda")
     behind = torch.arange(tokens, device="cuda")[None] >= length
     return sequence[:, :-1].masked_fill(behind, -1), sequence[:, 1:].masked_fill(behind, -1)
 

@@ -844,6 +844,13 @@ def test_the_training_loop_of_tokens(teacher):
     assert rows[:, model.d:].isnan().all()
 
 
+def test_the_training_loop_of_one_token():
+    """A user's only token is always there: no mean over no tokens."""
+    from paper_2203_09044_b200 import train_step
+    for seed in range(3):
+        assert all(math.isfinite(x) for x in train_step.run_tokens(iterations=8, n_users=1, vocab=50, dim=64, tokens=1, seed=seed))
+
+
 # ---- refusals -----------------------------------------------------------------------------------------------------------------
 def refused(call, *errors):
     with pytest.raises(errors or (ValueError, TypeError, b.Co3Error)):
