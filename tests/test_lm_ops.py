@@ -194,6 +194,55 @@ def test_embedding_whose_table_passes_32_bits():
     assert not any(bool(part.any()) for part in table.split(10_000))
 
 
+@pytest.mark.parametrize("dim,at,act,kind", [(1024, 0, BF16, BF16), (1024, 4, F32, F32), (1032, 8, F16, F32), (1032, 1, BF16, F32), (1028, 0, F32, BF16), (1028, 3, F16, F16), (1026, 0, BF16, BF16)])
+@pytest.mark.parametrize("users,skew", [(1, 1.0), (2, 4.0)])
+def test_embedding_gradient_of_many_wide_rows(dim, at, act, kind, users, skew):
+    """Eight, four and two columns a lane: the wider ones are taken from 2368 parts of 32 tokens and 256 (128) columns on, of a device of 148 SMs."""
+    g = gen(dim + at)
+    tokens, vocab = 20001 // users, 3001
+    e = b.Embedding(vocab, dim, n_users=users, tokens=tokens)
+    k = some_tokens(g, users, tokens, vocab, skew=skew)
+    dout = normal(g, users, tokens, dim, dtype=act)
+    dout.masked_fill_((k < 0)[..., None], NAN)
+    want, mag, n = embed_reference(dout, k, vocab, 0.3)
+    rows, part, untouched = rows_for(users, vocab * dim, at, kind)
+    got = part.view(users, vocab, dim) if users == 1 else part.unflatten(1, (vocab, dim))
+    e.backward(dout, k, part, scale=0.3)
+    within(got, want, (n + 2) * U32 * mag, kind)
+    first = part.clone()
+    e.backward(dout, k, part, scale=0.3, accumulate=True)
+    old = first.unflatten(1, (vocab, dim)).double()
+    within(got, old + want, (n + 2) * U32 * mag + U32 * (old.abs() + mag), kind)
+    assert untouched() and e.status() == (0, 0)
+
+
+@pytest.mark.parametrize("tokens,vocab,skew", [(70_001, 100_003, 3.0), (131_077, 700, 1.0), (200_000, 600_011, 2.0)])
+def test_embedding_gradient_of_long_batches(tokens, vocab, skew):
+    """Above 65536 tokens a warp of the sort has more keys than it holds and ranks them twice; two and three passes."""
+    g = gen(tokens)
+    e = b.Embedding(vocab, 8, tokens=tokens)
+    k = some_tokens(g, 1, tokens, vocab, skew=skew)
+    dout = normal(g, 1, tokens, 8)
+    want, mag, n = embed_reference(dout, k, vocab, 1.5)
+    d = torch.full((1, vocab, 8), NAN, device="cuda")
+    e.backward(dout, k, d, scale=1.5)
+    within(d, want, (n + 2) * U32 * mag)
+
+
+@pytest.mark.parametrize("tokens", [3, 300, 4098, 12_000, 70_002, 150_000])
+def test_equal_tokens_are_added_in_their_order(tokens):
+    """Each token stands three times: the sums, to the last bit, are those of the rows one after the other."""
+    g = gen(tokens)
+    vocab = tokens // 3
+    e = b.Embedding(vocab, 6, tokens=tokens)
+    k = torch.randperm(tokens, generator=g, device="cuda") // 3
+    dout = normal(g, tokens, 6) * 10.0 ** torch.randint(-3, 4, (tokens, 1), generator=g, device="cuda")
+    d = torch.empty((vocab, 6), device="cuda")
+    e.backward(dout, k, d)
+    x = dout[k.argsort(stable=True)].view(vocab, 3, 6)
+    assert torch.equal(d, (x[:, 0] + x[:, 1]) + x[:, 2])
+
+
 # ---- layer norm ---------------------------------------------------------------------------------------------------------------
 DIMS = [1, 2, 7, 8, 64, 255, 256, 257, 512, 768, 1000, 1024, 1025, 2048, 3000, 4096, 5000, 8192, 8200, 16384]
 

@@ -119,6 +119,19 @@ def test_embedding_launches(fake, users, n, vocab, dim):
         assert not e("backward", array(data=None), tokens(0, data=None), 0, 1.0, grad(b.F32, vocab * dim, 1), None)
 
 
+@pytest.mark.parametrize("users,n,dim,kind,at,grad_kind,columns", [
+    (1, 20001, 1024, b.BF16, 0, b.BF16, 256), (1, 20001, 1024, b.F32, 4, b.F32, 256), (2, 10000, 1032, b.F16, 8, b.F32, 256),       # eight neighbours a lane
+    (1, 20001, 1032, b.BF16, 1, b.F32, 128), (2, 10000, 1028, b.F32, 0, b.BF16, 128), (1, 20001, 1028, b.F16, 3, b.F16, 128),       # four
+    (1, 20001, 1026, b.BF16, 0, b.BF16, 64), (1, 2000, 1024, b.BF16, 0, b.BF16, 64), (1, 20001, 264, b.BF16, 0, b.BF16, 64),        # two
+    (1, 20001, 1027, b.BF16, 0, b.BF16, 64)])                                                                                       # one and one
+def test_columns_that_a_warp_of_the_embedding_gradient_takes(fake, users, n, dim, kind, at, grad_kind, columns):
+    """The wider ways are taken where rows begin at their multiples and 2368 warps are left: the sizes of the tests that compare their results."""
+    vocab, width = 3001, 4 if grad_kind == b.F32 else 2
+    with Made(fake, "embed", vocab, dim, users, n) as e:
+        seen = e("backward", array(kind, n * dim, dim), tokens(n), n, 1.0, grad(grad_kind, (at + vocab * dim + 9) // 4 * 4, data=A + at * width), None)
+        assert len(seen) == 3 and seen[1].grid[0] == (users * ((n + 31) // 32) * ((dim + columns - 1) // columns) + 7) // 8
+
+
 def test_embedding_calls_that_are_refused(fake):
     with Made(fake, "embed", 100, 16, 2, 10) as e:
         good = [tokens(10), 10, A, b.F32, 1.0, array(b.F32, 160, 16), None]
