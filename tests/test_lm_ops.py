@@ -381,6 +381,59 @@ def test_layer_norm_of_no_rows():
     assert not d.any()
 
 
+# (tokens, dim, type): several rows, and more than are on their way at a time, for each group of threads that the device holds; three users, of whose rows
+# a group's next one may be the next user's
+LONG = [(20_011, 64, BF16), (20_011, 200, F32), (12_007, 768, BF16), (7001, 1001, F32), (7001, 1001, BF16), (7001, 1024, F16), (2503, 4096, BF16), (2503, 4096, F32), (1201, 8192, BF16),
+        (701, 16_384, BF16), (701, 16_384, F32), (701, 16_383, F32)]
+
+
+@pytest.mark.parametrize("tokens,dim,dtype", LONG)
+@pytest.mark.parametrize("how", ["dense", "gaps", "tokens first"])
+def test_layer_norm_of_many_rows(tokens, dim, dtype, how):
+    g = gen(dim)
+    users = 3
+    n = b.LayerNorm(dim, n_users=users)
+    x = strided(g, users, tokens, dim, dtype, how)
+    x.mul_(torch.rand((users, tokens, 1), generator=g, device="cuda").to(dtype) * 3).add_(normal(g, users, tokens, 1, dtype=dtype))
+    w, bias = 1 + 0.3 * normal(g, dim), normal(g, dim)
+    y, mean, rstd = n.forward(x, w, bias)
+    for i in range(users):
+        for at in range(0, tokens, 2000):                 # bounds as in test_layer_norm
+            part = x[i, at:at + 2000].double()
+            m, r, xhat, want = norm_reference(part, w, bias, 1e-5)
+            mag = part.abs().mean(-1)
+            e_mean = (dim + 2) * U32 * mag
+            within(mean[i, at:at + 2000], m, e_mean)
+            shift = e_mean + U32 * (m.abs() + mag)
+            e_var = 2 * shift * (shift + (r ** -2).sqrt() * 2 * U32) + (dim + 6) * U32 * r ** -2
+            e_r = 0.5 * r ** 3 * e_var + 4 * U32 * r
+            within(rstd[i, at:at + 2000], r, e_r)
+            e_x = (part - m[..., None]).abs()
+            bound = w.double().abs() * (r[..., None] * (shift + U32 * e_x.amax(-1))[..., None] + (e_r + 2 * U32 * r)[..., None] * e_x) + 2 * U32 * (want.abs() + bias.double().abs())
+            within(y[i, at:at + 2000], want, bound, dtype)
+    dy, dw, db = normal(g, users, tokens, dim, dtype=dtype), torch.empty((users, dim), device="cuda"), torch.empty((users, dim), device="cuda")
+    dx = n.backward(dy, x, w, mean, rstd, dweight=dw, dbias=db)
+    for i in range(users):
+        sums = [torch.zeros(dim, dtype=torch.float64, device="cuda") for _ in range(5)]
+        for at in range(0, tokens, 2000):                 # bounds as in test_layer_norm_gradient
+            g2, x2, m2, r2 = dy[i, at:at + 2000], x[i, at:at + 2000], mean[i, at:at + 2000], rstd[i, at:at + 2000]
+            xhat, gain, c1, c2, want = grad_reference(g2, x2, w, m2, r2)
+            e_hat = 2 * U32 * r2.double()[..., None] * (x2.double().abs() + m2.double().abs()[..., None])
+            g1, gx = gain.abs().mean(-1, keepdim=True), (gain * xhat).abs().mean(-1, keepdim=True)
+            e_c1, e_c2 = (dim + 3) * U32 * g1, (dim + 4) * U32 * gx + (gain.abs() * e_hat).mean(-1, keepdim=True)
+            bound = r2.double()[..., None] * (3 * U32 * (gain.abs() + c1.abs() + (xhat * c2).abs()) + e_c1 + xhat.abs() * e_c2 + e_hat * c2.abs())
+            within(dx[i, at:at + 2000], want, bound, dtype)
+            d = g2.double()
+            for s, more in zip(sums, ((d * xhat).sum(0), (d * xhat).abs().sum(0), (d.abs() * e_hat).sum(0), d.sum(0), d.abs().sum(0))):
+                s.add_(more)
+        within(dw[i], sums[0], (tokens + 2) * U32 * sums[1] + sums[2])
+        within(db[i], sums[3], (tokens + 2) * U32 * sums[4])
+    # in place, with rows of it on their way
+    assert torch.equal(n.backward(dy, x, w, mean, rstd, dx=dy), dx)
+    other, m, r = n.forward(x, w, bias, y=x)
+    assert other is x and torch.equal(x, y) and torch.equal(m, mean) and torch.equal(r, rstd)
+
+
 # ---- losses -------------------------------------------------------------------------------------------------------------------
 def loss_reference(hidden, weight, index, q, tau):
     """Everything in 64 bits for one user's tokens that count.  index [n][k] with shares q [n][k]; (loss, lse, dz / c, error of a logit)."""
