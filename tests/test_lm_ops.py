@@ -684,6 +684,80 @@ def test_a_weight_that_passes_32_bits(at):
     assert bool((memory[:at] == 7).all()) and bool((memory[at + vocab * dim:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype,kind", [(BF16, F32), (BF16, BF16), (F16, F32), (F16, F16)])
+@pytest.mark.parametrize("tokens,vocab,dim", [(300, 20_011, 2056), (2500, 2603, 1032)])
+def test_losses_of_many_deep_tiles(tokens, vocab, dim, dtype, kind):
+    """More tiles than pairs of SMs, and a depth that accumulators take in an odd number of parts: of the logits (33 stages of 64), and of the weight's gradient
+    (users of different lengths, the longer of over 1024 tokens)."""
+    g = gen(tokens)
+    users = 2
+    t = b.TokenLoss(vocab, dim, n_users=users, tokens=tokens, dtype=dtype, grad_dtype=kind)
+    hidden, weight = normal(g, users, tokens, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype).mul_(2.0 / math.sqrt(dim))
+    k = some_targets(g, users, tokens, vocab, none=0.1)
+    k[1, tokens // 2:] = -1
+    there = k >= 0
+    hidden.masked_fill_(~there[..., None], NAN)
+    loss, lse = t.loss(hidden, weight, k)
+    c = 0.1 + torch.rand((users, tokens), generator=g, device="cuda")
+    for at in (0, 1):                                     # by TMA, and through shared memory
+        rows, part, untouched = rows_for(users, vocab * dim, at, kind)
+        dhidden = t.loss_grad(hidden, weight, k, lse, c, dweight=part)
+        check_losses(t, hidden, weight, there, k.clamp(min=0)[..., None], torch.ones((users, tokens, 1), dtype=torch.float64, device="cuda"), 1.0, loss, lse, c, dhidden,
+                     part.unflatten(1, (vocab, dim)), kind)
+        assert untouched() and t.status() == (0, 0)
+
+
+def test_rows_of_a_weight_that_passes_32_bits():
+    """Of 4.6e9 elements three rows are not zero, the first, one in the middle and the last: their logits are whole numbers."""
+    vocab, dim = 70_001, 65_536
+    t = b.TokenLoss(vocab, dim, tokens=3, dtype=BF16, grad_dtype=BF16)
+    weight, hidden = torch.zeros((vocab, dim), dtype=BF16, device="cuda"), torch.ones((3, dim), dtype=BF16, device="cuda")
+    rows = {0: 1.0, 35_003: -2.0, vocab - 1: 3.0}
+    for v, z in rows.items():
+        weight[v] = z / dim
+    k = torch.tensor([vocab - 1, 35_003, 17], device="cuda")
+    loss, lse = t.loss(hidden, weight, k)
+    want = math.log(vocab - 3 + sum(math.exp(z) for z in rows.values()))
+    # sums of 65536 equal products: each cut off at 16 of depth, 64 parts of 1024 added in 32 bits
+    e = (64 + 67) * 2 * U32 * 3.0 + 40 * U32 * want
+    assert (lse.double() - want).abs().max() <= e
+    assert (loss.double() - (want - torch.tensor([3.0, -2.0, 0.0], device="cuda").double())).abs().max() <= 2 * e
+    d = torch.empty((vocab, dim), dtype=BF16, device="cuda")
+    dhidden = t.loss_grad(hidden, weight, k, lse, torch.ones(3, device="cuda"), dweight=d)
+    # logits of the gradient call are one sum: 4096 parts of 16 of depth
+    e = 4096 * 2 * U32 * 3.0 + e
+    at = torch.tensor([0, 1, 17, 35_002, 35_003, 35_004, vocab - 2, vocab - 1], device="cuda")
+    p = torch.tensor([math.exp(rows.get(int(v), 0.0) - want) for v in at], device="cuda").double()
+    dz = p - (at == k[:, None]).double()                  # [3][8]
+    e_dz = p * e + u(BF16) * (dz.abs() + p * e) + 2.0 ** -20 * p
+    got = d[at].double()
+    assert bool((got == got[:, :1]).all())                # all hidden states are 1
+    assert ((got[:, 0] - dz.sum(0)).abs() <= e_dz.sum(0) * 1.01 + u(BF16) * dz.sum(0).abs() * 1.01).all()
+    some = [0, 4, 7]                                      # the rows that are not zero
+    w = torch.tensor(list(rows.values()), device="cuda").double() / dim
+    h = (dz[:, some] * w).sum(1, keepdim=True)
+    room = (e_dz[:, some] * w.abs()).sum(1, keepdim=True) * 1.01 + (vocab / 16) * 2 * U32 * (dz[:, some] * w).abs().sum(1, keepdim=True) + u(BF16) * h.abs() * 1.01
+    assert ((dhidden.double() - h).abs() <= room).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shape", SHAPES + [(2, 300, 20_011, 2056)])
+def test_cross_entropy_to_a_few_roundings(shape, dtype):
+    """One exact entry: the loss is off by what lse and the target's logit are, and the difference's rounding."""
+    users, tokens, vocab, dim = shape
+    g = gen(sum(shape) + 1)
+    t = b.TokenLoss(vocab, dim, n_users=users, tokens=tokens, dtype=dtype)
+    hidden, weight = normal(g, users, tokens, dim, dtype=dtype), normal(g, vocab, dim, dtype=dtype).mul_(2.0 / math.sqrt(dim))
+    k = torch.randint(0, vocab, (users, tokens), generator=g, device="cuda")
+    loss, lse = t.loss(hidden, weight, k)
+    for i in range(users):
+        want, want_lse, _, e_z, dense, z = loss_reference(hidden[i], weight, k[i][:, None], torch.ones((tokens, 1), dtype=torch.float64, device="cuda"), 1.0)
+        # the largest logit over the logarithm's and the exponents' conversion to powers of two and back; a tile's 64 and the tiles' sums
+        e_lse = e_z.amax(1) + 8 * U32 * (want_lse.abs() + z.abs().amax(1)) + (vocab // 64 + 80) * U32
+        within(lse[i], want_lse, e_lse)
+        within(loss[i], want, e_lse + (dense * e_z).sum(1) + U32 * want.abs())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_logits_far_apart(dtype):
     """Logits of hundreds: exponentials of differences only, losses of 0 and of hundreds."""
