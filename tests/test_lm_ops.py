@@ -974,6 +974,20 @@ def test_the_chain_on_other_streams_and_replayed():
     assert c.t.status() == c.e.status() == (0, 0)
 
 
+def test_a_chain_on_another_stream_whose_rows_were_filled_before():
+    """The fill is ordered before the side stream's work, and the rows are those of the first run."""
+    c = Chain(4)
+    want = [x.clone() for x in c.run()]
+    rows = [part.clone() for part in c.parts]
+    for fill in (NAN, 3.0):
+        c.rows.fill_(fill)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = c.run(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(x, y) for x, y in zip(want, got)) and all(torch.equal(x, y) for x, y in zip(rows, c.parts))
+
+
 def test_outputs_are_marked_as_changed():
     c = Chain(3)
     before = c.rows._version
