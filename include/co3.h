@@ -566,7 +566,8 @@ int64_t co3_layernorm_launch_count(const co3_layernorm* h);
  *   dz_v = c / tau (exp(z_v / tau - lse) - q_v);   dhidden = dz weight;   dweight[u] = sum over the user's tokens of dz_v hidden
  * hidden, weight and dhidden have the handle's type (bf16 or f16: what the tensor cores take).  dz is rounded to that type before the two
  * products; for dweight in 32 bits its remainder is carried along in a second number of that type (2^-17 of dz in bf16), which costs a
- * second product.  Products are summed in 32 bits.  Exponentials below 2^-126 count as 0.  f16: dz is scaled by a power of two per user, so that none is lost below 2^-24.
+ * second product.  Products are summed in 32 bits.  Exponentials below 2^-126 count as 0.  f16: dz is scaled by a power of two per user
+ * that brings the largest |c / tau| to 2^13 .. 2^14: beside its rounding a dz is off by up to 2^-38 of that factor, and 0 where it is smaller.
  * weight: device, vocab rows, weight_stride elements apart; its address and the stride are multiples of 16 bytes, dim is a multiple of 8.
  * loss, lse, dloss: device f32 [n_users][n_tokens].  lse is what the forward call gave for the same inputs.  dhidden, dweight: NULL where
  * not wanted.  top from 1 to max_top, which is at most 128.  tau from 1e-30 to 1e30 (1 for cross entropy), scale / tau finite.

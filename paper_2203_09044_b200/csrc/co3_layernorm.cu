@@ -80,7 +80,8 @@ template <int TPR, class V> __device__ __forceinline__ V row_sum(V x, RowSum<TPR
     }
 }
 
-// How rows are read: in whole 16 bytes; in words (f32 rows that begin anywhere, or of an odd length); element by element.
+// How rows are read: in whole 16 bytes; in words (f32 rows that begin anywhere, or of an odd length); element by element (16 bits, likewise: 65536 x
+// 1001 bf16 78 us forward and 124 backward, x 1000 in whole 16 bytes 48 and 83).
 enum Take { WHOLE, WORDS, SINGLES };
 
 // The elements that a thread holds of a row: E / V pieces of V neighbours, piece c at column (c TPR + t) V.  AHEAD: rows that are on
